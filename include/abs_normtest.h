@@ -48,7 +48,11 @@ extern "C" {
 
 typedef void* abs_stream_t; /* a cudaStream_t */
 
-typedef enum { ABS_F32 = 0, ABS_BF16 = 1 } abs_dtype;
+typedef enum {
+  ABS_F32 = 0,
+  ABS_BF16 = 1,
+  ABS_F16 = 2 /* only in abs_tensor lists; the calls on flat vectors answer ABS_ERR_DTYPE */
+} abs_dtype;
 
 typedef enum {
   ABS_OK = 0,
@@ -478,6 +482,109 @@ int abs_schedule_init(abs_schedule* s, int64_t J, int64_t M, int64_t micro0, int
 int abs_schedule_test_due(const abs_schedule* s);
 /* Returns ABS_OK, ABS_ERR_NULL, or ABS_ERR_RANGE (b_test < 1; the state is then unchanged). */
 int abs_schedule_advance(abs_schedule* s, int64_t b_test);
+
+/*
+ * ---- Lists of tensors -------------------------------------------------------------------
+ * A model's gradients as the backward pass leaves them: a list of tensors of different sizes and
+ * types, some of them views, instead of one flat vector.  Three calls work on such a list: the
+ * global norm, clipping by it, and AdamW on the clipped gradients (Sec. 5 "gradient clipping";
+ * "Gradient clipping 1.0" in the hyper-parameter tables of Appendix C).
+ *
+ *   x_t,i        element i of tensor t, and s = grad_scale, a factor known before the call
+ *                (1/micro-batches, 1/loss scale; finite, not 0)
+ *   N_t          the norm of s*x_t:  (sum_i |s x_t,i|^p)^(1/p) for p = 1, 2, or max_i |s x_t,i|
+ *   N            the same norm over all tensors, (sum_t N_t^p)^(1/p) or max_t N_t
+ *   c            min(1, max_norm / (N + 1e-6)), the clipping coefficient
+ *
+ * A list is described once by a plan (host memory of the caller) and a work area (device memory
+ * of the caller) that the plan is uploaded to; then each call is one or two launches.  Both hold
+ * the addresses of the tensors, which must stay where they are while the plan is in use.  One
+ * work area serves one call at a time: calls on it have to be ordered (one stream, or events).
+ *
+ * Range and accuracy: sums are held in fp64 (fp32 within 16 bytes of input); the norm of finite
+ * gradients is right also where their fp32 squares overflow or vanish.  Results do not depend on
+ * the order in which blocks run.  A norm that is not finite (a NaN or infinite gradient) raises
+ * ABS_FLAG_NONFINITE in the header; c is then 1 and AdamW leaves params, m and v as they are.
+ */
+typedef struct {
+  void* data;         /* device, aligned to its element size; may be NULL when numel = 0          */
+  int64_t numel;      /* >= 0                                                                      */
+  int64_t row_len;    /* 0: the elements are contiguous (the strides are not looked at).  Else     */
+  int64_t row_stride; /* numel is a multiple of row_len <= 2^30 and element i lies at              */
+  int64_t col_stride; /* (i / row_len) * row_stride + (i % row_len) * col_stride: columns of a     */
+                      /* matrix, a transposed matrix.  No two elements may lie at one place.       */
+  int32_t dtype;      /* an abs_dtype                                                              */
+  int32_t group;      /* in `grads`: which hyper-parameters AdamW uses, 0..ABS_MAX_GROUPS-1        */
+} abs_tensor;
+
+enum { ABS_MAX_GROUPS = 16, ABS_MAX_TENSORS = 1 << 20 };
+typedef enum { ABS_NORM_MAX = 0, ABS_NORM_1 = 1, ABS_NORM_2 = 2 } abs_norm_type;
+
+/* First ABS_STATS_HEADER doubles of a work area after a call that computed a norm.  SUM is what
+ * ranks that hold different tensors add up (maximum: take the maximum of): it is free of
+ * grad_scale and lies where abs_adamw_step_clipped looks for ||gbar||^2.  FLAGS is ABS_STAT_FLAGS. */
+enum {
+  ABS_GRAD_SUM = 0,  /* sum |x|^p over all tensors, or max |x|   */
+  ABS_GRAD_NORM = 1, /* N                                        */
+  ABS_GRAD_COEF = 2, /* c (1 when max_norm was 0)                */
+  ABS_GRAD_FLAGS = 4 /* ABS_FLAG_NONFINITE or 0                  */
+};
+
+/*
+ * The plan of a list of n tensors.  Host, no CUDA call.
+ *   grads         n tensors, any abs_dtype, mixed
+ *   outs          n tensors of the same sizes, any abs_dtype: abs_grad_clip writes them; NULL: it
+ *                 scales the gradients in place
+ *   params, m, v  n contiguous ABS_F32 tensors of the same sizes, or all three NULL: what
+ *                 abs_grad_adamw updates
+ *   params_bf16   n contiguous ABS_BF16 tensors for the copy of the updated parameters, or NULL
+ *   plan          abs_tensors_plan_bytes(grads, n) bytes, 8-byte aligned
+ * Elements correspond by their index i, whatever the rows.  n = 0 and empty tensors are allowed.
+ * No output may share an element with a gradient or another output (ABS_ERR_ALIAS).  Gradients may
+ * overlap each other unless abs_grad_clip is to scale them in place (it answers ABS_ERR_ALIAS).
+ * ABS_ERR_TOO_LARGE: plan_bytes is too small, or the host is out of memory.
+ */
+size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n);
+int abs_tensors_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor* params,
+                     const abs_tensor* m, const abs_tensor* v, const abs_tensor* params_bf16, int n,
+                     void* plan, size_t plan_bytes);
+/* Bytes of the work area of a plan; 0 if it is none. */
+size_t abs_tensors_work_bytes(const void* plan);
+/* Prepares a work area (16-byte aligned): once after planning, and again after a call that
+ * returned ABS_ERR_CUDA.  Copies from pageable host memory, so not while capturing a graph. */
+int abs_tensors_upload(const void* plan, void* work, abs_stream_t stream);
+
+/*
+ * The global norm and the norm of each tensor.
+ *   norm_type   an abs_norm_type
+ *   max_norm    > 0: c is computed as well; 0: it is reported as 1
+ *   norms_out   device, n + 2 floats: {N, c, N_0 .. N_(n-1)}
+ * One launch.  Bound by reading the gradients once.
+ */
+int abs_grad_norm(const void* plan, void* work, int norm_type, double grad_scale, double max_norm,
+                  float* norms_out, abs_stream_t stream);
+
+/*
+ * Clipping by the global norm: y = (s c) x, rounded once to the type of y.  y is the gradient
+ * itself, or the plan's `outs`.  max_norm finite, > 0.
+ *   sum_in   NULL: the call computes the norm first (norms_out as above).  Else a double in device
+ *            memory, the SUM over this and other ranks' tensors: no norm is computed, norms_out[0]
+ *            and [1] and the header follow from it, norms_out[2..] are left.
+ * In place, gradients are written only where s c differs from 1 (in fp32).
+ */
+int abs_grad_clip(const void* plan, void* work, int norm_type, double grad_scale, double max_norm,
+                  const double* sum_in, float* norms_out, abs_stream_t stream);
+
+/*
+ * AdamW on clipped gradients: abs_adamw_step for every tensor with g = (s c) x, which stays in
+ * registers; the gradients are not written.
+ *   hparams    host, n_groups entries (1..ABS_MAX_GROUPS); tensor t uses entry grads[t].group
+ *   max_norm   > 0: as abs_grad_clip, sum_in too; 0: no norm is computed, c = 1, sum_in and
+ *              norms_out are left alone
+ */
+int abs_grad_adamw(const void* plan, void* work, const abs_adamw_hparams* hparams, int n_groups,
+                   int64_t step, int norm_type, double grad_scale, double max_norm,
+                   const double* sum_in, float* norms_out, abs_stream_t stream);
 
 /*
  * Self-test of the bounded waits (no counterpart in the paper).  The staged kernels wait for

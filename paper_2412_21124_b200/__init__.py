@@ -3,7 +3,9 @@
 The product is the CUDA shared library behind ``include/abs_normtest.h``; this package
 is its thin Python binding plus the seeded synthetic-input generators.
 """
-from .binding import (ABS_BF16, ABS_F32, ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE,  # noqa: F401
+from .binding import (ABS_BF16, ABS_F16, ABS_F32, ABS_GRAD_COEF, ABS_GRAD_FLAGS,
+                      ABS_GRAD_NORM, ABS_GRAD_SUM, GradTensors, abs_grad_adamw, abs_grad_clip,
+                      abs_grad_norm, ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE,  # noqa: F401
                       ABS_FLAG_VIOLATED, AbsError, FusedStep, abs_adamw_hparams, abs_adamw_step, abs_adamw_step_clipped,
                       abs_adamw_step_mixed, abs_normtest_adamw_mixed,
                       abs_decide, abs_combine_sums, abs_noalloc_fits,

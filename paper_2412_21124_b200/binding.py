@@ -6,13 +6,14 @@ name.  All arithmetic of the path runs in the CUDA kernels of ``libabs_normtest.
 There is no CPU fallback: if the library has not been built, the first call raises.
 """
 import ctypes
+import math
 import os
 
 import torch
 
 from . import build as _build
 
-ABS_F32, ABS_BF16 = 0, 1
+ABS_F32, ABS_BF16, ABS_F16 = 0, 1, 2
 ABS_OK = 0
 ABS_ERR_NULL, ABS_ERR_RANGE, ABS_ERR_SHARDS, ABS_ERR_ALIGN, ABS_ERR_DTYPE, ABS_ERR_CUDA = (
     -1, -2, -3, -4, -5, -6)
@@ -24,11 +25,20 @@ ABS_MAX_WORKERS, ABS_MAX_SHARDS = 1024, 128
  ABS_STAT_NCHUNKS, ABS_STAT_ARGMAX) = range(8)
 ABS_STATS_HEADER, ABS_SHARD_STRIDE = 8, 4
 ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE, ABS_FLAG_VIOLATED = 1, 2, 4
+ABS_MAX_GROUPS, ABS_MAX_TENSORS = 16, 1 << 20
+ABS_NORM_MAX, ABS_NORM_1, ABS_NORM_2 = 0, 1, 2
+ABS_GRAD_SUM, ABS_GRAD_NORM, ABS_GRAD_COEF, ABS_GRAD_FLAGS = 0, 1, 2, 4
 
 
 class abs_adamw_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class abs_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("row_len", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("col_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("group", ctypes.c_int32)]
 
 
 class AbsError(RuntimeError):
@@ -110,6 +120,20 @@ def lib():
     L.abs_schedule_test_due.argtypes = [ptr]
     L.abs_schedule_advance.restype = cint
     L.abs_schedule_advance.argtypes = [ptr, i64]
+    L.abs_tensors_plan_bytes.restype = sz
+    L.abs_tensors_plan_bytes.argtypes = [ptr, cint]
+    L.abs_tensors_plan.restype = cint
+    L.abs_tensors_plan.argtypes = [ptr, ptr, ptr, ptr, ptr, ptr, cint, ptr, sz]
+    L.abs_tensors_work_bytes.restype = sz
+    L.abs_tensors_work_bytes.argtypes = [ptr]
+    L.abs_tensors_upload.restype = cint
+    L.abs_tensors_upload.argtypes = [ptr, ptr, ptr]
+    L.abs_grad_norm.restype = cint
+    L.abs_grad_norm.argtypes = [ptr, ptr, cint, dbl, dbl, ptr, ptr]
+    L.abs_grad_clip.restype = cint
+    L.abs_grad_clip.argtypes = [ptr, ptr, cint, dbl, dbl, ptr, ptr, ptr]
+    L.abs_grad_adamw.restype = cint
+    L.abs_grad_adamw.argtypes = [ptr, ptr, ptr, cint, i64, cint, dbl, dbl, ptr, ptr, ptr]
     L.abs_selftest_bounded_wait.restype = cint
     L.abs_selftest_bounded_wait.argtypes = [cint, ptr, ptr]
     L.abs_status_string.restype = ctypes.c_char_p
@@ -559,6 +583,212 @@ def abs_persample_norm_test_coordwise(G, eta, stats_out, gbar_out, b_next_out, s
     the column in the ABS_STAT_ARGMAX slot)."""
     abs_persample_norm_test(G, eta, stats_out, gbar_out, b_next_out, stream,
                             _entry="abs_persample_norm_test_coordwise")
+
+
+# ---------------------------------------------------------------------- lists of tensors
+_TENSOR_DTYPES = {torch.float32: ABS_F32, torch.bfloat16: ABS_BF16, torch.float16: ABS_F16}
+_NORM_TYPES = {2: ABS_NORM_2, 1: ABS_NORM_1, math.inf: ABS_NORM_MAX}
+
+
+def _rows(t, order, name):
+    """(row_len, row_stride, col_stride) of a tensor whose dimensions are walked in `order`, zeros
+    when its elements are contiguous in that order."""
+    dims = []  # (size, stride), outer first, neighbours merged
+    for d in order:
+        size, stride = t.shape[d], t.stride(d)
+        if size == 1:
+            continue
+        if dims and dims[-1][1] == size * stride:
+            dims[-1] = (dims[-1][0] * size, stride)
+        else:
+            dims.append((size, stride))
+    if not dims or (len(dims) == 1 and dims[0][1] == 1):
+        return 0, 0, 0
+    if len(dims) == 1:
+        dims.append((1, 1))  # a column: rows of one element
+    if len(dims) > 2 or dims[0][1] == 0 or dims[1][1] == 0:
+        raise TypeError("%s: strides %s of shape %s are not those of a matrix"
+                        % (name, tuple(t.stride()), tuple(t.shape)))
+    return dims[1][0], dims[0][1], dims[1][1]
+
+
+def _tensor_array(tensors, orders, name, dtypes, groups=None, dense=False):
+    """The abs_tensor array of one role."""
+    arr = (abs_tensor * max(len(tensors), 1))()
+    for i, t in enumerate(tensors):
+        code = _TENSOR_DTYPES.get(t.dtype)
+        if code not in dtypes:
+            raise TypeError("%s[%d] must not be %s" % (name, i, t.dtype))
+        rows = (0, 0, 0)
+        if t.numel() and not (orders[i] is None and t.is_contiguous()):
+            rows = _rows(t, orders[i] or range(t.dim()), "%s[%d]" % (name, i))
+            if dense and rows[0]:
+                raise TypeError("%s[%d] must be dense, in the order of params[%d]" % (name, i, i))
+        arr[i] = abs_tensor(t.data_ptr() or None, t.numel(), *rows, code, groups[i] if groups else 0)
+    return arr
+
+
+class GradTensors:
+    """A list of gradient tensors (and what goes with them), for abs_grad_norm, abs_grad_clip and
+    abs_grad_adamw.
+
+      grads        CUDA tensors of any shapes, float32 / bfloat16 / float16 mixed: dense in any
+                   order of dimensions, or with the strides of a matrix once neighbouring dimensions
+                   are merged (columns of a wider matrix, a transposed one).  Empty ones are fine.
+      out          same shapes, any of the types: abs_grad_clip writes there; None: in place
+      params, m, v float32, same shapes, dense, all three in one order of dimensions: updated by
+                   abs_grad_adamw, with the hyper-parameters of groups[i] (None: all group 0)
+      params_bf16  bfloat16, the same: receives the copy of the updated parameters
+
+    The object keeps the plan of the list and its work area, and the results of the latest call:
+    `norm` (global norm, one float32), `coef` (clipping coefficient), `norms` (one per tensor).
+    Built once for tensors that stay where they are (a training loop's buckets and state); build
+    another when a gradient moves.  Calls on one object have to be ordered: one stream, or events
+    between streams."""
+
+    def __init__(self, grads, out=None, params=None, m=None, v=None, params_bf16=None, groups=None):
+        grads = list(grads)
+        roles = {"out": out, "params": params, "m": m, "v": v, "params_bf16": params_bf16}
+        roles = {k: list(x) if x is not None else None for k, x in roles.items()}
+        n = len(grads)
+        if n > ABS_MAX_TENSORS:
+            raise ValueError("at most %d tensors" % ABS_MAX_TENSORS)
+        given = [roles[k] is not None for k in ("params", "m", "v")]
+        if any(given) != all(given) or (roles["params_bf16"] is not None and not given[0]):
+            raise ValueError("params, m and v go together, params_bf16 with them")
+        for name, x in roles.items():
+            if x is None:
+                continue
+            if len(x) != n:
+                raise ValueError("%s: %d tensors for %d gradients" % (name, len(x), n))
+            for i, (t, g) in enumerate(zip(x, grads)):
+                if t.shape != g.shape:
+                    raise ValueError("%s[%d] has shape %s, its gradient %s"
+                                     % (name, i, tuple(t.shape), tuple(g.shape)))
+        groups = [0] * n if groups is None else [int(k) for k in groups]
+        if len(groups) != n or any(not 0 <= k < ABS_MAX_GROUPS for k in groups):
+            raise ValueError("groups: one number in 0..%d per tensor" % (ABS_MAX_GROUPS - 1))
+        self._keep = (grads, roles)
+        _check_one_device(*grads, *(t for x in roles.values() if x is not None for t in x))
+        # the order in which a tensor's dimensions are walked: the parameter's own, else the
+        # gradient's, largest stride first (None: the order of the shape)
+        orders = [None if x.is_contiguous() else
+                  sorted(range(x.dim()), key=lambda d: (-x.stride(d), d))
+                  for x in (roles["params"] or grads)]
+        every = (ABS_F32, ABS_BF16, ABS_F16)
+        arrays = {"grads": _tensor_array(grads, orders, "grads", every, groups)}
+        for name, dtypes, dense in (("out", every, False), ("params", (ABS_F32,), True),
+                                    ("m", (ABS_F32,), True), ("v", (ABS_F32,), True),
+                                    ("params_bf16", (ABS_BF16,), True)):
+            x = roles[name]
+            arrays[name] = None if x is None else _tensor_array(x, orders, name, dtypes, None, dense)
+        nbytes = lib().abs_tensors_plan_bytes(arrays["grads"], n)
+        self._plan = (ctypes.c_uint64 * (nbytes // 8 + 1))()
+        rc = lib().abs_tensors_plan(*(arrays[k] for k in ("grads", "out", "params", "m", "v",
+                                                          "params_bf16")), n, self._plan, nbytes)
+        if rc != ABS_OK:
+            raise AbsError(rc, "abs_tensors_plan")
+        self._adam = roles["params"] is not None
+        self.n_groups = max(groups, default=0) + 1
+        self._device = torch.cuda.current_device()
+        self._plan_ptr = ctypes.addressof(self._plan)
+        self._work = torch.empty(lib().abs_tensors_work_bytes(self._plan_ptr), dtype=torch.uint8,
+                                 device="cuda")
+        self._results = torch.empty(n + 2, dtype=torch.float32, device="cuda")
+        self.norm, self.coef, self.norms = self._results[0], self._results[1], self._results[2:]
+        self._work_ptr, self._results_ptr = self._work.data_ptr(), self._results.data_ptr()
+        rc = lib().abs_tensors_upload(self._plan_ptr, self._work_ptr, _stream(None))
+        if rc != ABS_OK:
+            raise AbsError(rc, "abs_tensors_upload")
+        self._uploaded_on = torch.cuda.current_stream().cuda_stream
+        self._uploaded = torch.cuda.Event()
+        self._uploaded.record()
+        self._hparams, self._hparams_of = None, None
+
+    @property
+    def header(self):
+        """The ABS_GRAD_* slots (float64, device); header[ABS_GRAD_SUM] is what ranks add up."""
+        return self._work[:8 * ABS_STATS_HEADER].view(torch.float64)
+
+    def _enter(self, stream):
+        """The stream of a call, as a number; a stream other than the one the plan was uploaded on
+        first waits for the upload."""
+        if stream is None:
+            raw = torch.cuda.current_stream().cuda_stream
+        else:
+            raw = _stream(stream).value or 0
+        if raw != self._uploaded_on and not torch.cuda.is_current_stream_capturing():
+            other = torch.cuda.ExternalStream(raw)
+            other.wait_event(self._uploaded)
+            self._work.record_stream(other)
+            self._results.record_stream(other)
+        return raw
+
+    def _groups(self, hparams):
+        """The hyper-parameters of all groups as a C array, kept while they are the same values."""
+        if isinstance(hparams, (dict, abs_adamw_hparams)):
+            hparams = [hparams]
+        key = [tuple(h.values()) if isinstance(h, dict) else
+               (h.lr, h.beta1, h.beta2, h.eps, h.weight_decay) for h in hparams]
+        if key != self._hparams_of:
+            if len(hparams) < self.n_groups:
+                raise ValueError("hparams for %d groups are needed" % self.n_groups)
+            self._hparams = (abs_adamw_hparams * len(hparams))(*[_hparams(h) for h in hparams])
+            self._hparams_of = key
+        return self._hparams
+
+
+def _norm_type(norm_type):
+    code = _NORM_TYPES.get(norm_type)
+    if code is None:
+        raise ValueError("norm_type must be 2, 1 or inf, got %r" % (norm_type,))
+    return code
+
+
+def _sum_in(sum_in):
+    if sum_in is None:
+        return None
+    if not sum_in.is_cuda or sum_in.dtype != torch.float64 or sum_in.numel() < 1:
+        raise TypeError("sum_in must be a CUDA float64 tensor")
+    return sum_in.data_ptr()
+
+
+def abs_grad_norm(tensors, norm_type=2, grad_scale=1.0, max_norm=0.0, stream=None):
+    """The global norm of grad_scale times the gradients (`tensors`: a GradTensors) and the norm of
+    each, and with max_norm > 0 the clipping coefficient.  Returns the global norm, a view of the
+    object's results."""
+    rc = lib().abs_grad_norm(tensors._plan_ptr, tensors._work_ptr, _norm_type(norm_type), grad_scale,
+                             max_norm, tensors._results_ptr, tensors._enter(stream))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_grad_norm")
+    return tensors.norm
+
+
+def abs_grad_clip(tensors, max_norm, norm_type=2, grad_scale=1.0, sum_in=None, stream=None):
+    """Scales the gradients by grad_scale * min(1, max_norm / (norm + 1e-6)), in place or into the
+    object's `out`.  `sum_in`: the power sum over all ranks instead of this list's own norm.
+    Returns the global norm, a view of the object's results."""
+    rc = lib().abs_grad_clip(tensors._plan_ptr, tensors._work_ptr, _norm_type(norm_type), grad_scale,
+                             max_norm, _sum_in(sum_in), tensors._results_ptr,
+                             tensors._enter(stream))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_grad_clip")
+    return tensors.norm
+
+
+def abs_grad_adamw(tensors, hparams, step, max_norm=0.0, norm_type=2, grad_scale=1.0, sum_in=None,
+                   stream=None):
+    """AdamW on the gradients scaled by grad_scale and, with max_norm > 0, clipped by their global
+    norm.  `hparams`: one dict for all tensors or a list with one per group.  An update whose norm
+    is not finite is left out.  Returns the global norm, a view of the object's results (not
+    written when max_norm is 0)."""
+    hp = tensors._groups(hparams)
+    rc = lib().abs_grad_adamw(tensors._plan_ptr, tensors._work_ptr, hp, len(hp), step,
+                              _norm_type(norm_type), grad_scale, max_norm, _sum_in(sum_in),
+                              tensors._results_ptr, tensors._enter(stream))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_grad_adamw")
+    return tensors.norm
 
 
 def abs_decide(S, n2, norm, eta, b_cur):

@@ -9,6 +9,7 @@
 #include <unordered_map>
 #include <utility>
 
+#include "host_checks.cuh"
 #include "launch.cuh"
 #include "normtest_accumulate.cuh"
 #include "persample.cuh"
@@ -34,13 +35,15 @@ ABS_DECLARE_STREAM(BF16, false, kStatCoordwise)
 }  // namespace absnt
 
 namespace {
-
 thread_local int g_last_cuda_error = 0;
+}  // namespace
 
-int cuda_fail(cudaError_t e) {
+int absnt::cuda_fail(cudaError_t e) {
   g_last_cuda_error = static_cast<int>(e);
   return ABS_ERR_CUDA;
 }
+
+namespace {
 
 // Elements per reduction chunk (= the work of one CTA).  A function of the problem (d and
 // the entry point) alone, so that the summation tree -- and with it every output bit --
@@ -50,34 +53,6 @@ int cuda_fail(cudaError_t e) {
 // 8192).  abs_stats_bytes sizes the scratch for the smaller of the two.
 int chunk_elems_for(int64_t d, bool fused) {
   return d >= (int64_t{1} << 23) ? (fused ? 8192 : 16384) : 4096;
-}
-
-bool finite_nonneg(float x) { return std::isfinite(x) && x >= 0.f; }
-
-int check_hparams(const abs_adamw_hparams* h, int64_t step) {
-  if (!h) return ABS_ERR_NULL;
-  if (step < 1) return ABS_ERR_RANGE;
-  if (!finite_nonneg(h->lr) || !finite_nonneg(h->eps) || !finite_nonneg(h->weight_decay))
-    return ABS_ERR_RANGE;
-  if (!(h->beta1 >= 0.f && h->beta1 < 1.f) || !(h->beta2 >= 0.f && h->beta2 < 1.f))
-    return ABS_ERR_RANGE;
-  return ABS_OK;
-}
-
-AdamScalars make_adam(const abs_adamw_hparams* h, int64_t step) {
-  AdamScalars a;
-  const double b1 = h->beta1, b2 = h->beta2;
-  a.beta1 = h->beta1;
-  a.omb1 = static_cast<float>(1.0 - b1);
-  a.beta2 = h->beta2;
-  a.omb2 = static_cast<float>(1.0 - b2);
-  a.step_size = static_cast<float>(static_cast<double>(h->lr) /
-                                   (1.0 - std::pow(b1, static_cast<double>(step))));
-  a.inv_bc2 = static_cast<float>(1.0 / (1.0 - std::pow(b2, static_cast<double>(step))));
-  a.eps = h->eps;
-  a.decay =
-      static_cast<float>(1.0 - static_cast<double>(h->lr) * static_cast<double>(h->weight_decay));
-  return a;
 }
 
 // Largest cluster (8, 4, 2 or 1 CTAs) of finalize_kernel that the current device can
@@ -160,16 +135,6 @@ cudaError_t launch_finalize(FinalizeParams fp, int max_ctas, cudaStream_t st,
   cfg.numAttrs = n_ctas > 1 ? 2 : 1;  // one CTA: an ordinary launch (its own implicit cluster)
   return coordwise ? cudaLaunchKernelEx(&cfg, finalize_kernel<true>, fp)
                    : cudaLaunchKernelEx(&cfg, finalize_kernel<false>, fp);
-}
-
-bool misaligned(const void* p, size_t a) {
-  return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0;
-}
-
-// [a, a+na) and [b, b+nb) share a byte
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + nb && b0 < a0 + na;
 }
 
 // Aliasing rule of the norm-test calls: no output range may share a byte with a gradient
