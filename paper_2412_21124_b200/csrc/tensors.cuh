@@ -1,9 +1,11 @@
 // Kernels over a list of tensors: the global norm (and the norm of each tensor), scaling by the
 // clipping factor that follows from it, and AdamW on the clipped gradients.
 //
-// A list is cut into units: runs of `unit` consecutive elements of one tensor (the last one of a
-// tensor is short).  The table of tensors and the tensor of each unit lie in device memory, written
-// there once by the upload of the plan.
+// A list is cut in two ways.  For the norm every warp of a fixed number of warps gets an equal share
+// of the list's bytes, a run of whole 512-byte rows that is cut into segments where a tensor ends.
+// For scaling and AdamW, which join nothing, it is cut into units: runs of `unit` consecutive
+// elements of one tensor, one CTA each.  The tables lie in device memory, written there once by the
+// upload of the plan.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -12,13 +14,11 @@
 namespace absnt {
 
 constexpr int kTensorThreads = 256;
-constexpr int kTensorWarps = kTensorThreads / 32;
 constexpr int kMaxGroups = ABS_MAX_GROUPS;
 
 // One tensor of the list.  A view with rows has `row` elements in each row, `stride` elements from
 // one row to the next and `col` from one column to the next; element i lies at
-// (i / row) * stride + (i % row) * col, and the quotient is (i * magic) >> (31 + shift) for every i
-// below 2^31.
+// (i / row) * stride + (i % row) * col.
 struct TensorEntry {
   const void* g;
   void* out;
@@ -26,9 +26,10 @@ struct TensorEntry {
   uint16_t* p16;
   int64_t numel;
   int64_t g_stride, g_col, out_stride, out_col;
-  uint32_t g_row, g_magic, out_row, out_magic;
+  uint32_t g_row, out_row;
   int32_t first_unit, n_units;
-  uint8_t g_shift, out_shift, g_dtype, out_dtype;
+  int32_t first_seg, n_segs;
+  uint8_t g_dtype, out_dtype;
   uint8_t head;   // elements before the first one that lies on a vector boundary in every array
   uint8_t flags;  // kEntry* bits
   uint16_t group;
@@ -41,17 +42,40 @@ enum {
   kEntryVecAdam = 16,  // from `head` on, 8 elements of gradient, state and bf16 copy are
 };
 
+// A run of elements of one tensor, the work of one warp: [start, start + n), `head` of them before
+// the first 16-byte boundary.
+struct Segment {
+  const void* g;  // of element `start`, for a gradient without rows
+  int64_t start;
+  uint32_t n;
+  int32_t tensor;
+  uint8_t dtype, vec, rows, head;
+  int32_t pad;
+};
+constexpr int kNormThreads = 1024;
+constexpr int kNormWarps = kNormThreads / 32;
+constexpr int kNormCtas = 148;  // one for each SM
+
+// A tensor whose segments lie in several blocks, first..last.
+struct Spanning {
+  int32_t tensor, first, last, pad;
+};
+
 enum { kNormMax = ABS_NORM_MAX, kNorm1 = ABS_NORM_1, kNorm2 = ABS_NORM_2 };
 
 struct TensorsParams {
   const TensorEntry* entries;
   const int32_t* unit_tensor;
-  double* header;       // ABS_GRAD_* slots
-  unsigned int* tickets;  // [0]: finished tensors, [1 + t]: finished units of tensor t
-  double* tensor_sum;   // n
-  double* unit_sum;     // n_units
-  float* norms_out;     // 2 + n
-  int n, n_units, n_nonempty, unit;
+  const Segment* segments;
+  const int32_t* warp_first;  // first segment of each warp, and the number of segments
+  const Spanning* spanning;
+  const int32_t* empty;  // tensors without elements
+  double* header;         // ABS_GRAD_* slots
+  unsigned int* ticket;   // blocks that have finished
+  double* block_sum;      // kNormCtas
+  double* edge_sum;       // 2 kNormCtas: each block's part of its first and of its last tensor
+  float* norms_out;       // 2 + n
+  int n, n_units, unit, n_segments, n_warps, n_spanning, n_empty;
   int norm_type;
   double scale, max_norm;
   const double* sum_in;  // null: header[ABS_GRAD_SUM]
@@ -115,33 +139,35 @@ __device__ __forceinline__ void with_type(int dtype, F&& f) {
     f(TF16{});
 }
 
-// Where the elements of one unit lie in one array: offset of the unit's element i.
-struct Span {
-  int64_t base, stride, col_stride;
-  uint32_t col, row, magic;
-  int shift;
-  bool rows;
-  __device__ __forceinline__ int64_t at(uint32_t i) const {
-    if (!rows) return base + i;
-    const uint32_t idx = col + i;  // below 2^30 + 2^30
-    const uint32_t q = static_cast<uint32_t>((static_cast<uint64_t>(idx) * magic) >> (31 + shift));
-    return base + static_cast<int64_t>(q) * stride + static_cast<int64_t>(idx - q * row) * col_stride;
+// Walks the elements start + i0, start + i0 + step, ... of a view: `offset()` of the current one,
+// `next()` to the one `step` further.  One division at the beginning, none on the way.
+struct Walk {
+  int64_t off, step_off, wrap_off;
+  uint32_t col, step_col, row;
+  __device__ __forceinline__ int64_t offset() const { return off; }
+  __device__ __forceinline__ void next() {
+    off += step_off;
+    col += step_col;
+    if (col >= row) {
+      col -= row;
+      off += wrap_off;
+    }
   }
 };
-__device__ __forceinline__ Span make_span(int64_t start, bool rows, uint32_t row, uint32_t magic,
-                                          int shift, int64_t stride, int64_t col_stride) {
-  if (!rows) return Span{start, 0, 0, 0, 0, 0, 0, false};
-  const int64_t r0 = start / row;
-  return Span{r0 * stride, stride, col_stride, static_cast<uint32_t>(start - r0 * row), row, magic,
-              shift, true};
+__device__ __forceinline__ Walk make_walk(int64_t first, uint32_t step, bool rows, uint32_t row,
+                                          int64_t stride, int64_t col_stride) {
+  if (!rows) return Walk{first, step, 0, 0, 0, 1};
+  const int64_t r = first / row;
+  const uint32_t c = static_cast<uint32_t>(first - r * row);
+  const uint32_t dr = step / row, dc = step - dr * row;
+  return Walk{r * stride + c * col_stride, dr * stride + dc * col_stride,
+              stride - static_cast<int64_t>(row) * col_stride, c, dc, row};
 }
-__device__ __forceinline__ Span grad_span(const TensorEntry& e, int64_t start) {
-  return make_span(start, e.flags & kEntryRowsG, e.g_row, e.g_magic, e.g_shift, e.g_stride,
-                   e.g_col);
+__device__ __forceinline__ Walk grad_walk(const TensorEntry& e, int64_t first, uint32_t step) {
+  return make_walk(first, step, e.flags & kEntryRowsG, e.g_row, e.g_stride, e.g_col);
 }
-__device__ __forceinline__ Span out_span(const TensorEntry& e, int64_t start) {
-  return make_span(start, e.flags & kEntryRowsOut, e.out_row, e.out_magic, e.out_shift,
-                   e.out_stride, e.out_col);
+__device__ __forceinline__ Walk out_walk(const TensorEntry& e, int64_t first, uint32_t step) {
+  return make_walk(first, step, e.flags & kEntryRowsOut, e.out_row, e.out_stride, e.out_col);
 }
 
 // The elements [start, start + n) of a unit; unit 0 also holds the head.
@@ -198,45 +224,37 @@ __device__ __forceinline__ double norm_join(double a, double b) {
   return NORM == kNormMax ? max_keep_nan(a, b) : a + b;
 }
 
-// Joins one value per thread in a fixed order; the result is in every thread.
 template <int NORM>
-__device__ __forceinline__ double block_join(double x, double* sm) {
+__device__ __forceinline__ double warp_join(double x) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1)
-    x = norm_join<NORM>(x, __shfl_down_sync(0xffffffffu, x, off));
-  if ((threadIdx.x & 31) == 0) sm[threadIdx.x >> 5] = x;
-  __syncthreads();
-  double r = sm[0];
-#pragma unroll
-  for (int w = 1; w < kTensorWarps; ++w) r = norm_join<NORM>(r, sm[w]);
-  __syncthreads();
-  return r;
+    x = norm_join<NORM>(x, __shfl_xor_sync(0xffffffffu, x, off));
+  return x;
 }
 
-// One thread's share of a unit.
+// One lane's share of a segment.
 template <typename T, int NORM>
-__device__ __forceinline__ NormAcc<NORM> unit_acc(const TensorEntry& e, const UnitRange& r) {
+__device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, const Segment& s,
+                                                     uint32_t lane) {
   using S = typename T::scalar;
   constexpr int kBatch = 8;
   NormAcc<NORM> acc;
-  const S* g = static_cast<const S*>(e.g);
-  const Span sp = grad_span(e, r.start);
-  const uint32_t tid = threadIdx.x;
-  auto one = [&](uint32_t i) {
-    const S raw = g[sp.at(i)];
+  auto one = [&](S raw) {
     const float x = T::to_float(raw);
     acc.bits |= __float_as_uint(x);
     acc.template add<1>(&x);
   };
-  if (e.flags & kEntryVecG) {
-    if (tid < r.head) one(tid);
-    const uint32_t nv = (r.n - r.head) / T::kVec;
-    for (uint32_t v0 = tid; v0 < nv; v0 += kBatch * kTensorThreads) {
+  if (s.vec) {
+    const S* g = static_cast<const S*>(s.g);
+    if (lane < s.head) one(g[lane]);
+    const uint32_t nv = (s.n - s.head) / T::kVec;
+    const S* gv = g + s.head;
+    for (uint32_t v0 = lane; v0 < nv; v0 += kBatch * 32) {
       uint4 raw[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t v = v0 + j * kTensorThreads;
-        raw[j] = v < nv ? ld_once_16(g + sp.at(r.head + v * T::kVec)) : make_uint4(0, 0, 0, 0);
+        const uint32_t v = v0 + j * 32;
+        raw[j] = v < nv ? ld_once_16(gv + static_cast<size_t>(v) * T::kVec) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
@@ -246,15 +264,18 @@ __device__ __forceinline__ NormAcc<NORM> unit_acc(const TensorEntry& e, const Un
         acc.template add<T::kVec>(x);
       }
     }
-    const uint32_t i = r.head + nv * T::kVec + tid;
-    if (i < r.n) one(i);
+    const uint32_t i = s.head + nv * T::kVec + lane;
+    if (i < s.n) one(g[i]);
   } else {
-    for (uint32_t i0 = tid; i0 < r.n; i0 += kBatch * kTensorThreads) {
+    const TensorEntry& e = prm.entries[s.tensor];
+    const S* g = static_cast<const S*>(e.g);
+    Walk w = grad_walk(e, s.start + lane, 32);
+    for (uint32_t i0 = lane; i0 < s.n; i0 += kBatch * 32) {
       float x[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t i = i0 + j * kTensorThreads;
-        x[j] = i < r.n ? T::to_float(g[sp.at(i)]) : 0.f;
+        x[j] = i0 + j * 32 < s.n ? T::to_float(g[w.offset()]) : 0.f;
+        w.next();
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) acc.bits |= __float_as_uint(x[j]);
@@ -264,18 +285,39 @@ __device__ __forceinline__ NormAcc<NORM> unit_acc(const TensorEntry& e, const Un
   return acc;
 }
 
-// The same sum with every product in fp64, for units whose fp32 products leave the range.
+// The same sum with every product in fp64, for segments whose fp32 products leave the range.
 template <typename T, int NORM>
-__device__ __noinline__ double unit_acc_wide(const TensorEntry& e, const UnitRange& r) {
-  using S = typename T::scalar;
-  const S* g = static_cast<const S*>(e.g);
-  const Span sp = grad_span(e, r.start);
-  double s = 0.0;
-  for (uint32_t i = threadIdx.x; i < r.n; i += kTensorThreads) {
-    const double x = T::to_float(g[sp.at(i)]);
-    s += NORM == kNorm2 ? x * x : fabs(x);
+__device__ __noinline__ double segment_acc_wide(const TensorsParams& prm, const Segment& s,
+                                                uint32_t lane) {
+  const TensorEntry& e = prm.entries[s.tensor];
+  const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
+  Walk w = grad_walk(e, s.start + lane, 32);
+  double sum = 0.0;
+  for (uint32_t i = lane; i < s.n; i += 32, w.next()) {
+    const double x = T::to_float(g[w.offset()]);
+    sum += NORM == kNorm2 ? x * x : fabs(x);
   }
-  return s;
+  return sum;
+}
+
+// The sum of a segment, in every lane of its warp.
+template <int NORM>
+__device__ __forceinline__ double segment_sum(const TensorsParams& prm, const Segment& s,
+                                              uint32_t lane) {
+  double x = 0.0;
+  with_type(s.dtype, [&](auto type) {
+    using T = decltype(type);
+    const NormAcc<NORM> acc = segment_acc<T, NORM>(prm, s, lane);
+    x = warp_join<NORM>(NORM == kNormMax ? static_cast<double>(acc.mx) : acc.s);
+    if constexpr (NORM != kNormMax) {
+      // fp32 squares overflow above 1.8e19 and lose bits below 1e-19; sums of |x| overflow
+      // near the largest float.  A segment whose sum says so is taken again in fp64.
+      const bool wide = !(x < 0x1p120) || (NORM == kNorm2 && x < 0x1p-90);
+      if (wide && __any_sync(0xffffffffu, acc.bits != 0))
+        x = warp_join<NORM>(segment_acc_wide<T, NORM>(prm, s, lane));
+    }
+  });
+  return x;
 }
 
 // What a caller makes of the power sum: the norm, the clipping coefficient and the factor that
@@ -306,75 +348,136 @@ __device__ __forceinline__ void write_clip(const TensorsParams& prm, double sum,
   prm.norms_out[1] = static_cast<float>(c.coef);
 }
 
-// Closes the list: the sums of all tensors are joined in order (by the block of the last unit).
 template <int NORM>
-__device__ __forceinline__ void close_list(const TensorsParams& prm, double* sm) {
-  double s = 0.0;
-  for (int t = threadIdx.x; t < prm.n; t += kTensorThreads) {
-    const double x = __ldcg(prm.tensor_sum + t);
-    s = norm_join<NORM>(s, x);
-    prm.norms_out[2 + t] =
-        static_cast<float>(fabs(prm.scale) * (NORM == kNorm2 ? sqrt(x) : x));
-  }
-  s = block_join<NORM>(s, sm);
-  if (threadIdx.x == 0) write_clip(prm, s, clip_of(s, NORM, prm.scale, prm.max_norm));
+__device__ __forceinline__ void write_norm(const TensorsParams& prm, int t, double x) {
+  prm.norms_out[2 + t] = static_cast<float>(fabs(prm.scale) * (NORM == kNorm2 ? sqrt(x) : x));
 }
 
-// One CTA per unit.  The last unit of a tensor to finish adds that tensor's units in order, the
-// last tensor to finish adds the tensors: one launch, and no order of finishing shows in the sums.
+// The sums of one block.  Segments are dealt out in order, so a tensor that is neither the first
+// nor the last of a warp lies in that warp whole, and one that is neither the first nor the last
+// of a block in that block: its norm is written where it is known.  What remains of a warp, its
+// parts of its first and its last tensor, is joined through shared memory; what remains of a block
+// goes to edge_sum.
+struct WarpParts {
+  double first[kNormWarps], last[kNormWarps];
+  int first_tensor[kNormWarps];  // -1: the warp does not begin inside a tensor
+  int last_tensor[kNormWarps];   // -1: the warp has no work
+};
 template <int NORM>
-__global__ void __launch_bounds__(kTensorThreads)
-    tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
-  __shared__ double sm[kTensorWarps];
-  __shared__ unsigned int s_ticket;
-  grid_dependency_wait();
-  if (prm.n_units == 0) {  // only empty tensors, or none
-    close_list<NORM>(prm, sm);
-    return;
-  }
-  const int u = blockIdx.x;
-  const int t = prm.unit_tensor[u];
-  const TensorEntry& e = prm.entries[t];
-  const UnitRange r = unit_range(e, u, prm.unit);
-  double x = 0.0;
-  with_type(e.g_dtype, [&](auto type) {
-    using T = decltype(type);
-    const NormAcc<NORM> acc = unit_acc<T, NORM>(e, r);
-    x = block_join<NORM>(NORM == kNormMax ? static_cast<double>(acc.mx) : acc.s, sm);
-    if constexpr (NORM != kNormMax) {
-      // fp32 squares overflow above 1.8e19 and lose bits below 1e-19; sums of |x| overflow
-      // near the largest float.  A unit whose sum says so is taken again in fp64.
-      const bool wide = !(x < 0x1p120) || (NORM == kNorm2 && x < 0x1p-90);
-      if (wide && __syncthreads_or(acc.bits != 0))
-        x = block_join<NORM>(unit_acc_wide<T, NORM>(e, r), sm);
+__device__ __forceinline__ double block_sums(const TensorsParams& prm, WarpParts& parts,
+                                             double* sm) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int w = blockIdx.x * kNormWarps + warp;
+  int first_tensor = -1, tensor = -1;
+  double first = 0.0, x = 0.0, sum = 0.0;
+  if (w < prm.n_warps) {
+    const int begin = prm.warp_first[w], end = prm.warp_first[w + 1];
+    bool closed = false;  // a tensor has ended in this warp
+    for (int i = begin; i < end; ++i) {
+      const Segment s = prm.segments[i];
+      if (tensor >= 0 && s.tensor != tensor) {
+        if (!closed && prm.entries[tensor].first_seg < begin) {
+          first_tensor = tensor;
+          first = x;
+        } else if (lane == 0) {
+          write_norm<NORM>(prm, tensor, x);
+        }
+        closed = true;
+        x = 0.0;
+      }
+      tensor = s.tensor;
+      const double y = segment_sum<NORM>(prm, s, lane);
+      x = norm_join<NORM>(x, y);
+      sum = norm_join<NORM>(sum, y);
     }
-  });
-  grid_launch_dependents();
-  if (e.n_units > 1) {
-    if (threadIdx.x == 0) {
-      prm.unit_sum[u] = x;
-      __threadfence();
-      s_ticket = atomicAdd(prm.tickets + 1 + t, 1u);
+    if (!closed && prm.entries[tensor].first_seg < begin) {
+      first_tensor = tensor;
+      first = x;
     }
-    __syncthreads();
-    if (s_ticket != static_cast<unsigned>(e.n_units - 1)) return;
-    __threadfence();
-    x = 0.0;
-    for (int k = threadIdx.x; k < e.n_units; k += kTensorThreads)
-      x = norm_join<NORM>(x, __ldcg(prm.unit_sum + e.first_unit + k));
-    x = block_join<NORM>(x, sm);
-    if (threadIdx.x == 0) prm.tickets[1 + t] = 0;  // ready for the next call
   }
-  if (threadIdx.x == 0) {
-    prm.tensor_sum[t] = x;
-    __threadfence();
-    s_ticket = atomicAdd(prm.tickets, 1u);
+  if (lane == 0) {
+    parts.first[warp] = first;
+    parts.last[warp] = x;
+    parts.first_tensor[warp] = first_tensor;
+    parts.last_tensor[warp] = tensor;
+    sm[warp] = sum;
   }
   __syncthreads();
-  if (s_ticket != static_cast<unsigned>(prm.n_nonempty - 1)) return;
+  // each warp: the tensor that it ends with, unless that one began in an earlier warp of the block
+  if (tensor >= 0 && !(warp > 0 && first_tensor == tensor)) {
+    double y = lane == warp ? x
+               : lane > warp && parts.first_tensor[lane] == tensor ? parts.first[lane]
+                                                                   : 0.0;
+    y = warp_join<NORM>(y);
+    const int seg = prm.entries[tensor].first_seg, n_seg = prm.entries[tensor].n_segs;
+    const int w0 = blockIdx.x * kNormWarps, w1 = min(w0 + kNormWarps, prm.n_warps);
+    const bool from = seg >= prm.warp_first[w0], to = seg + n_seg <= prm.warp_first[w1];
+    if (lane == 0) {
+      if (from && to) write_norm<NORM>(prm, tensor, y);
+      if (!from) prm.edge_sum[2 * blockIdx.x] = y;
+      if (!to) prm.edge_sum[2 * blockIdx.x + 1] = y;
+    }
+  }
+  if (threadIdx.x == 0 && first_tensor >= 0 && first_tensor != tensor)
+    prm.edge_sum[2 * blockIdx.x] = first;
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < prm.n_empty; i += kNormThreads)
+      write_norm<NORM>(prm, prm.empty[i], 0.0);
+  return warp_join<NORM>(sm[lane]);
+}
+
+// The norm of a tensor that lies in several blocks, by one warp.
+template <int NORM>
+__device__ __forceinline__ void join_spanning(const TensorsParams& prm, int i) {
+  const int lane = threadIdx.x & 31;
+  const Spanning s = prm.spanning[i];
+  double x = 0.0;
+  for (int b = s.first + lane; b <= s.last; b += 32)
+    x = norm_join<NORM>(x, __ldcg(prm.edge_sum + 2 * b + (b == s.first ? 1 : 0)));
+  x = warp_join<NORM>(x);
+  if (lane == 0) write_norm<NORM>(prm, s.tensor, x);
+}
+
+// The power sum of the list from the sums of the blocks, in every lane.
+template <int NORM>
+__device__ __forceinline__ double join_blocks(const TensorsParams& prm) {
+  double x = 0.0;
+  for (int b = threadIdx.x & 31; b < static_cast<int>(gridDim.x); b += 32)
+    x = norm_join<NORM>(x, __ldcg(prm.block_sum + b));
+  return warp_join<NORM>(x);
+}
+
+// Every warp sums its segments, every block its warps, the block that finishes last the blocks: one
+// launch, and no order of finishing shows in a sum.
+template <int NORM>
+__global__ void __launch_bounds__(kNormThreads, 1)
+    tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
+  __shared__ WarpParts parts;
+  __shared__ double sm[kNormWarps];
+  __shared__ unsigned int s_ticket;
+  grid_dependency_wait();
+  const double sum = block_sums<NORM>(prm, parts, sm);
+  grid_launch_dependents();
   __threadfence();
-  if (threadIdx.x == 0) prm.tickets[0] = 0;
-  close_list<NORM>(prm, sm);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    prm.block_sum[blockIdx.x] = sum;
+    __threadfence();
+    s_ticket = atomicAdd(prm.ticket, 1u);
+  }
+  __syncthreads();
+  if (s_ticket != gridDim.x - 1) return;
+  __threadfence();
+  const int warp = threadIdx.x >> 5;
+  if (warp == 0) {
+    const double total = join_blocks<NORM>(prm);
+    if (threadIdx.x == 0) {
+      write_clip(prm, total, clip_of(total, NORM, prm.scale, prm.max_norm));
+      *prm.ticket = 0;  // ready for the next call
+    }
+  }
+  for (int i = (warp + kNormWarps - 1) % kNormWarps; i < prm.n_spanning; i += kNormWarps)
+    join_spanning<NORM>(prm, i);
 }
 
 // ---- scaling -------------------------------------------------------------------------
@@ -423,58 +526,64 @@ __device__ __forceinline__ void store8(typename T::scalar* p, const float* x) {
 
 template <typename TI, typename TO>
 __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange& r, float factor,
-                                           const void* in, void* out, const Span& si,
-                                           const Span& so, bool vec) {
+                                           const void* in, void* out, bool in_place, bool vec) {
   const typename TI::scalar* g = static_cast<const typename TI::scalar*>(in);
   typename TO::scalar* y = static_cast<typename TO::scalar*>(out);
   const uint32_t tid = threadIdx.x;
-  auto one = [&](uint32_t i) {
-    y[so.at(i)] = TO::from_float(factor * TI::to_float(g[si.at(i)]));
-  };
   if (vec) {
+    // rows are whole vectors here, and there is no head then: the walk goes by vectors
     constexpr int kBatch = 4;
+    auto one = [&](uint32_t i) {
+      y[r.start + i] = TO::from_float(factor * TI::to_float(g[r.start + i]));
+    };
     if (tid < r.head) one(tid);
     const uint32_t nv = (r.n - r.head) / 8;
+    const int64_t first = r.start + r.head + tid * 8;
+    Walk wi = grad_walk(e, first, 8 * kTensorThreads);
+    Walk wo = in_place ? wi : out_walk(e, first, 8 * kTensorThreads);
     for (uint32_t v0 = tid; v0 < nv; v0 += kBatch * kTensorThreads) {
       Vec8<TI> raw[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t v = v0 + j * kTensorThreads;
-        if (v < nv) raw[j] = load8<TI>(g + si.at(r.head + v * 8));
+        if (v0 + j * kTensorThreads < nv) raw[j] = load8<TI>(g + wi.offset());
+        wi.next();
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t v = v0 + j * kTensorThreads;
-        if (v < nv) {
+        if (v0 + j * kTensorThreads < nv) {
           float x[8];
           unpack8<TI>(raw[j], x);
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] *= factor;
-          store8<TO>(y + so.at(r.head + v * 8), x);
+          store8<TO>(y + wo.offset(), x);
         }
+        wo.next();
       }
     }
     const uint32_t i = r.head + nv * 8 + tid;
-    if (i < r.n) one(i);
+    if (i < r.n) one(i);  // only without rows: the elements of a view with rows are whole vectors
   } else {
-    constexpr int kBatch = 8;
+    constexpr int kBatch = 16;
+    Walk wi = grad_walk(e, r.start + tid, kTensorThreads);
+    Walk wo = in_place ? wi : out_walk(e, r.start + tid, kTensorThreads);
     for (uint32_t i0 = tid; i0 < r.n; i0 += kBatch * kTensorThreads) {
-      float x[kBatch];
+      typename TI::scalar x[kBatch];
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t i = i0 + j * kTensorThreads;
-        x[j] = i < r.n ? TI::to_float(g[si.at(i)]) : 0.f;
+        if (i0 + j * kTensorThreads < r.n) x[j] = g[wi.offset()];
+        wi.next();
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        const uint32_t i = i0 + j * kTensorThreads;
-        if (i < r.n) y[so.at(i)] = TO::from_float(factor * x[j]);
+        if (i0 + j * kTensorThreads < r.n)
+          y[wo.offset()] = TO::from_float(factor * TI::to_float(x[j]));
+        wo.next();
       }
     }
   }
 }
 
-__global__ void __launch_bounds__(kTensorThreads)
+__global__ void __launch_bounds__(kTensorThreads, 3)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
   __shared__ Clip s_clip;
   grid_dependency_wait();
@@ -487,16 +596,12 @@ __global__ void __launch_bounds__(kTensorThreads)
   with_type(e.g_dtype, [&](auto ti) {
     using TI = decltype(ti);
     if (prm.in_place) {
-      const Span sp = grad_span(e, r.start);
-      // one array only: 8 elements are aligned wherever 16-byte loads are, for 16-bit types; fp32
-      // vectors of 8 want 32 bytes
-      const bool vec = e.flags & kEntryVecClip;
-      unit_scale<TI, TI>(e, r, clip.factor, e.g, const_cast<void*>(e.g), sp, sp, vec);
+      unit_scale<TI, TI>(e, r, clip.factor, e.g, const_cast<void*>(e.g), true,
+                         e.flags & kEntryVecClip);
     } else {
       with_type(e.out_dtype, [&](auto to) {
         using TO = decltype(to);
-        unit_scale<TI, TO>(e, r, clip.factor, e.g, e.out, grad_span(e, r.start),
-                           out_span(e, r.start), e.flags & kEntryVecClip);
+        unit_scale<TI, TO>(e, r, clip.factor, e.g, e.out, false, e.flags & kEntryVecClip);
       });
     }
   });
@@ -532,25 +637,25 @@ __global__ void __launch_bounds__(kTensorThreads)
   const TensorEntry& e = prm.entries[prm.unit_tensor[u]];
   const UnitRange r = unit_range(e, u, prm.unit);
   const AdamScalars& a = groups.a[e.group];
-  const Span sp = grad_span(e, r.start);
   float *p = e.p + r.start, *m = e.m + r.start, *v = e.v + r.start;
   uint16_t* p16 = e.p16 ? e.p16 + r.start : nullptr;
   const uint32_t tid = threadIdx.x;
   with_type(e.g_dtype, [&](auto type) {
     using T = decltype(type);
     const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
-    auto one = [&](uint32_t i) {
+    auto one = [&](uint32_t i, int64_t at) {
       float w = p[i], mi = m[i], vi = v[i];
-      adamw_elem(a, a.omb1, a.omb2, factor * T::to_float(g[sp.at(i)]), w, mi, vi);
+      adamw_elem(a, a.omb1, a.omb2, factor * T::to_float(g[at]), w, mi, vi);
       p[i] = w, m[i] = mi, v[i] = vi;
       if (p16) p16[i] = to_bf16(w);
     };
     if (e.flags & kEntryVecAdam) {
-      if (tid < r.head) one(tid);
+      if (tid < r.head) one(tid, r.start + tid);
       const uint32_t nv = (r.n - r.head) / 8;
-      for (uint32_t q = tid; q < nv; q += kTensorThreads) {
+      Walk wg = grad_walk(e, r.start + r.head + tid * 8, 8 * kTensorThreads);
+      for (uint32_t q = tid; q < nv; q += kTensorThreads, wg.next()) {
         const uint32_t i = r.head + q * 8;
-        const Vec8<T> raw = load8<T>(g + sp.at(i));
+        const Vec8<T> raw = load8<T>(g + wg.offset());
         Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
         float x[8];
         unpack8<T>(raw, x);
@@ -566,9 +671,10 @@ __global__ void __launch_bounds__(kTensorThreads)
         if (p16) st_bf16x8(p16 + i, w.lo, w.hi);
       }
       const uint32_t i = r.head + nv * 8 + tid;
-      if (i < r.n) one(i);
+      if (i < r.n) one(i, r.start + i);
     } else {
-      for (uint32_t i = tid; i < r.n; i += kTensorThreads) one(i);
+      Walk wg = grad_walk(e, r.start + tid, kTensorThreads);
+      for (uint32_t i = tid; i < r.n; i += kTensorThreads, wg.next()) one(i, wg.offset());
     }
   });
 }

@@ -15,31 +15,60 @@ namespace {
 constexpr uint64_t kPlanMagic = 0x6e616c7054534241ull;  // "ABSTplan"
 constexpr int64_t kMaxRow = int64_t{1} << 30;
 constexpr int64_t kMaxElements = int64_t{1} << 46;
+constexpr int64_t kMaxUnits = int64_t{1} << 30;
 enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
 
-// Host image of a plan: this header, the table of tensors, the tensor of each unit.
+// Host image of a plan: this header, then the tables in the order of `Image`.
 struct PlanHeader {
   uint64_t magic;
-  int32_t n, n_units, n_nonempty, unit, roles, n_groups;
+  int32_t n, n_units, n_segments, n_warps, n_spanning, n_empty, unit, roles, n_groups, pad;
 };
-TensorEntry* entries_of(void* plan) {
-  return reinterpret_cast<TensorEntry*>(static_cast<char*>(plan) + sizeof(PlanHeader));
-}
-size_t image_bytes(int64_t n, int64_t n_units) {
-  return static_cast<size_t>(n) * sizeof(TensorEntry) + static_cast<size_t>(n_units) * 4;
-}
-
-// Device work area: header, sums of tensors and units, tickets, then the image of the plan.
-struct WorkLayout {
-  size_t tensor_sum, unit_sum, tickets, image, bytes;
-  WorkLayout(int64_t n, int64_t n_units) {
-    tensor_sum = sizeof(double) * ABS_STATS_HEADER;
-    unit_sum = tensor_sum + sizeof(double) * static_cast<size_t>(n);
-    tickets = unit_sum + sizeof(double) * static_cast<size_t>(n_units);
-    image = (tickets + 4 * (static_cast<size_t>(n) + 1) + 15) / 16 * 16;
-    bytes = image + image_bytes(n, n_units);
+// Offsets of the tables in the image (which the device holds as well).
+struct Image {
+  size_t segments, spanning, warp_first, unit_tensor, empty, bytes;
+  explicit Image(const PlanHeader& h) {
+    segments = static_cast<size_t>(h.n) * sizeof(TensorEntry);
+    spanning = segments + static_cast<size_t>(h.n_segments) * sizeof(Segment);
+    warp_first = spanning + static_cast<size_t>(h.n_spanning) * sizeof(Spanning);
+    unit_tensor = warp_first + 4 * (static_cast<size_t>(h.n_warps) + 1);
+    empty = unit_tensor + 4 * static_cast<size_t>(h.n_units);
+    bytes = empty + 4 * static_cast<size_t>(h.n_empty);
   }
 };
+char* image_of(void* plan) { return static_cast<char*>(plan) + sizeof(PlanHeader); }
+
+// Device work area: header, sums and edge sums of the blocks, the ticket, then the image of the plan.
+struct WorkLayout {
+  size_t block_sum, edge_sum, ticket, image, bytes;
+  explicit WorkLayout(const PlanHeader& h) {
+    block_sum = sizeof(double) * ABS_STATS_HEADER;
+    edge_sum = block_sum + sizeof(double) * kNormCtas;
+    ticket = edge_sum + sizeof(double) * 2 * kNormCtas;
+    image = (ticket + 4 + 15) / 16 * 16;
+    bytes = image + Image(h).bytes;
+  }
+};
+
+// How the bytes of a list are shared out: `rows` rows of 512 bytes (32 lanes of 16 bytes) to each of
+// `warps` warps, at most as many as fill the device.
+constexpr int64_t kRowBytes = 512;
+struct Share {
+  int64_t rows;
+  int64_t warps;
+};
+Share share_of(int64_t total_rows) {
+  const int64_t most = static_cast<int64_t>(kNormCtas) * kNormWarps;
+  Share s;
+  s.rows = std::max<int64_t>(1, (total_rows + most - 1) / most);
+  s.warps = (total_rows + s.rows - 1) / s.rows;
+  return s;
+}
+// Rows of a tensor, the last one short.
+int64_t rows_of(int64_t numel, size_t esz) {
+  return (numel * static_cast<int64_t>(esz) + kRowBytes - 1) / kRowBytes;
+}
+// A segment is counted in 32 bits; longer runs of one warp are cut.
+constexpr int64_t kMaxSegmentRows = int64_t{1} << 20;
 
 // Elements per unit: a power of two that gives about eight units to each of the 148 SMs, between
 // 1024 (a quarter of a vector per thread, so that small lists spread over the SMs) and 32768.  A
@@ -91,15 +120,6 @@ int view_of(const abs_tensor& t, View* v) {
   v->stride = t.row_stride;
   v->col = t.col_stride;
   return ABS_OK;
-}
-
-// i / d = (i * magic) >> (31 + shift) for 0 <= i < 2^31, 1 <= d <= 2^30: with 2^shift >= d the
-// excess of magic / 2^(31+shift) over 1/d is at most 2^-(31+shift), less than 1/(d i).
-void divisor(uint32_t d, uint32_t* magic, uint8_t* shift) {
-  int s = 0;
-  while ((uint64_t{1} << s) < d) ++s;
-  *magic = static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + d - 1) / d);
-  *shift = static_cast<uint8_t>(s);
 }
 
 // Whether elements [head, ...) of a view can be taken in groups of `vec`, each aligned.
@@ -154,20 +174,29 @@ int fill_params(const void* plan, void* work, int norm_type, double scale, doubl
   if (!std::isfinite(max_norm) || max_norm < 0.0) return ABS_ERR_RANGE;
   if (misaligned(work, 16) || misaligned(norms_out, 4) || misaligned(sum_in, 8))
     return ABS_ERR_ALIGN;
-  const WorkLayout L(h->n, h->n_units);
+  const WorkLayout L(*h);
   char* w = static_cast<char*>(work);
   if (norms_out && overlaps(norms_out, 4 * (static_cast<size_t>(h->n) + 2), work, L.bytes)) return ABS_ERR_ALIAS;
   prm->header = reinterpret_cast<double*>(w);
-  prm->tensor_sum = reinterpret_cast<double*>(w + L.tensor_sum);
-  prm->unit_sum = reinterpret_cast<double*>(w + L.unit_sum);
-  prm->tickets = reinterpret_cast<unsigned int*>(w + L.tickets);
-  prm->entries = reinterpret_cast<const TensorEntry*>(w + L.image);
-  prm->unit_tensor = reinterpret_cast<const int32_t*>(prm->entries + h->n);
+  prm->block_sum = reinterpret_cast<double*>(w + L.block_sum);
+  prm->edge_sum = reinterpret_cast<double*>(w + L.edge_sum);
+  prm->ticket = reinterpret_cast<unsigned int*>(w + L.ticket);
+  const Image I(*h);
+  w += L.image;
+  prm->entries = reinterpret_cast<const TensorEntry*>(w);
+  prm->segments = reinterpret_cast<const Segment*>(w + I.segments);
+  prm->spanning = reinterpret_cast<const Spanning*>(w + I.spanning);
+  prm->empty = reinterpret_cast<const int32_t*>(w + I.empty);
+  prm->warp_first = reinterpret_cast<const int32_t*>(w + I.warp_first);
+  prm->unit_tensor = reinterpret_cast<const int32_t*>(w + I.unit_tensor);
   prm->norms_out = norms_out;
   prm->n = h->n;
   prm->n_units = h->n_units;
-  prm->n_nonempty = h->n_nonempty;
   prm->unit = h->unit;
+  prm->n_segments = h->n_segments;
+  prm->n_warps = h->n_warps;
+  prm->n_spanning = h->n_spanning;
+  prm->n_empty = h->n_empty;
   prm->norm_type = norm_type;
   prm->scale = scale;
   prm->max_norm = max_norm;
@@ -181,7 +210,7 @@ dim3 unit_grid(const TensorsParams& prm) {
 }
 
 cudaError_t launch_norm(const TensorsParams& prm, cudaStream_t st) {
-  const dim3 grid = unit_grid(prm), block(kTensorThreads);
+  const dim3 grid(std::max(1, (prm.n_warps + kNormWarps - 1) / kNormWarps)), block(kNormThreads);
   return prm.norm_type == ABS_NORM_2   ? launch_pdl(tensors_norm_kernel<kNorm2>, grid, block, st, prm)
          : prm.norm_type == ABS_NORM_1 ? launch_pdl(tensors_norm_kernel<kNorm1>, grid, block, st, prm)
                                        : launch_pdl(tensors_norm_kernel<kNormMax>, grid, block, st, prm);
@@ -198,7 +227,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   h.magic = kPlanMagic;
   h.n = n;
   h.roles = (outs ? kRoleOut : 0) | (params ? kRoleAdam : 0) | (params_bf16 ? kRoleBf16 : 0);
-  int64_t total = 0;
+  int64_t total = 0, total_rows = 0;
   for (int t = 0; t < n; ++t) {
     View g;
     const int rc = view_of(grads[t], &g);
@@ -206,11 +235,11 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     if (grads[t].group < 0 || grads[t].group >= ABS_MAX_GROUPS) return ABS_ERR_RANGE;
     if (g.numel > kMaxElements - total) return ABS_ERR_RANGE;
     total += g.numel;
+    total_rows += rows_of(g.numel, g.esz);
   }
   h.unit = unit_for(total);
-  TensorEntry* entries = entries_of(plan);
-  if (plan_bytes < sizeof(PlanHeader) + image_bytes(n, 0)) return ABS_ERR_TOO_LARGE;
-  int64_t units = 0;
+  std::vector<TensorEntry> entries(n);
+  std::vector<int32_t> unit_tensor;
   for (int t = 0; t < n; ++t) {
     View g, out, state[3], b16;
     view_of(grads[t], &g);
@@ -227,7 +256,6 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
       e.g_row = static_cast<uint32_t>(g.row);
       e.g_stride = g.stride;
       e.g_col = g.col;
-      divisor(e.g_row, &e.g_magic, &e.g_shift);
     }
     if (outs) {
       const int rc = view_of(outs[t], &out);
@@ -240,7 +268,6 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
         e.out_row = static_cast<uint32_t>(out.row);
         e.out_stride = out.stride;
         e.out_col = out.col;
-        divisor(e.out_row, &e.out_magic, &e.out_shift);
       }
       if (out.numel) all.push_back({out, true});
     }
@@ -288,21 +315,92 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     if (e.numel) {
       const int64_t body = e.numel > e.head ? e.numel - e.head : 1;
       const int64_t k = (body + h.unit - 1) / h.unit;
-      if (units + k > (int64_t{1} << 30)) return ABS_ERR_RANGE;
-      e.first_unit = static_cast<int32_t>(units);
+      if (k > kMaxUnits - static_cast<int64_t>(unit_tensor.size())) return ABS_ERR_RANGE;
+      e.first_unit = static_cast<int32_t>(unit_tensor.size());
       e.n_units = static_cast<int32_t>(k);
-      units += k;
-      ++h.n_nonempty;
+      unit_tensor.insert(unit_tensor.end(), static_cast<size_t>(k), t);
     }
     entries[t] = e;
   }
-  h.n_units = static_cast<int32_t>(units);
-  if (plan_bytes < sizeof(PlanHeader) + image_bytes(n, units)) return ABS_ERR_TOO_LARGE;
   if (any_conflict(all)) return ABS_ERR_ALIAS;
   if (any_conflict(grads_written)) h.roles |= kGradsOverlap;
-  int32_t* unit_tensor = reinterpret_cast<int32_t*>(entries + n);
-  for (int t = 0; t < n; ++t)
-    for (int k = 0; k < entries[t].n_units; ++k) unit_tensor[entries[t].first_unit + k] = t;
+
+  // the segments: the rows of all tensors in order, dealt out to the warps
+  const Share share = share_of(total_rows);
+  std::vector<Segment> segments;
+  std::vector<int32_t> warp_first;
+  int64_t left = 0;  // rows that the current warp still takes
+  for (int t = 0; t < n; ++t) {
+    TensorEntry& e = entries[t];
+    const size_t esz = element_size(e.g_dtype);
+    const int64_t per_row = kRowBytes / static_cast<int64_t>(esz);
+    const int head = (e.flags & kEntryVecG) ? e.head : 0;
+    int64_t rows = rows_of(e.numel, esz), start = 0;
+    e.first_seg = static_cast<int32_t>(segments.size());
+    while (rows > 0) {
+      if (left == 0) {
+        warp_first.push_back(static_cast<int32_t>(segments.size()));
+        left = share.rows;
+      }
+      const int64_t take = std::min(std::min(rows, left), kMaxSegmentRows);
+      rows -= take;
+      left -= take;
+      // every segment but the last ends on a 16-byte boundary: `head` elements further
+      const int64_t end = rows ? start + take * per_row + (start ? 0 : head) : e.numel;
+      Segment s;
+      std::memset(&s, 0, sizeof s);
+      s.start = start;
+      s.n = static_cast<uint32_t>(std::min(end, e.numel) - start);
+      s.g = static_cast<const char*>(e.g) + (e.flags & kEntryRowsG ? 0 : start * esz);
+      s.tensor = t;
+      s.dtype = e.g_dtype;
+      s.rows = (e.flags & kEntryRowsG) ? 1 : 0;
+      s.vec = (e.flags & kEntryVecG) && !s.rows;
+      s.head = static_cast<uint8_t>(start ? 0 : std::min<int64_t>(head, s.n));
+      start += s.n;
+      segments.push_back(s);
+      if (start == e.numel) {  // the head has taken the last, short row
+        left += rows;
+        rows = 0;
+      }
+    }
+    e.n_segs = static_cast<int32_t>(segments.size()) - e.first_seg;
+  }
+  // the tensors that blocks (kNormWarps warps each) share
+  std::vector<Spanning> spanning;
+  std::vector<int32_t> empty;
+  const auto block_of = [&](int32_t segment) {  // the warps' first segments ascend
+    const auto it = std::upper_bound(warp_first.begin(), warp_first.end(), segment);
+    return static_cast<int32_t>((it - warp_first.begin() - 1) / kNormWarps);
+  };
+  for (int t = 0; t < n; ++t) {
+    const TensorEntry& e = entries[t];
+    if (!e.n_segs) {
+      empty.push_back(t);
+      continue;
+    }
+    const int32_t a = block_of(e.first_seg), b = block_of(e.first_seg + e.n_segs - 1);
+    if (a != b) spanning.push_back({t, a, b, 0});
+  }
+  h.n_spanning = static_cast<int32_t>(spanning.size());
+  h.n_empty = static_cast<int32_t>(empty.size());
+  h.n_warps = static_cast<int32_t>(warp_first.size());
+  h.n_segments = static_cast<int32_t>(segments.size());
+  h.n_units = static_cast<int32_t>(unit_tensor.size());
+  warp_first.push_back(h.n_segments);
+
+  const Image I(h);
+  if (plan_bytes < sizeof(PlanHeader) + I.bytes) return ABS_ERR_TOO_LARGE;
+  char* image = image_of(plan);
+  const auto put = [](char* to, const void* from, size_t bytes) {
+    if (bytes) std::memcpy(to, from, bytes);
+  };
+  put(image, entries.data(), entries.size() * sizeof(TensorEntry));
+  put(image + I.segments, segments.data(), segments.size() * sizeof(Segment));
+  put(image + I.warp_first, warp_first.data(), warp_first.size() * 4);
+  put(image + I.spanning, spanning.data(), spanning.size() * sizeof(Spanning));
+  put(image + I.empty, empty.data(), empty.size() * 4);
+  put(image + I.unit_tensor, unit_tensor.data(), unit_tensor.size() * 4);
   std::memcpy(plan, &h, sizeof h);
   return ABS_OK;
 }
@@ -312,15 +410,30 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
 extern "C" {
 
 size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n) {
-  if (n < 0 || (n > 0 && !grads)) return 0;
-  int64_t total = 0, units = 0;
+  if (n < 0 || n > ABS_MAX_TENSORS || (n > 0 && !grads)) return 0;
+  int64_t total = 0, rows = 0, units = 0, segments = 0;
   for (int t = 0; t < n; ++t) {
     if (grads[t].numel < 0 || grads[t].numel > kMaxElements - total) return 0;
     total += grads[t].numel;
+    rows += rows_of(grads[t].numel, element_size(grads[t].dtype));
   }
+  // upper bounds: a tensor has a segment of its own and one more for each warp that begins in it
   const int unit = unit_for(total);
-  for (int t = 0; t < n; ++t) units += (grads[t].numel + unit - 1) / unit;
-  return sizeof(PlanHeader) + image_bytes(n, units);
+  const Share share = share_of(rows);
+  for (int t = 0; t < n; ++t) {
+    const int64_t r = rows_of(grads[t].numel, element_size(grads[t].dtype));
+    units += (grads[t].numel + unit - 1) / unit;
+    segments += r ? 1 + r / share.rows + r / kMaxSegmentRows + 1 : 0;
+  }
+  if (units > kMaxUnits || segments > kMaxUnits) return 0;
+  PlanHeader h;
+  std::memset(&h, 0, sizeof h);
+  h.n = h.n_empty = n;
+  h.n_units = static_cast<int32_t>(units);
+  h.n_segments = static_cast<int32_t>(segments);
+  h.n_warps = static_cast<int32_t>(share.warps);
+  h.n_spanning = std::min(n, kNormCtas);
+  return sizeof h + Image(h).bytes;
 }
 
 int abs_tensors_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor* params,
@@ -341,7 +454,7 @@ int abs_tensors_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_
 
 size_t abs_tensors_work_bytes(const void* plan) {
   const PlanHeader* h = plan_of(plan);
-  return h ? WorkLayout(h->n, h->n_units).bytes : 0;
+  return h ? WorkLayout(*h).bytes : 0;
 }
 
 int abs_tensors_upload(const void* plan, void* work, abs_stream_t stream) {
@@ -349,7 +462,7 @@ int abs_tensors_upload(const void* plan, void* work, abs_stream_t stream) {
   const PlanHeader* h = plan_of(plan);
   if (!h) return ABS_ERR_RANGE;
   if (misaligned(work, 16)) return ABS_ERR_ALIGN;
-  const WorkLayout L(h->n, h->n_units);
+  const WorkLayout L(*h);
   char* w = static_cast<char*>(work);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaMemsetAsync(w, 0, L.image, st);

@@ -137,10 +137,7 @@ def test_plan_arguments(L):
     assert L.abs_tensors_plan(g, None, None, None, None, None, B.ABS_MAX_TENSORS + 1, buf, 8000) == B.ABS_ERR_RANGE
     at = ctypes.addressof(buf)
     assert L.abs_tensors_plan(g, None, None, None, None, None, 1, at + 4, 7000) == B.ABS_ERR_ALIGN
-    for short in (0, 1, 100):
-        assert plan(L, [T(numel=500_000)], short=short)[0] == (B.ABS_ERR_TOO_LARGE if short else B.ABS_OK)
-    need = L.abs_tensors_plan_bytes(g, 1)
-    for have in (0, 8, need - 1):
+    for have in (0, 8, 100):
         assert L.abs_tensors_plan(g, None, None, None, None, None, 1, buf, have) == B.ABS_ERR_TOO_LARGE
     assert plan(L, [])[0] == B.ABS_OK
     assert L.abs_tensors_work_bytes(None) == 0
