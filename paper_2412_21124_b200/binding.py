@@ -713,8 +713,11 @@ class GradTensors:
     def _enter(self, stream):
         """The stream of a call, as a number; a stream other than the one the plan was uploaded on
         first waits for the upload."""
-        if stream is None:
-            raw = torch.cuda.current_stream().cuda_stream
+        if torch._C._cuda_getDevice() != self._device:
+            raise ValueError("the tensors live on cuda:%d, which is not the current device"
+                             % self._device)
+        if stream is None:  # the number alone: torch's stream object would cost more than the call
+            raw = torch._C._cuda_getCurrentRawStream(self._device)
         else:
             raw = _stream(stream).value or 0
         if raw != self._uploaded_on and not torch.cuda.is_current_stream_capturing():

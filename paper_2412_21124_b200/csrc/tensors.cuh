@@ -1,11 +1,11 @@
 // Kernels over a list of tensors: the global norm (and the norm of each tensor), scaling by the
 // clipping factor that follows from it, and AdamW on the clipped gradients.
 //
-// A list is cut in two ways.  For the norm every warp of a fixed number of warps gets an equal share
-// of the list's bytes, a run of whole 512-byte rows that is cut into segments where a tensor ends.
-// For scaling and AdamW, which join nothing, it is cut into units: runs of `unit` consecutive
-// elements of one tensor, one CTA each.  The tables lie in device memory, written there once by the
-// upload of the plan.
+// A list is cut in two ways.  For the norm its bytes are dealt out to warps in rows of 512 bytes (32
+// lanes of 16): every warp of every block gets the same number of rows, and where a tensor ends
+// inside a warp's rows they are cut into segments.  For scaling and AdamW, which join nothing, it is
+// cut into units: runs of consecutive elements of one tensor, one CTA each.
+// The tables lie in device memory, written there once by the upload of the plan.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -15,6 +15,12 @@ namespace absnt {
 
 constexpr int kTensorThreads = 256;
 constexpr int kMaxGroups = ABS_MAX_GROUPS;
+constexpr int kListBlocks = 148;     // blocks of the norm kernel, one for each SM
+constexpr int kListWarps = 32;       // their warps
+constexpr int kClusterBlocks = 16;   // blocks of the one-cluster kernel
+constexpr int kClusterWarps = 16;
+constexpr int kClusterRows = 16;     // most rows that one of its warps takes
+constexpr int kAdamwUnit = 4096;     // elements of a unit of AdamW
 
 // One tensor of the list.  A view with rows has `row` elements in each row, `stride` elements from
 // one row to the next and `col` from one column to the next; element i lies at
@@ -27,8 +33,7 @@ struct TensorEntry {
   int64_t numel;
   int64_t g_stride, g_col, out_stride, out_col;
   uint32_t g_row, out_row;
-  int32_t first_unit, n_units;
-  int32_t first_seg, n_segs;
+  int32_t first_scale, first_adamw;  // its first unit for scaling and for AdamW
   uint8_t g_dtype, out_dtype;
   uint8_t head;   // elements before the first one that lies on a vector boundary in every array
   uint8_t flags;  // kEntry* bits
@@ -43,43 +48,52 @@ enum {
 };
 
 // A run of elements of one tensor, the work of one warp: [start, start + n), `head` of them before
-// the first 16-byte boundary.
-struct Segment {
+// the first 16-byte boundary.  The segments that open a warp's rows lie in one table, by warp;
+// `more` others follow in another one from `next` on.
+struct alignas(16) Segment {
   const void* g;  // of element `start`, for a gradient without rows
   int64_t start;
   uint32_t n;
-  int32_t tensor;
-  uint8_t dtype, vec, rows, head;
-  int32_t pad;
+  int32_t tensor;               // -1: no work
+  uint8_t dtype, head, flags, pos;  // flags: the kEntryVec* bits that hold; pos: kSeg* bits
+  int32_t more, next, pad;
 };
-constexpr int kNormThreads = 1024;
-constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kNormCtas = 148;  // one for each SM
+enum { kSegBegins = 1, kSegEnds = 2 };  // the first / last segment of its tensor
 
 // A tensor whose segments lie in several blocks, first..last.
 struct Spanning {
   int32_t tensor, first, last, pad;
+};
+// The tensors that a block shares with the blocks before and after it: places in the table of
+// those, -1: none.
+struct Shared2 {
+  int32_t before, after;
 };
 
 enum { kNormMax = ABS_NORM_MAX, kNorm1 = ABS_NORM_1, kNorm2 = ABS_NORM_2 };
 
 struct TensorsParams {
   const TensorEntry* entries;
-  const int32_t* unit_tensor;
-  const Segment* segments;
-  const int32_t* warp_first;  // first segment of each warp, and the number of segments
+  const int32_t* scale_tensor;  // the tensor of each unit
+  const int32_t* adamw_tensor;
+  const Segment* opening;   // blocks * warps
+  const Segment* further;
   const Spanning* spanning;
-  const int32_t* empty;  // tensors without elements
-  double* header;         // ABS_GRAD_* slots
-  unsigned int* ticket;   // blocks that have finished
-  double* block_sum;      // kNormCtas
-  double* edge_sum;       // 2 kNormCtas: each block's part of its first and of its last tensor
-  float* norms_out;       // 2 + n
-  int n, n_units, unit, n_segments, n_warps, n_spanning, n_empty;
+  const Shared2* shared;    // blocks
+  const int32_t* empty;     // tensors without elements
+  double* header;           // ABS_GRAD_* slots
+  float* factor;            // what gradients are multiplied by; NaN: the norm is not finite
+  unsigned int* tickets;    // [0]: finished blocks, [1 + i]: those of spanning tensor i
+  double* block_sum;        // blocks
+  double* edge_sum;         // 2 * blocks: a block's parts of the tensors it shares
+  float* norms_out;         // 2 + n
+  int n, n_scale, n_adamw, n_spanning, n_empty;
+  int scale_unit;  // elements of a unit for scaling
   int norm_type;
   double scale, max_norm;
-  const double* sum_in;  // null: header[ABS_GRAD_SUM]
+  const double* sum_in;
   int in_place;
+  int after_norm;  // the kernel before this one in the stream is this call's norm kernel
 };
 struct GroupScalars {
   AdamScalars a[kMaxGroups];
@@ -170,13 +184,12 @@ __device__ __forceinline__ Walk out_walk(const TensorEntry& e, int64_t first, ui
   return make_walk(first, step, e.flags & kEntryRowsOut, e.out_row, e.out_stride, e.out_col);
 }
 
-// The elements [start, start + n) of a unit; unit 0 also holds the head.
+// The elements [start, start + n) of unit k of a tensor; unit 0 also holds the head.
 struct UnitRange {
   int64_t start;
   uint32_t n, head;
 };
-__device__ __forceinline__ UnitRange unit_range(const TensorEntry& e, int u, int unit) {
-  const int k = u - e.first_unit;
+__device__ __forceinline__ UnitRange unit_range(const TensorEntry& e, int k, int unit) {
   UnitRange r;
   r.start = k ? e.head + static_cast<int64_t>(k) * unit : 0;
   int64_t end = e.head + static_cast<int64_t>(k + 1) * unit;
@@ -232,10 +245,21 @@ __device__ __forceinline__ double warp_join(double x) {
   return x;
 }
 
-// One lane's share of a segment.
-template <typename T, int NORM>
+// 16 bytes of a gradient.  Not the read-only path: a kernel may scale its gradients in place.
+__device__ __forceinline__ uint4 ld_grad_16(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p)
+               : "memory");
+  return r;
+}
+
+// One lane's share of a segment.  KEEP: its rows are also left in shared memory, at `keep` (this
+// lane's place in row 0), one after the other.
+template <typename T, int NORM, bool KEEP>
 __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, const Segment& s,
-                                                     uint32_t lane) {
+                                                     uint32_t lane, uint4* keep) {
   using S = typename T::scalar;
   constexpr int kBatch = 8;
   NormAcc<NORM> acc;
@@ -244,7 +268,7 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
     acc.bits |= __float_as_uint(x);
     acc.template add<1>(&x);
   };
-  if (s.vec) {
+  if (s.flags & kEntryVecG) {
     const S* g = static_cast<const S*>(s.g);
     if (lane < s.head) one(g[lane]);
     const uint32_t nv = (s.n - s.head) / T::kVec;
@@ -254,7 +278,7 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
         const uint32_t v = v0 + j * 32;
-        raw[j] = v < nv ? ld_once_16(gv + static_cast<size_t>(v) * T::kVec) : make_uint4(0, 0, 0, 0);
+        raw[j] = v < nv ? ld_grad_16(gv + static_cast<size_t>(v) * T::kVec) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
@@ -262,24 +286,33 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
         T::unpack(raw[j], x);
         acc.bits |= raw[j].x | raw[j].y | raw[j].z | raw[j].w;
         acc.template add<T::kVec>(x);
+        if (KEEP && v0 + j * 32 < nv) keep[v0 - lane + j * 32] = raw[j];
       }
     }
     const uint32_t i = s.head + nv * T::kVec + lane;
     if (i < s.n) one(g[i]);
   } else {
+    constexpr int kWalk = 16;
     const TensorEntry& e = prm.entries[s.tensor];
     const S* g = static_cast<const S*>(e.g);
     Walk w = grad_walk(e, s.start + lane, 32);
-    for (uint32_t i0 = lane; i0 < s.n; i0 += kBatch * 32) {
-      float x[kBatch];
+    for (uint32_t i0 = lane; i0 < s.n; i0 += kWalk * 32) {
+      S raw[kWalk];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        x[j] = i0 + j * 32 < s.n ? T::to_float(g[w.offset()]) : 0.f;
+      for (int j = 0; j < kWalk; ++j) {
+        raw[j] = i0 + j * 32 < s.n ? g[w.offset()] : S(0);
         w.next();
       }
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) acc.bits |= __float_as_uint(x[j]);
-      acc.template add<kBatch>(x);
+      for (int j = 0; j < kWalk; j += 8) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = T::to_float(raw[j + k]);
+          acc.bits |= __float_as_uint(x[k]);
+        }
+        acc.template add<8>(x);
+      }
     }
   }
   return acc;
@@ -287,12 +320,13 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
 
 // The same sum with every product in fp64, for segments whose fp32 products leave the range.
 template <typename T, int NORM>
-__device__ __noinline__ double segment_acc_wide(const TensorsParams& prm, const Segment& s,
-                                                uint32_t lane) {
+__device__ __forceinline__ double segment_acc_wide(const TensorsParams& prm, const Segment& s,
+                                                   uint32_t lane) {
   const TensorEntry& e = prm.entries[s.tensor];
   const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
   Walk w = grad_walk(e, s.start + lane, 32);
   double sum = 0.0;
+#pragma unroll 1
   for (uint32_t i = lane; i < s.n; i += 32, w.next()) {
     const double x = T::to_float(g[w.offset()]);
     sum += NORM == kNorm2 ? x * x : fabs(x);
@@ -301,13 +335,13 @@ __device__ __noinline__ double segment_acc_wide(const TensorsParams& prm, const 
 }
 
 // The sum of a segment, in every lane of its warp.
-template <int NORM>
+template <int NORM, bool KEEP>
 __device__ __forceinline__ double segment_sum(const TensorsParams& prm, const Segment& s,
-                                              uint32_t lane) {
+                                              uint32_t lane, uint4* keep) {
   double x = 0.0;
   with_type(s.dtype, [&](auto type) {
     using T = decltype(type);
-    const NormAcc<NORM> acc = segment_acc<T, NORM>(prm, s, lane);
+    const NormAcc<NORM> acc = segment_acc<T, NORM, KEEP>(prm, s, lane, keep);
     x = warp_join<NORM>(NORM == kNormMax ? static_cast<double>(acc.mx) : acc.s);
     if constexpr (NORM != kNormMax) {
       // fp32 squares overflow above 1.8e19 and lose bits below 1e-19; sums of |x| overflow
@@ -346,6 +380,7 @@ __device__ __forceinline__ void write_clip(const TensorsParams& prm, double sum,
   prm.header[ABS_GRAD_FLAGS] = c.finite ? 0.0 : static_cast<double>(ABS_FLAG_NONFINITE);
   prm.norms_out[0] = static_cast<float>(c.norm);
   prm.norms_out[1] = static_cast<float>(c.coef);
+  *prm.factor = c.finite ? c.factor : __int_as_float(0x7fc00000);
 }
 
 template <int NORM>
@@ -353,145 +388,233 @@ __device__ __forceinline__ void write_norm(const TensorsParams& prm, int t, doub
   prm.norms_out[2 + t] = static_cast<float>(fabs(prm.scale) * (NORM == kNorm2 ? sqrt(x) : x));
 }
 
-// The sums of one block.  Segments are dealt out in order, so a tensor that is neither the first
-// nor the last of a warp lies in that warp whole, and one that is neither the first nor the last
-// of a block in that block: its norm is written where it is known.  What remains of a warp, its
-// parts of its first and its last tensor, is joined through shared memory; what remains of a block
-// goes to edge_sum.
-struct WarpParts {
-  double first[kNormWarps], last[kNormWarps];
-  int first_tensor[kNormWarps];  // -1: the warp does not begin inside a tensor
-  int last_tensor[kNormWarps];   // -1: the warp has no work
+// What a warp's rows leave to be joined.  A tensor that begins and ends in them is done
+// with there.  There may be one at the front that began before them (kHead: and ends in them), and
+// one at the back that goes on after them (kTail: and begins in them; kThrough: began before them).
+enum { kHead = 1, kTail = 2, kThrough = 4 };
+template <int WARPS>
+struct BlockParts {
+  double head[WARPS], open[WARPS], sum[WARPS];
+  int tensor[WARPS], state[WARPS];
 };
-template <int NORM>
-__device__ __forceinline__ double block_sums(const TensorsParams& prm, WarpParts& parts,
-                                             double* sm) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int w = blockIdx.x * kNormWarps + warp;
-  int first_tensor = -1, tensor = -1;
-  double first = 0.0, x = 0.0, sum = 0.0;
-  if (w < prm.n_warps) {
-    const int begin = prm.warp_first[w], end = prm.warp_first[w + 1];
-    bool closed = false;  // a tensor has ended in this warp
-    for (int i = begin; i < end; ++i) {
-      const Segment s = prm.segments[i];
-      if (tensor >= 0 && s.tensor != tensor) {
-        if (!closed && prm.entries[tensor].first_seg < begin) {
-          first_tensor = tensor;
-          first = x;
-        } else if (lane == 0) {
-          write_norm<NORM>(prm, tensor, x);
-        }
-        closed = true;
-        x = 0.0;
-      }
-      tensor = s.tensor;
-      const double y = segment_sum<NORM>(prm, s, lane);
-      x = norm_join<NORM>(x, y);
+
+// One warp's rows; returns their sum.
+template <int NORM, bool KEEP, int WARPS>
+__device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segment& opening,
+                                           BlockParts<WARPS>& parts, uint4* keep) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double sum = 0.0, x = 0.0, head = 0.0;
+  int state = 0, tensor = -1;
+  bool begun = false, open = false;
+  Segment s = opening;
+  if (s.tensor >= 0) {
+    for (int k = 0;; ++k) {
+      Segment next = s;
+      if (k < opening.more) next = prm.further[opening.next + k];
+      const double y = segment_sum<NORM, KEEP>(prm, s, lane, keep);
+      if (KEEP && (s.flags & kEntryVecG))
+        keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
       sum = norm_join<NORM>(sum, y);
+      x = norm_join<NORM>(x, y);
+      begun |= (s.pos & kSegBegins) != 0;
+      open = !(s.pos & kSegEnds);
+      tensor = s.tensor;
+      if (!open) {
+        if (begun) {
+          if (lane == 0) write_norm<NORM>(prm, tensor, x);
+        } else {
+          head = x;
+          state = kHead;
+        }
+        x = 0.0;
+        begun = false;
+      }
+      if (k == opening.more) break;
+      s = next;
     }
-    if (!closed && prm.entries[tensor].first_seg < begin) {
-      first_tensor = tensor;
-      first = x;
-    }
+    if (open) state |= begun ? kTail : kThrough;
   }
   if (lane == 0) {
-    parts.first[warp] = first;
-    parts.last[warp] = x;
-    parts.first_tensor[warp] = first_tensor;
-    parts.last_tensor[warp] = tensor;
-    sm[warp] = sum;
+    parts.head[warp] = head;
+    parts.open[warp] = x;
+    parts.tensor[warp] = tensor;
+    parts.state[warp] = state;
   }
-  __syncthreads();
-  // each warp: the tensor that it ends with, unless that one began in an earlier warp of the block
-  if (tensor >= 0 && !(warp > 0 && first_tensor == tensor)) {
-    double y = lane == warp ? x
-               : lane > warp && parts.first_tensor[lane] == tensor ? parts.first[lane]
-                                                                   : 0.0;
-    y = warp_join<NORM>(y);
-    const int seg = prm.entries[tensor].first_seg, n_seg = prm.entries[tensor].n_segs;
-    const int w0 = blockIdx.x * kNormWarps, w1 = min(w0 + kNormWarps, prm.n_warps);
-    const bool from = seg >= prm.warp_first[w0], to = seg + n_seg <= prm.warp_first[w1];
-    if (lane == 0) {
-      if (from && to) write_norm<NORM>(prm, tensor, y);
-      if (!from) prm.edge_sum[2 * blockIdx.x] = y;
-      if (!to) prm.edge_sum[2 * blockIdx.x + 1] = y;
-    }
-  }
-  if (threadIdx.x == 0 && first_tensor >= 0 && first_tensor != tensor)
-    prm.edge_sum[2 * blockIdx.x] = first;
-  if (blockIdx.x == 0)
-    for (int i = threadIdx.x; i < prm.n_empty; i += kNormThreads)
-      write_norm<NORM>(prm, prm.empty[i], 0.0);
-  return warp_join<NORM>(sm[lane]);
+  return sum;
 }
 
-// The norm of a tensor that lies in several blocks, by one warp.
-template <int NORM>
-__device__ __forceinline__ void join_spanning(const TensorsParams& prm, int i) {
-  const int lane = threadIdx.x & 31;
-  const Spanning s = prm.spanning[i];
-  double x = 0.0;
-  for (int b = s.first + lane; b <= s.last; b += 32)
-    x = norm_join<NORM>(x, __ldcg(prm.edge_sum + 2 * b + (b == s.first ? 1 : 0)));
+// Joins the parts of a block's warps, each tensor by the warp in which it begins (by warp 0, if it
+// began before the block); `edge[0]` and `edge[1]` receive the parts of a tensor that the block
+// shares with the one before and the one after it.  After a __syncthreads.
+template <int NORM, int WARPS>
+__device__ __forceinline__ void join_parts(const TensorsParams& prm, const BlockParts<WARPS>& parts,
+                                          double* edge) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int state = lane < WARPS ? parts.state[lane] : 0;
+  const uint32_t heads = __ballot_sync(0xffffffffu, state & kHead);
+  const uint32_t throughs = __ballot_sync(0xffffffffu, state & kThrough);
+  const int mine = parts.state[warp];
+  if (warp == 0 && lane == 0 && (mine & kHead)) edge[0] = parts.head[0];
+  if (!((mine & kTail) || (warp == 0 && (mine & kThrough)))) return;
+  const uint32_t stop = ~throughs & ~((2u << warp) - 1u);  // warps after this one that end it
+  const uint32_t u = stop ? static_cast<uint32_t>(__ffs(stop)) - 1u : 32u;
+  const bool ends = u < 32 && ((heads >> u) & 1u);
+  double x = lane == warp || (lane > warp && lane < u && lane < WARPS) ? parts.open[lane]
+             : lane == u && ends                                       ? parts.head[lane]
+                                                                       : 0.0;
   x = warp_join<NORM>(x);
-  if (lane == 0) write_norm<NORM>(prm, s.tensor, x);
+  if (lane == 0) {
+    if ((mine & kTail) && ends) write_norm<NORM>(prm, parts.tensor[warp], x);
+    if (!(mine & kTail)) edge[0] = x;
+    if (!ends) edge[1] = x;
+  }
 }
 
-// The power sum of the list from the sums of the blocks, in every lane.
-template <int NORM>
-__device__ __forceinline__ double join_blocks(const TensorsParams& prm) {
+// The sum of a block from those of its warps, in every lane.  After a __syncthreads.
+template <int NORM, int WARPS>
+__device__ __forceinline__ double join_warps(const double* sums) {
+  const uint32_t lane = threadIdx.x & 31;
+  return warp_join<NORM>(lane < WARPS ? sums[lane] : 0.0);
+}
+
+// The norm of a tensor that several blocks share, by one warp.  edge(b, i): edge i of block b.
+template <int NORM, typename F>
+__device__ __forceinline__ void join_spanning(const TensorsParams& prm, const Spanning& s, F&& edge) {
   double x = 0.0;
-  for (int b = threadIdx.x & 31; b < static_cast<int>(gridDim.x); b += 32)
-    x = norm_join<NORM>(x, __ldcg(prm.block_sum + b));
-  return warp_join<NORM>(x);
+  for (int b = s.first + (threadIdx.x & 31); b <= s.last; b += 32)
+    x = norm_join<NORM>(x, edge(b, b == s.first ? 1 : 0));
+  x = warp_join<NORM>(x);
+  if ((threadIdx.x & 31) == 0) write_norm<NORM>(prm, s.tensor, x);
 }
 
-// Every warp sums its segments, every block its warps, the block that finishes last the blocks: one
-// launch, and no order of finishing shows in a sum.
-template <int NORM>
-__global__ void __launch_bounds__(kNormThreads, 1)
-    tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
-  __shared__ WarpParts parts;
-  __shared__ double sm[kNormWarps];
-  __shared__ unsigned int s_ticket;
-  grid_dependency_wait();
-  const double sum = block_sums<NORM>(prm, parts, sm);
-  grid_launch_dependents();
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    prm.block_sum[blockIdx.x] = sum;
+// Counts this block off; true in the whole warp if it was the last of `of` blocks.  Its sums are
+// visible to the warp that gets true, and the counter is back at zero for the next call.
+__device__ __forceinline__ bool last_of(unsigned int* ticket, unsigned int of) {
+  unsigned int before = 0;
+  if ((threadIdx.x & 31) == 0) {
     __threadfence();
-    s_ticket = atomicAdd(prm.ticket, 1u);
+    before = atomicAdd(ticket, 1u);
+    if (before == of - 1) *ticket = 0;
+    __threadfence();
   }
+  return __shfl_sync(0xffffffffu, before, 0) == of - 1;
+}
+
+// Every warp sums its rows, every block its warps; the block that finishes last joins the blocks,
+// and of the blocks that share a tensor the last one joins that tensor: one launch, and no order of
+// finishing shows in a sum.
+template <int NORM, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1)
+    tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
+  __shared__ BlockParts<WARPS> parts;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // the tables were there before any kernel of the stream
+  const Segment opening = prm.opening[blockIdx.x * WARPS + warp];
+  Shared2 shared{-1, -1};
+  if (warp == 1 || warp == 2) shared = prm.shared[blockIdx.x];
+  grid_dependency_wait();
+  double sum = warp_sum<NORM, false>(prm, opening, parts, nullptr);
+  if (lane == 0) parts.sum[warp] = sum;
+  grid_launch_dependents();
   __syncthreads();
-  if (s_ticket != gridDim.x - 1) return;
-  __threadfence();
-  const int warp = threadIdx.x >> 5;
+  join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x);
   if (warp == 0) {
-    const double total = join_blocks<NORM>(prm);
-    if (threadIdx.x == 0) {
-      write_clip(prm, total, clip_of(total, NORM, prm.scale, prm.max_norm));
-      *prm.ticket = 0;  // ready for the next call
-    }
+    sum = join_warps<NORM, WARPS>(parts.sum);
+    if (lane == 0) prm.block_sum[blockIdx.x] = sum;
   }
-  for (int i = (warp + kNormWarps - 1) % kNormWarps; i < prm.n_spanning; i += kNormWarps)
-    join_spanning<NORM>(prm, i);
+  const int i = warp == 1 ? shared.before : warp == 2 ? shared.after : -1;
+  Spanning span;
+  if (i >= 0) span = prm.spanning[i];
+  __syncthreads();  // all edges are written
+  if (warp == 0 && last_of(prm.tickets, gridDim.x)) {
+    double total = 0.0;
+    for (int b = lane; b < static_cast<int>(gridDim.x); b += 32)
+      total = norm_join<NORM>(total, __ldcg(prm.block_sum + b));
+    total = warp_join<NORM>(total);
+    if (lane == 0) write_clip(prm, total, clip_of(total, NORM, prm.scale, prm.max_norm));
+  }
+  if (i >= 0 && last_of(prm.tickets + 1 + i, span.last - span.first + 1))
+    join_spanning<NORM>(prm, span, [&](int b, int k) { return __ldcg(prm.edge_sum + 2 * b + k); });
+  if (blockIdx.x == 0)
+    for (int k = threadIdx.x; k < prm.n_empty; k += WARPS * 32)
+      write_norm<NORM>(prm, prm.empty[k], 0.0);
+}
+
+// Norm and factor from a power sum that comes from elsewhere (added up over ranks).
+__global__ void tensors_clip_kernel(const __grid_constant__ TensorsParams prm) {
+  grid_dependency_wait();
+  const double sum = __ldcg(prm.sum_in);
+  if (threadIdx.x == 0) write_clip(prm, sum, clip_of(sum, prm.norm_type, prm.scale, prm.max_norm));
 }
 
 // ---- scaling -------------------------------------------------------------------------
-// The factor that this call's gradients are multiplied by, the same in every thread.
-__device__ __forceinline__ Clip block_clip(const TensorsParams& prm, Clip* sm) {
-  if (threadIdx.x == 0) {
-    const double sum = __ldcg(prm.sum_in ? prm.sum_in : prm.header + ABS_GRAD_SUM);
-    *sm = clip_of(sum, prm.norm_type, prm.scale, prm.max_norm);
-    // a sum from elsewhere (added up over ranks): norm and coefficient follow it
-    if (prm.sum_in && blockIdx.x == 0) write_clip(prm, sum, *sm);
-  }
-  __syncthreads();
-  return *sm;
+// Values of a type known at run time.  A list mixes types, and nine loops for the pairs of them take
+// more registers than one loop with uniform branches takes time.
+__device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype) {
+  if (dtype == ABS_F32) return static_cast<const float*>(p)[i];
+  const uint16_t x = static_cast<const uint16_t*>(p)[i];
+  return dtype == ABS_BF16 ? TBF16::to_float(x) : TF16::to_float(x);
 }
+__device__ __forceinline__ void store_any(void* p, int64_t i, int dtype, float x) {
+  if (dtype == ABS_F32)
+    static_cast<float*>(p)[i] = x;
+  else
+    static_cast<uint16_t*>(p)[i] = dtype == ABS_BF16 ? TBF16::from_float(x) : TF16::from_float(x);
+}
+// The 4 (fp32) or 8 values of 16 bytes of input, scaled, to an output whose groups of 8 are aligned.
+__device__ __forceinline__ void store_scaled(const uint4& raw, int in, void* p, int64_t i, int out,
+                                             float factor) {
+  float x[8] = {};
+  if (in == ABS_F32)
+    TF32::unpack(raw, x);
+  else if (in == ABS_BF16)
+    TBF16::unpack(raw, x);
+  else
+    TF16::unpack(raw, x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] *= factor;
+  if (out == ABS_F32) {
+    float* y = static_cast<float*>(p) + i;
+    st_stream_16(y, make_float4(x[0], x[1], x[2], x[3]));
+    if (in != ABS_F32) st_stream_16(y + 4, make_float4(x[4], x[5], x[6], x[7]));
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      w[k] = out == ABS_BF16
+                 ? pack_bf16x2(x[2 * k], x[2 * k + 1])
+                 : static_cast<uint32_t>(TF16::from_float(x[2 * k])) |
+                       (static_cast<uint32_t>(TF16::from_float(x[2 * k + 1])) << 16);
+    uint16_t* y = static_cast<uint16_t*>(p) + i;
+    if (in == ABS_F32)
+      __stcs(reinterpret_cast<uint2*>(y), make_uint2(w[0], w[1]));
+    else
+      __stcs(reinterpret_cast<uint4*>(y), make_uint4(w[0], w[1], w[2], w[3]));
+  }
+}
+// n elements from `first` on, every step-th of them by this thread.
+__device__ __forceinline__ void scale_walk(const TensorEntry& e, int64_t first, uint32_t i0,
+                                           uint32_t n, uint32_t step, float factor, bool in_place) {
+  constexpr int kBatch = 8;
+  Walk wi = grad_walk(e, first + i0, step);
+  Walk wo = in_place ? wi : out_walk(e, first + i0, step);
+  void* y = in_place ? const_cast<void*>(e.g) : e.out;
+  const int in = e.g_dtype, out = in_place ? e.g_dtype : e.out_dtype;
+  for (; i0 < n; i0 += kBatch * step) {
+    float x[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (i0 + j * step < n) x[j] = load_any(e.g, wi.offset(), in);
+      wi.next();
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (i0 + j * step < n) store_any(y, wo.offset(), out, factor * x[j]);
+      wo.next();
+    }
+  }
+}
+
 
 // Eight consecutive values, 16- or 32-byte aligned.
 template <typename T>
@@ -526,17 +649,13 @@ __device__ __forceinline__ void store8(typename T::scalar* p, const float* x) {
 
 template <typename TI, typename TO>
 __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange& r, float factor,
-                                           const void* in, void* out, bool in_place, bool vec) {
-  const typename TI::scalar* g = static_cast<const typename TI::scalar*>(in);
+                                           void* out, bool in_place) {
+  const typename TI::scalar* g = static_cast<const typename TI::scalar*>(e.g);
   typename TO::scalar* y = static_cast<typename TO::scalar*>(out);
   const uint32_t tid = threadIdx.x;
-  if (vec) {
+  if (e.flags & kEntryVecClip) {
     // rows are whole vectors here, and there is no head then: the walk goes by vectors
     constexpr int kBatch = 4;
-    auto one = [&](uint32_t i) {
-      y[r.start + i] = TO::from_float(factor * TI::to_float(g[r.start + i]));
-    };
-    if (tid < r.head) one(tid);
     const uint32_t nv = (r.n - r.head) / 8;
     const int64_t first = r.start + r.head + tid * 8;
     Walk wi = grad_walk(e, first, 8 * kTensorThreads);
@@ -560,8 +679,13 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
         wo.next();
       }
     }
-    const uint32_t i = r.head + nv * 8 + tid;
-    if (i < r.n) one(i);  // only without rows: the elements of a view with rows are whole vectors
+    // head and rest of a tensor without rows: the elements of a view with rows are whole vectors
+    const auto one = [&](uint32_t i) {
+      y[r.start + i] = TO::from_float(factor * TI::to_float(g[r.start + i]));
+    };
+    if (tid < r.head) one(tid);
+    const uint32_t rest = r.head + nv * 8 + tid;
+    if (rest < r.n) one(rest);
   } else {
     constexpr int kBatch = 16;
     Walk wi = grad_walk(e, r.start + tid, kTensorThreads);
@@ -583,27 +707,24 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
   }
 }
 
+// One CTA per unit, the last unit of the list first.
 __global__ void __launch_bounds__(kTensorThreads, 3)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
-  __shared__ Clip s_clip;
+  const int u = prm.n_scale - 1 - blockIdx.x;
+  const TensorEntry& e = prm.entries[prm.scale_tensor[u]];
+  const UnitRange r = unit_range(e, u - e.first_scale, prm.scale_unit);
   grid_dependency_wait();
-  const Clip clip = block_clip(prm, &s_clip);
-  if (prm.n_units == 0) return;
-  if (prm.in_place && clip.factor == 1.f) return;  // x * 1 is x
-  const int u = prm.n_units - 1 - blockIdx.x;  // last read, first scaled: it may still be in L2
-  const TensorEntry& e = prm.entries[prm.unit_tensor[u]];
-  const UnitRange r = unit_range(e, u, prm.unit);
+  float factor = __ldcg(prm.factor);
+  if (factor != factor) factor = static_cast<float>(prm.scale);  // not finite: not clipped
+  if (prm.in_place && factor == 1.f) return;                     // x * 1 is x
   with_type(e.g_dtype, [&](auto ti) {
     using TI = decltype(ti);
-    if (prm.in_place) {
-      unit_scale<TI, TI>(e, r, clip.factor, e.g, const_cast<void*>(e.g), true,
-                         e.flags & kEntryVecClip);
-    } else {
+    if (prm.in_place)
+      unit_scale<TI, TI>(e, r, factor, const_cast<void*>(e.g), true);
+    else
       with_type(e.out_dtype, [&](auto to) {
-        using TO = decltype(to);
-        unit_scale<TI, TO>(e, r, clip.factor, e.g, e.out, false, e.flags & kEntryVecClip);
+        unit_scale<TI, decltype(to)>(e, r, factor, e.out, false);
       });
-    }
   });
 }
 
@@ -621,62 +742,253 @@ __device__ __forceinline__ void adamw_quad(const AdamScalars& a, float2 g0, floa
   v = make_float4(v0.x, v0.y, v1.x, v1.y);
 }
 
-__global__ void __launch_bounds__(kTensorThreads)
+
+// One coordinate: element `at` of the gradient, element i of the other arrays.
+struct StateArrays {
+  float *p, *m, *v;
+  uint16_t* p16;
+};
+__device__ __forceinline__ void adamw_one(const AdamScalars& a, const StateArrays& s, int64_t i,
+                                          float g) {
+  float w = s.p[i], m = s.m[i], v = s.v[i];
+  adamw_elem(a, a.omb1, a.omb2, g, w, m, v);
+  s.p[i] = w, s.m[i] = m, s.v[i] = v;
+  if (s.p16) s.p16[i] = to_bf16(w);
+}
+// n elements from `first` on, every step-th of them by this thread.
+template <typename T>
+__device__ __forceinline__ void adamw_walk(const AdamScalars& a, const StateArrays& s,
+                                           const TensorEntry& e, int64_t first, uint32_t i0,
+                                           uint32_t n, uint32_t step, float factor) {
+  constexpr int kBatch = 4;
+  const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
+  Walk wg = grad_walk(e, first + i0, step);
+  for (; i0 < n; i0 += kBatch * step) {
+    typename T::scalar x[kBatch];
+    float w[kBatch], m[kBatch], v[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int64_t i = first + i0 + j * step;
+      if (i0 + j * step < n) x[j] = g[wg.offset()], w[j] = s.p[i], m[j] = s.m[i], v[j] = s.v[i];
+      wg.next();
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int64_t i = first + i0 + j * step;
+      if (i0 + j * step < n) {
+        adamw_elem(a, a.omb1, a.omb2, factor * T::to_float(x[j]), w[j], m[j], v[j]);
+        s.p[i] = w[j], s.m[i] = m[j], s.v[i] = v[j];
+        if (s.p16) s.p16[i] = to_bf16(w[j]);
+      }
+    }
+  }
+}
+
+// One CTA per unit, the last unit of the list first.  After this call's norm kernel the first loads
+// are made before the factor is waited for: that kernel lets this one start only after its own wait,
+// so whatever wrote the tensors before is done.
+__global__ void __launch_bounds__(kTensorThreads, 4)
     tensors_adamw_kernel(const __grid_constant__ TensorsParams prm,
                          const __grid_constant__ GroupScalars groups, int clipped) {
-  __shared__ Clip s_clip;
-  grid_dependency_wait();
-  float factor = static_cast<float>(prm.scale);
-  if (clipped) {
-    const Clip clip = block_clip(prm, &s_clip);
-    if (!clip.finite) return;  // no update from a gradient that is not finite
-    factor = clip.factor;
-  }
-  if (prm.n_units == 0) return;
-  const int u = prm.n_units - 1 - blockIdx.x;
-  const TensorEntry& e = prm.entries[prm.unit_tensor[u]];
-  const UnitRange r = unit_range(e, u, prm.unit);
+  const bool after_norm = prm.after_norm;
+  if (!after_norm) grid_dependency_wait();
+  const int u = prm.n_adamw - 1 - blockIdx.x;
+  const TensorEntry& e = prm.entries[prm.adamw_tensor[u]];
+  const UnitRange r = unit_range(e, u - e.first_adamw, kAdamwUnit);
   const AdamScalars& a = groups.a[e.group];
-  float *p = e.p + r.start, *m = e.m + r.start, *v = e.v + r.start;
-  uint16_t* p16 = e.p16 ? e.p16 + r.start : nullptr;
+  const StateArrays state{e.p, e.m, e.v, e.p16};
   const uint32_t tid = threadIdx.x;
+  float factor = static_cast<float>(prm.scale);
   with_type(e.g_dtype, [&](auto type) {
     using T = decltype(type);
     const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
-    auto one = [&](uint32_t i, int64_t at) {
-      float w = p[i], mi = m[i], vi = v[i];
-      adamw_elem(a, a.omb1, a.omb2, factor * T::to_float(g[at]), w, mi, vi);
-      p[i] = w, m[i] = mi, v[i] = vi;
-      if (p16) p16[i] = to_bf16(w);
-    };
-    if (e.flags & kEntryVecAdam) {
-      if (tid < r.head) one(tid, r.start + tid);
-      const uint32_t nv = (r.n - r.head) / 8;
-      Walk wg = grad_walk(e, r.start + r.head + tid * 8, 8 * kTensorThreads);
-      for (uint32_t q = tid; q < nv; q += kTensorThreads, wg.next()) {
-        const uint32_t i = r.head + q * 8;
-        const Vec8<T> raw = load8<T>(g + wg.offset());
-        Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
-        float x[8];
-        unpack8<T>(raw, x);
-        const float2 g0 = make_float2(factor * x[0], factor * x[1]);
-        const float2 g1 = make_float2(factor * x[2], factor * x[3]);
-        const float2 g2 = make_float2(factor * x[4], factor * x[5]);
-        const float2 g3 = make_float2(factor * x[6], factor * x[7]);
-        adamw_quad(a, g0, g1, w.lo, mm.lo, vv.lo);
-        adamw_quad(a, g2, g3, w.hi, mm.hi, vv.hi);
-        st_stream_32(p + i, w.lo, w.hi);
-        st_stream_32(m + i, mm.lo, mm.hi);
-        st_stream_32(v + i, vv.lo, vv.hi);
-        if (p16) st_bf16x8(p16 + i, w.lo, w.hi);
+    if (!(e.flags & kEntryVecAdam)) {
+      if (after_norm) grid_dependency_wait();
+      if (clipped) factor = __ldcg(prm.factor);
+      if (factor != factor) return;  // no update from a gradient that is not finite
+      adamw_walk<T>(a, state, e, r.start, tid, r.n, kTensorThreads, factor);
+      return;
+    }
+    const uint32_t nv = (r.n - r.head) / 8;
+    const int64_t first = r.start + r.head;
+    float *p = e.p + first, *m = e.m + first, *v = e.v + first;
+    Walk wg = grad_walk(e, first + tid * 8, 8 * kTensorThreads);
+    bool have = false;
+    for (uint32_t q = tid; q < nv; q += kTensorThreads, wg.next()) {
+      const uint32_t i = q * 8;
+      const Vec8<T> raw = load8<T>(g + wg.offset());
+      Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
+      if (!have) {
+        if (after_norm) grid_dependency_wait();
+        if (clipped) factor = __ldcg(prm.factor);
+        if (factor != factor) return;
+        have = true;
       }
-      const uint32_t i = r.head + nv * 8 + tid;
-      if (i < r.n) one(i, r.start + i);
-    } else {
-      Walk wg = grad_walk(e, r.start + tid, kTensorThreads);
-      for (uint32_t i = tid; i < r.n; i += kTensorThreads, wg.next()) one(i, wg.offset());
+      float x[8];
+      unpack8<T>(raw, x);
+      const float2 g0 = make_float2(factor * x[0], factor * x[1]);
+      const float2 g1 = make_float2(factor * x[2], factor * x[3]);
+      const float2 g2 = make_float2(factor * x[4], factor * x[5]);
+      const float2 g3 = make_float2(factor * x[6], factor * x[7]);
+      adamw_quad(a, g0, g1, w.lo, mm.lo, vv.lo);
+      adamw_quad(a, g2, g3, w.hi, mm.hi, vv.hi);
+      st_stream_32(p + i, w.lo, w.hi);
+      st_stream_32(m + i, mm.lo, mm.hi);
+      st_stream_32(v + i, vv.lo, vv.hi);
+      if (e.p16) st_bf16x8(e.p16 + first + i, w.lo, w.hi);
+    }
+    // head and rest of a tensor whose gradient has no rows
+    const uint32_t rest = r.head + nv * 8 + tid;
+    if (tid < r.head || rest < r.n) {
+      if (!have) {
+        if (after_norm) grid_dependency_wait();
+        if (clipped) factor = __ldcg(prm.factor);
+        if (factor != factor) return;
+      }
+      if (tid < r.head) adamw_one(a, state, r.start + tid, factor * T::to_float(g[r.start + tid]));
+      if (rest < r.n) adamw_one(a, state, r.start + rest, factor * T::to_float(g[r.start + rest]));
     }
   });
+}
+
+// ---- small lists: everything in one cluster -------------------------------------------------
+// Norm and second pass in one launch.  Up to kClusterBlocks blocks, launched as one cluster, hold
+// the whole list in shared memory; the cluster's barrier takes the place of tickets, and sums are
+// read from the other blocks' shared memory.
+enum { kOpNone = 0, kOpScale = 1, kOpAdamw = 2 };
+
+__device__ __forceinline__ void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A double in another block's shared memory, at the place where `p` points to in this one's.
+__device__ __forceinline__ double ld_block(const double* p, int block) {
+  uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(p));
+  double x;
+  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(a) : "r"(block));
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(a) : "memory");
+  return x;
+}
+
+template <int OP>
+__device__ __forceinline__ void segment_apply(const TensorsParams& prm, const GroupScalars& groups,
+                                              const Segment& s, uint32_t lane, float factor,
+                                              const uint4* keep) {
+  const TensorEntry& e = prm.entries[s.tensor];
+  const int in = s.dtype;
+  const uint32_t per = in == ABS_F32 ? 4 : 8;
+  const uint32_t nv = (s.n - s.head) / per;
+  const int64_t first = s.start + s.head;
+  if constexpr (OP == kOpScale) {
+    const int out = prm.in_place ? in : e.out_dtype;
+    void* y = prm.in_place ? const_cast<void*>(e.g) : e.out;
+    if (!(s.flags & kEntryVecClip)) {
+      scale_walk(e, s.start, lane, s.n, 32, factor, prm.in_place);
+      return;
+    }
+    for (uint32_t v = lane; v < nv; v += 32)
+      store_scaled(keep[v - lane], in, y, first + static_cast<int64_t>(v) * per, out, factor);
+    const auto one = [&](uint32_t i) {
+      store_any(y, s.start + i, out, factor * load_any(e.g, s.start + i, in));
+    };
+    if (lane < s.head) one(lane);
+    const uint32_t i = s.head + nv * per + lane;
+    if (i < s.n) one(i);
+  } else {
+    const AdamScalars& a = groups.a[e.group];
+    const StateArrays state{e.p, e.m, e.v, e.p16};
+    if (!(s.flags & kEntryVecAdam)) {
+      with_type(in, [&](auto type) {
+        adamw_walk<decltype(type)>(a, state, e, s.start, lane, s.n, 32, factor);
+      });
+      return;
+    }
+    for (uint32_t v = lane; v < nv; v += 32) {
+      const int64_t i = first + static_cast<int64_t>(v) * per;
+      float x[8] = {};
+      const uint4 raw = keep[v - lane];
+      if (in == ABS_F32)
+        TF32::unpack(raw, x);
+      else if (in == ABS_BF16)
+        TBF16::unpack(raw, x);
+      else
+        TF16::unpack(raw, x);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (k == 1 && in == ABS_F32) break;
+        const int64_t j = i + 4 * k;
+        float4 w = ld_state_16(e.p + j), m = ld_state_16(e.m + j), q = ld_state_16(e.v + j);
+        adamw_quad(a, make_float2(factor * x[4 * k], factor * x[4 * k + 1]),
+                   make_float2(factor * x[4 * k + 2], factor * x[4 * k + 3]), w, m, q);
+        st_stream_16(e.p + j, w);
+        st_stream_16(e.m + j, m);
+        st_stream_16(e.v + j, q);
+        if (e.p16) st_bf16x4(e.p16 + j, w);
+      }
+    }
+    const auto one = [&](uint32_t i) {
+      adamw_one(a, state, s.start + i, factor * load_any(e.g, s.start + i, in));
+    };
+    if (lane < s.head) one(lane);
+    const uint32_t i = s.head + nv * per + lane;
+    if (i < s.n) one(i);
+  }
+}
+
+template <int NORM, int OP>
+__global__ void __launch_bounds__(kClusterWarps * 32)
+    tensors_cluster_kernel(const __grid_constant__ TensorsParams prm,
+                           const __grid_constant__ GroupScalars groups, int rows) {
+  extern __shared__ uint4 kept[];  // `rows` rows for each warp
+  __shared__ BlockParts<kClusterWarps> parts;
+  __shared__ double s_edge[2], s_sum;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int blocks = gridDim.x;
+  const Segment opening = prm.opening[blockIdx.x * kClusterWarps + warp];
+  uint4* keep = kept + warp * rows * 32 + lane;
+  grid_dependency_wait();
+  double sum = warp_sum<NORM, OP != kOpNone>(prm, opening, parts, keep);
+  if (lane == 0) parts.sum[warp] = sum;
+  __syncthreads();
+  join_parts<NORM>(prm, parts, s_edge);
+  if (warp == 0) {
+    sum = join_warps<NORM, kClusterWarps>(parts.sum);
+    if (lane == 0) s_sum = sum;
+  }
+  cluster_arrive();
+  // tensors that several blocks share, dealt out to the warps of the cluster
+  const int w = blockIdx.x + blocks * warp;
+  Spanning span{-1, 0, 0, 0};
+  if (w < prm.n_spanning) span = prm.spanning[w];  // at most blocks - 1 of them
+  cluster_wait();
+  grid_launch_dependents();
+  const double total = warp_join<NORM>(lane < blocks ? ld_block(&s_sum, lane) : 0.0);
+  if (span.tensor >= 0)
+    join_spanning<NORM>(prm, span, [&](int b, int k) { return ld_block(s_edge + k, b); });
+  cluster_arrive();  // nothing more is read from other blocks
+  const Clip clip = clip_of(total, NORM, prm.scale, prm.max_norm);
+  if (blockIdx.x == 0) {
+    if (threadIdx.x == 0) write_clip(prm, total, clip);
+    for (int i = threadIdx.x; i < prm.n_empty; i += kClusterWarps * 32)
+      write_norm<NORM>(prm, prm.empty[i], 0.0);
+  }
+  const bool skip = OP == kOpNone || (OP == kOpAdamw && !clip.finite) ||
+                    (OP == kOpScale && prm.in_place && clip.factor == 1.f);
+  if (!skip && opening.tensor >= 0) {
+    if constexpr (OP != kOpNone) {
+      Segment s = opening;
+      for (int k = 0;; ++k) {
+        segment_apply<OP>(prm, groups, s, lane, clip.factor, keep);
+        if (s.flags & kEntryVecG)
+          keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
+        if (k == opening.more) break;
+        s = prm.further[opening.next + k];
+      }
+    }
+  }
+  cluster_wait();
 }
 
 }  // namespace absnt

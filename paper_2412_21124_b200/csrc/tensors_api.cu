@@ -1,7 +1,9 @@
 // C ABI of the calls over a list of tensors: the plan of a list (host), its upload, and the norm,
 // clipping and AdamW calls.
 #include <algorithm>
+#include <atomic>
 #include <cstring>
+#include <mutex>
 #include <vector>
 
 #include "host_checks.cuh"
@@ -14,6 +16,9 @@ namespace {
 
 constexpr uint64_t kPlanMagic = 0x6e616c7054534241ull;  // "ABSTplan"
 constexpr int64_t kMaxRow = int64_t{1} << 30;
+// Most elements that AdamW takes in one cluster: above, the state's traffic wants all SMs.
+constexpr int64_t kClusterAdamw = 128 * 1024;
+constexpr size_t kKeepBytes = size_t{kClusterWarps} * 512;  // one row of each warp of a block
 constexpr int64_t kMaxElements = int64_t{1} << 46;
 constexpr int64_t kMaxUnits = int64_t{1} << 30;
 enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
@@ -21,62 +26,73 @@ enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
 // Host image of a plan: this header, then the tables in the order of `Image`.
 struct PlanHeader {
   uint64_t magic;
-  int32_t n, n_units, n_segments, n_warps, n_spanning, n_empty, unit, roles, n_groups, pad;
+  int32_t n, n_scale, n_adamw, n_further, n_spanning, n_empty, scale_unit;
+  int32_t blocks, warps, rows;  // rows: of each warp
+  int32_t roles, n_groups;
+  int64_t total;  // elements
+  bool cluster() const { return warps == kClusterWarps; }
 };
 // Offsets of the tables in the image (which the device holds as well).
 struct Image {
-  size_t segments, spanning, warp_first, unit_tensor, empty, bytes;
+  size_t opening, further, spanning, shared, scale_tensor, adamw_tensor, empty, bytes;
   explicit Image(const PlanHeader& h) {
-    segments = static_cast<size_t>(h.n) * sizeof(TensorEntry);
-    spanning = segments + static_cast<size_t>(h.n_segments) * sizeof(Segment);
-    warp_first = spanning + static_cast<size_t>(h.n_spanning) * sizeof(Spanning);
-    unit_tensor = warp_first + 4 * (static_cast<size_t>(h.n_warps) + 1);
-    empty = unit_tensor + 4 * static_cast<size_t>(h.n_units);
+    opening = (static_cast<size_t>(h.n) * sizeof(TensorEntry) + 15) / 16 * 16;
+    further = opening + sizeof(Segment) * static_cast<size_t>(h.blocks) * h.warps;
+    spanning = further + sizeof(Segment) * static_cast<size_t>(h.n_further);
+    shared = spanning + sizeof(Spanning) * static_cast<size_t>(h.n_spanning);
+    scale_tensor = shared + sizeof(Shared2) * static_cast<size_t>(h.blocks);
+    adamw_tensor = scale_tensor + 4 * static_cast<size_t>(h.n_scale);
+    empty = adamw_tensor + 4 * static_cast<size_t>(h.n_adamw);
     bytes = empty + 4 * static_cast<size_t>(h.n_empty);
   }
 };
 char* image_of(void* plan) { return static_cast<char*>(plan) + sizeof(PlanHeader); }
 
-// Device work area: header, sums and edge sums of the blocks, the ticket, then the image of the plan.
+// Device work area: header, sums of the blocks, their edge sums, the factor, the tickets, the image
+// of the plan.
 struct WorkLayout {
-  size_t block_sum, edge_sum, ticket, image, bytes;
+  size_t block_sum, edge_sum, factor, tickets, image, bytes;
   explicit WorkLayout(const PlanHeader& h) {
     block_sum = sizeof(double) * ABS_STATS_HEADER;
-    edge_sum = block_sum + sizeof(double) * kNormCtas;
-    ticket = edge_sum + sizeof(double) * 2 * kNormCtas;
-    image = (ticket + 4 + 15) / 16 * 16;
+    edge_sum = block_sum + sizeof(double) * static_cast<size_t>(h.blocks);
+    factor = edge_sum + sizeof(double) * 2 * static_cast<size_t>(h.blocks);
+    tickets = factor + sizeof(float);
+    image = (tickets + 4 * (1 + static_cast<size_t>(h.n_spanning)) + 15) / 16 * 16;
     bytes = image + Image(h).bytes;
   }
 };
 
-// How the bytes of a list are shared out: `rows` rows of 512 bytes (32 lanes of 16 bytes) to each of
-// `warps` warps, at most as many as fill the device.
+// How the rows of a list are dealt out, a function of their number alone (and with it the shape of
+// every sum): up to 2 MiB to the warps of one cluster, above to the warps of all SMs.
 constexpr int64_t kRowBytes = 512;
-struct Share {
-  int64_t rows;
-  int64_t warps;
+struct Deal {
+  int blocks, warps;
+  int64_t rows;  // of each warp
 };
-Share share_of(int64_t total_rows) {
-  const int64_t most = static_cast<int64_t>(kNormCtas) * kNormWarps;
-  Share s;
-  s.rows = std::max<int64_t>(1, (total_rows + most - 1) / most);
-  s.warps = (total_rows + s.rows - 1) / s.rows;
-  return s;
+Deal deal_of(int64_t rows) {
+  Deal d;
+  const bool small = rows <= int64_t{kClusterBlocks} * kClusterWarps * kClusterRows;
+  d.warps = small ? kClusterWarps : kListWarps;
+  const int64_t most = static_cast<int64_t>(small ? kClusterBlocks : kListBlocks) * d.warps;
+  d.rows = std::max<int64_t>(1, (rows + most - 1) / most);
+  const int64_t slots = std::max<int64_t>(1, (rows + d.rows - 1) / d.rows);
+  d.blocks = static_cast<int>((slots + d.warps - 1) / d.warps);
+  return d;
 }
 // Rows of a tensor, the last one short.
 int64_t rows_of(int64_t numel, size_t esz) {
   return (numel * static_cast<int64_t>(esz) + kRowBytes - 1) / kRowBytes;
 }
-// A segment is counted in 32 bits; longer runs of one warp are cut.
-constexpr int64_t kMaxSegmentRows = int64_t{1} << 20;
 
-// Elements per unit: a power of two that gives about eight units to each of the 148 SMs, between
-// 1024 (a quarter of a vector per thread, so that small lists spread over the SMs) and 32768.  A
-// function of the element count alone, and with it the shape of every sum.
-int unit_for(int64_t total) {
-  int unit = 1024;
+// Elements per unit of scaling: a power of two that gives about eight units to each of the 148 SMs,
+// between 4096 and 32768.
+int scale_unit_for(int64_t total) {
+  int unit = 4096;
   while (unit < 32768 && total / unit > 8 * 148) unit *= 2;
   return unit;
+}
+int64_t units_of(int64_t numel, int head, int unit) {
+  return numel > head ? (numel - head + unit - 1) / unit : 1;
 }
 
 size_t element_size(int dtype) { return dtype == ABS_F32 ? 4 : 2; }
@@ -180,21 +196,23 @@ int fill_params(const void* plan, void* work, int norm_type, double scale, doubl
   prm->header = reinterpret_cast<double*>(w);
   prm->block_sum = reinterpret_cast<double*>(w + L.block_sum);
   prm->edge_sum = reinterpret_cast<double*>(w + L.edge_sum);
-  prm->ticket = reinterpret_cast<unsigned int*>(w + L.ticket);
+  prm->factor = reinterpret_cast<float*>(w + L.factor);
+  prm->tickets = reinterpret_cast<unsigned int*>(w + L.tickets);
   const Image I(*h);
   w += L.image;
   prm->entries = reinterpret_cast<const TensorEntry*>(w);
-  prm->segments = reinterpret_cast<const Segment*>(w + I.segments);
+  prm->opening = reinterpret_cast<const Segment*>(w + I.opening);
+  prm->further = reinterpret_cast<const Segment*>(w + I.further);
   prm->spanning = reinterpret_cast<const Spanning*>(w + I.spanning);
+  prm->shared = reinterpret_cast<const Shared2*>(w + I.shared);
+  prm->scale_tensor = reinterpret_cast<const int32_t*>(w + I.scale_tensor);
+  prm->adamw_tensor = reinterpret_cast<const int32_t*>(w + I.adamw_tensor);
   prm->empty = reinterpret_cast<const int32_t*>(w + I.empty);
-  prm->warp_first = reinterpret_cast<const int32_t*>(w + I.warp_first);
-  prm->unit_tensor = reinterpret_cast<const int32_t*>(w + I.unit_tensor);
   prm->norms_out = norms_out;
   prm->n = h->n;
-  prm->n_units = h->n_units;
-  prm->unit = h->unit;
-  prm->n_segments = h->n_segments;
-  prm->n_warps = h->n_warps;
+  prm->n_scale = h->n_scale;
+  prm->n_adamw = h->n_adamw;
+  prm->scale_unit = h->scale_unit;
   prm->n_spanning = h->n_spanning;
   prm->n_empty = h->n_empty;
   prm->norm_type = norm_type;
@@ -202,18 +220,99 @@ int fill_params(const void* plan, void* work, int norm_type, double scale, doubl
   prm->max_norm = max_norm;
   prm->sum_in = sum_in;
   prm->in_place = !(h->roles & kRoleOut);
+  prm->after_norm = 0;
   return ABS_OK;
 }
 
-dim3 unit_grid(const TensorsParams& prm) {
-  return dim3(static_cast<unsigned>(prm.n_units > 0 ? prm.n_units : 1));
+// Whether the current device can run a cluster kernel with all its blocks.  Asked once per device,
+// for the kernel with the largest need; sets what each kernel has to be allowed.
+template <int NORM, int OP>
+cudaError_t allow_cluster() {
+  const auto kernel = tensors_cluster_kernel<NORM, OP>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess || OP == kOpNone) return e;
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              static_cast<int>(kKeepBytes * kClusterRows));
+}
+template <int OP>
+cudaError_t allow_clusters() {
+  cudaError_t e = allow_cluster<kNorm2, OP>();
+  if (e == cudaSuccess) e = allow_cluster<kNorm1, OP>();
+  return e == cudaSuccess ? allow_cluster<kNormMax, OP>() : e;
+}
+bool cluster_runs() {
+  static std::mutex mu;
+  static std::atomic<int> cached[64] = {};  // 0: not asked, 1: no, 2: yes
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  if (const int c = cached[dev].load(std::memory_order_acquire)) return c == 2;
+  std::lock_guard<std::mutex> lock(mu);
+  int clusters = 0;
+  bool yes = allow_clusters<kOpNone>() == cudaSuccess && allow_clusters<kOpScale>() == cudaSuccess &&
+             allow_clusters<kOpAdamw>() == cudaSuccess;
+  if (yes) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kClusterBlocks);
+    cfg.blockDim = dim3(kClusterWarps * 32);
+    cfg.dynamicSmemBytes = kKeepBytes * kClusterRows;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kClusterBlocks;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    yes = cudaOccupancyMaxActiveClusters(&clusters, tensors_cluster_kernel<kNorm2, kOpAdamw>, &cfg) ==
+              cudaSuccess && clusters >= 1;
+  }
+  (void)cudaGetLastError();  // a refused query is an answer, not an error of the call
+  cached[dev].store(yes ? 2 : 1, std::memory_order_release);
+  return yes;
 }
 
-cudaError_t launch_norm(const TensorsParams& prm, cudaStream_t st) {
-  const dim3 grid(std::max(1, (prm.n_warps + kNormWarps - 1) / kNormWarps)), block(kNormThreads);
-  return prm.norm_type == ABS_NORM_2   ? launch_pdl(tensors_norm_kernel<kNorm2>, grid, block, st, prm)
-         : prm.norm_type == ABS_NORM_1 ? launch_pdl(tensors_norm_kernel<kNorm1>, grid, block, st, prm)
-                                       : launch_pdl(tensors_norm_kernel<kNormMax>, grid, block, st, prm);
+template <int OP>
+cudaError_t launch_cluster(const PlanHeader& h, const TensorsParams& prm, const GroupScalars& groups,
+                           cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h.blocks);
+  cfg.blockDim = dim3(kClusterWarps * 32);
+  cfg.dynamicSmemBytes = OP == kOpNone ? 0 : kKeepBytes * h.rows;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = h.blocks;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const int rows = h.rows;
+  return prm.norm_type == ABS_NORM_2
+             ? cudaLaunchKernelEx(&cfg, tensors_cluster_kernel<kNorm2, OP>, prm, groups, rows)
+         : prm.norm_type == ABS_NORM_1
+             ? cudaLaunchKernelEx(&cfg, tensors_cluster_kernel<kNorm1, OP>, prm, groups, rows)
+             : cudaLaunchKernelEx(&cfg, tensors_cluster_kernel<kNormMax, OP>, prm, groups, rows);
+}
+
+template <int WARPS>
+cudaError_t launch_norm_blocks(int blocks, const TensorsParams& prm, cudaStream_t st) {
+  const dim3 grid(blocks), block(WARPS * 32);
+  return prm.norm_type == ABS_NORM_2
+             ? launch_pdl(tensors_norm_kernel<kNorm2, WARPS>, grid, block, st, prm)
+         : prm.norm_type == ABS_NORM_1
+             ? launch_pdl(tensors_norm_kernel<kNorm1, WARPS>, grid, block, st, prm)
+             : launch_pdl(tensors_norm_kernel<kNormMax, WARPS>, grid, block, st, prm);
+}
+cudaError_t launch_norm(const PlanHeader& h, const TensorsParams& prm, cudaStream_t st) {
+  return h.cluster() ? launch_norm_blocks<kClusterWarps>(h.blocks, prm, st)
+                     : launch_norm_blocks<kListWarps>(h.blocks, prm, st);
+}
+
+// The factor of a call: from the list's own norm, or from the sum that it is given.
+cudaError_t launch_norm_or_clip(const PlanHeader& h, const TensorsParams& prm, cudaStream_t st) {
+  return prm.sum_in ? launch_pdl(tensors_clip_kernel, dim3(1), dim3(32), st, prm)
+                    : launch_norm(h, prm, st);
 }
 
 // Everything of abs_tensors_plan that can run out of memory or throw.
@@ -237,9 +336,14 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     total += g.numel;
     total_rows += rows_of(g.numel, g.esz);
   }
-  h.unit = unit_for(total);
+  h.total = total;
+  h.scale_unit = scale_unit_for(total);
+  const Deal deal = deal_of(total_rows);
+  h.blocks = deal.blocks;
+  h.warps = deal.warps;
+  h.rows = static_cast<int32_t>(deal.rows);
   std::vector<TensorEntry> entries(n);
-  std::vector<int32_t> unit_tensor;
+  std::vector<int32_t> scale_tensor, adamw_tensor;
   for (int t = 0; t < n; ++t) {
     View g, out, state[3], b16;
     view_of(grads[t], &g);
@@ -313,81 +417,91 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     }
     e.flags |= static_cast<uint8_t>(best);
     if (e.numel) {
-      const int64_t body = e.numel > e.head ? e.numel - e.head : 1;
-      const int64_t k = (body + h.unit - 1) / h.unit;
-      if (k > kMaxUnits - static_cast<int64_t>(unit_tensor.size())) return ABS_ERR_RANGE;
-      e.first_unit = static_cast<int32_t>(unit_tensor.size());
-      e.n_units = static_cast<int32_t>(k);
-      unit_tensor.insert(unit_tensor.end(), static_cast<size_t>(k), t);
+      e.first_scale = static_cast<int32_t>(scale_tensor.size());
+      e.first_adamw = static_cast<int32_t>(adamw_tensor.size());
+      const int64_t k = units_of(e.numel, e.head, kAdamwUnit);
+      if (k > kMaxUnits - static_cast<int64_t>(adamw_tensor.size())) return ABS_ERR_RANGE;
+      scale_tensor.insert(scale_tensor.end(),
+                          static_cast<size_t>(units_of(e.numel, e.head, h.scale_unit)), t);
+      if (params) adamw_tensor.insert(adamw_tensor.end(), static_cast<size_t>(k), t);
     }
     entries[t] = e;
   }
   if (any_conflict(all)) return ABS_ERR_ALIAS;
   if (any_conflict(grads_written)) h.roles |= kGradsOverlap;
 
-  // the segments: the rows of all tensors in order, dealt out to the warps
-  const Share share = share_of(total_rows);
-  std::vector<Segment> segments;
-  std::vector<int32_t> warp_first;
-  int64_t left = 0;  // rows that the current warp still takes
-  for (int t = 0; t < n; ++t) {
-    TensorEntry& e = entries[t];
-    const size_t esz = element_size(e.g_dtype);
-    const int64_t per_row = kRowBytes / static_cast<int64_t>(esz);
-    const int head = (e.flags & kEntryVecG) ? e.head : 0;
-    int64_t rows = rows_of(e.numel, esz), start = 0;
-    e.first_seg = static_cast<int32_t>(segments.size());
-    while (rows > 0) {
-      if (left == 0) {
-        warp_first.push_back(static_cast<int32_t>(segments.size()));
-        left = share.rows;
-      }
-      const int64_t take = std::min(std::min(rows, left), kMaxSegmentRows);
-      rows -= take;
-      left -= take;
-      // every segment but the last ends on a 16-byte boundary: `head` elements further
-      const int64_t end = rows ? start + take * per_row + (start ? 0 : head) : e.numel;
-      Segment s;
-      std::memset(&s, 0, sizeof s);
-      s.start = start;
-      s.n = static_cast<uint32_t>(std::min(end, e.numel) - start);
-      s.g = static_cast<const char*>(e.g) + (e.flags & kEntryRowsG ? 0 : start * esz);
-      s.tensor = t;
-      s.dtype = e.g_dtype;
-      s.rows = (e.flags & kEntryRowsG) ? 1 : 0;
-      s.vec = (e.flags & kEntryVecG) && !s.rows;
-      s.head = static_cast<uint8_t>(start ? 0 : std::min<int64_t>(head, s.n));
-      start += s.n;
-      segments.push_back(s);
-      if (start == e.numel) {  // the head has taken the last, short row
-        left += rows;
-        rows = 0;
-      }
-    }
-    e.n_segs = static_cast<int32_t>(segments.size()) - e.first_seg;
-  }
-  // the tensors that blocks (kNormWarps warps each) share
+  // the segments: the rows of all tensors in order, dealt out warp by warp
+  Segment idle;
+  std::memset(&idle, 0, sizeof idle);
+  idle.tensor = -1;
+  std::vector<Segment> opening(static_cast<size_t>(deal.blocks) * deal.warps, idle), further;
   std::vector<Spanning> spanning;
   std::vector<int32_t> empty;
-  const auto block_of = [&](int32_t segment) {  // the warps' first segments ascend
-    const auto it = std::upper_bound(warp_first.begin(), warp_first.end(), segment);
-    return static_cast<int32_t>((it - warp_first.begin() - 1) / kNormWarps);
-  };
+  int64_t slot = -1, left = 0;  // the warp that is dealt to, and the rows that it still takes
   for (int t = 0; t < n; ++t) {
     const TensorEntry& e = entries[t];
-    if (!e.n_segs) {
+    if (!e.numel) {
       empty.push_back(t);
       continue;
     }
-    const int32_t a = block_of(e.first_seg), b = block_of(e.first_seg + e.n_segs - 1);
-    if (a != b) spanning.push_back({t, a, b, 0});
+    const size_t esz = element_size(e.g_dtype);
+    const int64_t per_row = kRowBytes / static_cast<int64_t>(esz);
+    const int head = (e.flags & kEntryVecG) ? e.head : 0;
+    int64_t rows = rows_of(e.numel, esz), start = 0, first_block = 0;
+    while (start < e.numel) {
+      const bool opens = left == 0;
+      if (opens) {
+        ++slot;
+        left = deal.rows;
+      }
+      const int64_t take = std::min(rows, left);
+      rows -= take;
+      left -= take;
+      // every segment but the last ends on a 16-byte boundary: `head` elements further
+      int64_t end = rows ? start + take * per_row + (start ? 0 : head) : e.numel;
+      if (end >= e.numel) {  // perhaps the head has taken the last, short row
+        end = e.numel;
+        left += rows;
+        rows = 0;
+      }
+      Segment s;
+      std::memset(&s, 0, sizeof s);
+      s.g = static_cast<const char*>(e.g) + (e.flags & kEntryRowsG ? 0 : start * esz);
+      s.start = start;
+      s.n = static_cast<uint32_t>(end - start);
+      s.tensor = t;
+      s.dtype = e.g_dtype;
+      s.head = static_cast<uint8_t>(start ? 0 : std::min<int64_t>(head, s.n));
+      // vectors in one run of bytes only: a view with rows is walked
+      if (!(e.flags & kEntryRowsG)) s.flags = e.flags & (kEntryVecG | kEntryVecClip | kEntryVecAdam);
+      if (e.flags & kEntryRowsOut) s.flags &= ~kEntryVecClip;
+      s.pos = (start ? 0 : kSegBegins) | (end == e.numel ? kSegEnds : 0);
+      if (opens) {
+        s.next = static_cast<int32_t>(further.size());
+        opening[slot] = s;
+      } else {
+        ++opening[slot].more;
+        further.push_back(s);
+      }
+      const int64_t block = slot / deal.warps;
+      if (!start) first_block = block;
+      if (end == e.numel && block != first_block)
+        spanning.push_back({t, static_cast<int32_t>(first_block), static_cast<int32_t>(block), 0});
+      start = end;
+    }
   }
+  std::vector<Shared2> shared(static_cast<size_t>(deal.blocks), Shared2{-1, -1});
+  for (size_t i = 0; i < spanning.size(); ++i)
+    for (int32_t b = spanning[i].first; b <= spanning[i].last; ++b) {
+      // a tensor that fills a block whole is counted off once there, as one from before
+      if (b > spanning[i].first) shared[b].before = static_cast<int32_t>(i);
+      if (b == spanning[i].first) shared[b].after = static_cast<int32_t>(i);
+    }
   h.n_spanning = static_cast<int32_t>(spanning.size());
   h.n_empty = static_cast<int32_t>(empty.size());
-  h.n_warps = static_cast<int32_t>(warp_first.size());
-  h.n_segments = static_cast<int32_t>(segments.size());
-  h.n_units = static_cast<int32_t>(unit_tensor.size());
-  warp_first.push_back(h.n_segments);
+  h.n_further = static_cast<int32_t>(further.size());
+  h.n_scale = static_cast<int32_t>(scale_tensor.size());
+  h.n_adamw = static_cast<int32_t>(adamw_tensor.size());
 
   const Image I(h);
   if (plan_bytes < sizeof(PlanHeader) + I.bytes) return ABS_ERR_TOO_LARGE;
@@ -396,11 +510,13 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     if (bytes) std::memcpy(to, from, bytes);
   };
   put(image, entries.data(), entries.size() * sizeof(TensorEntry));
-  put(image + I.segments, segments.data(), segments.size() * sizeof(Segment));
-  put(image + I.warp_first, warp_first.data(), warp_first.size() * 4);
+  put(image + I.opening, opening.data(), opening.size() * sizeof(Segment));
+  put(image + I.further, further.data(), further.size() * sizeof(Segment));
   put(image + I.spanning, spanning.data(), spanning.size() * sizeof(Spanning));
+  put(image + I.shared, shared.data(), shared.size() * sizeof(Shared2));
+  put(image + I.scale_tensor, scale_tensor.data(), scale_tensor.size() * 4);
+  put(image + I.adamw_tensor, adamw_tensor.data(), adamw_tensor.size() * 4);
   put(image + I.empty, empty.data(), empty.size() * 4);
-  put(image + I.unit_tensor, unit_tensor.data(), unit_tensor.size() * 4);
   std::memcpy(plan, &h, sizeof h);
   return ABS_OK;
 }
@@ -411,28 +527,27 @@ extern "C" {
 
 size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n) {
   if (n < 0 || n > ABS_MAX_TENSORS || (n > 0 && !grads)) return 0;
-  int64_t total = 0, rows = 0, units = 0, segments = 0;
+  int64_t total = 0, rows = 0, scale = 0, adamw = 0;
   for (int t = 0; t < n; ++t) {
     if (grads[t].numel < 0 || grads[t].numel > kMaxElements - total) return 0;
     total += grads[t].numel;
     rows += rows_of(grads[t].numel, element_size(grads[t].dtype));
   }
-  // upper bounds: a tensor has a segment of its own and one more for each warp that begins in it
-  const int unit = unit_for(total);
-  const Share share = share_of(rows);
+  const int unit = scale_unit_for(total);
   for (int t = 0; t < n; ++t) {
-    const int64_t r = rows_of(grads[t].numel, element_size(grads[t].dtype));
-    units += (grads[t].numel + unit - 1) / unit;
-    segments += r ? 1 + r / share.rows + r / kMaxSegmentRows + 1 : 0;
+    scale += (grads[t].numel + unit - 1) / unit;
+    adamw += (grads[t].numel + kAdamwUnit - 1) / kAdamwUnit;
   }
-  if (units > kMaxUnits || segments > kMaxUnits) return 0;
-  PlanHeader h;
+  if (adamw > kMaxUnits) return 0;
+  const Deal deal = deal_of(rows);
+  PlanHeader h;  // upper bounds
   std::memset(&h, 0, sizeof h);
-  h.n = h.n_empty = n;
-  h.n_units = static_cast<int32_t>(units);
-  h.n_segments = static_cast<int32_t>(segments);
-  h.n_warps = static_cast<int32_t>(share.warps);
-  h.n_spanning = std::min(n, kNormCtas);
+  h.n = h.n_empty = h.n_further = n;
+  h.n_scale = static_cast<int32_t>(scale);
+  h.n_adamw = static_cast<int32_t>(adamw);
+  h.blocks = deal.blocks;
+  h.warps = deal.warps;
+  h.n_spanning = std::min(n, deal.blocks);
   return sizeof h + Image(h).bytes;
 }
 
@@ -478,7 +593,11 @@ int abs_grad_norm(const void* plan, void* work, int norm_type, double grad_scale
   const int rc = fill_params(plan, work, norm_type, grad_scale, max_norm, nullptr, norms_out, &prm);
   if (rc != ABS_OK) return rc;
   if (!norms_out) return ABS_ERR_NULL;
-  const cudaError_t e = launch_norm(prm, static_cast<cudaStream_t>(stream));
+  const PlanHeader& h = *plan_of(plan);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = h.cluster() && cluster_runs()
+                            ? launch_cluster<kOpNone>(h, prm, GroupScalars{}, st)
+                            : launch_norm(h, prm, st);
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
 
@@ -489,11 +608,18 @@ int abs_grad_clip(const void* plan, void* work, int norm_type, double grad_scale
   if (rc != ABS_OK) return rc;
   if (!norms_out) return ABS_ERR_NULL;
   if (!(max_norm > 0.0)) return ABS_ERR_RANGE;
-  if (prm.in_place && (plan_of(plan)->roles & kGradsOverlap)) return ABS_ERR_ALIAS;
+  const PlanHeader& h = *plan_of(plan);
+  if (prm.in_place && (h.roles & kGradsOverlap)) return ABS_ERR_ALIAS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = sum_in ? cudaSuccess : launch_norm(prm, st);
-  if (e == cudaSuccess && (prm.n_units > 0 || sum_in))
-    e = launch_pdl(tensors_scale_kernel, unit_grid(prm), dim3(kTensorThreads), st, prm);
+  cudaError_t e;
+  if (!sum_in && h.cluster() && cluster_runs()) {
+    e = launch_cluster<kOpScale>(h, prm, GroupScalars{}, st);
+  } else {
+    e = launch_norm_or_clip(h, prm, st);
+    prm.after_norm = !sum_in;
+    if (e == cudaSuccess && prm.n_scale > 0)
+      e = launch_pdl(tensors_scale_kernel, dim3(prm.n_scale), dim3(kTensorThreads), st, prm);
+  }
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
 
@@ -516,10 +642,16 @@ int abs_grad_adamw(const void* plan, void* work, const abs_adamw_hparams* hparam
     groups.a[i] = make_adam(hparams + i, step);
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = clipped && !sum_in ? launch_norm(prm, st) : cudaSuccess;
-  if (e == cudaSuccess && (prm.n_units > 0 || (clipped && sum_in)))
-    e = launch_pdl(tensors_adamw_kernel, unit_grid(prm), dim3(kTensorThreads), st, prm, groups,
-                   clipped ? 1 : 0);
+  cudaError_t e;
+  if (clipped && !sum_in && h->cluster() && h->total <= kClusterAdamw && cluster_runs()) {
+    e = launch_cluster<kOpAdamw>(*h, prm, groups, st);
+  } else {
+    e = clipped ? launch_norm_or_clip(*h, prm, st) : cudaSuccess;
+    prm.after_norm = clipped && !sum_in;
+    if (e == cudaSuccess && prm.n_adamw > 0)
+      e = launch_pdl(tensors_adamw_kernel, dim3(prm.n_adamw), dim3(kTensorThreads), st, prm, groups,
+                     clipped ? 1 : 0);
+  }
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
 
