@@ -35,16 +35,19 @@ struct TensorEntry {
   uint32_t g_row, out_row;
   int32_t first_scale, first_adamw;  // its first unit for scaling and for AdamW
   uint8_t g_dtype, out_dtype;
-  uint8_t head;   // elements before the first one that lies on a vector boundary in every array
+  // elements before the first one on a boundary of 16 bytes of the gradient, of 8 elements of what
+  // scaling writes, of 8 elements of the parameters; 0 for a view with rows
+  uint8_t g_head, scale_head, adamw_head;
   uint8_t flags;  // kEntry* bits
   uint16_t group;
 };
 enum {
-  kEntryRowsG = 1,     // the gradient has rows (else it is one run of elements)
-  kEntryRowsOut = 2,   // so has the clipped output
-  kEntryVecG = 4,      // from `head` on, 16-byte loads of the gradient are aligned
-  kEntryVecClip = 8,   // from `head` on, 8 elements of gradient and output are
-  kEntryVecAdam = 16,  // from `head` on, 8 elements of gradient, state and bf16 copy are
+  kEntryRowsG = 1,      // the gradient has rows (else it is one run of elements)
+  kEntryRowsOut = 2,    // so has the clipped output
+  kEntryFar = 4,        // a unit of the gradient's view spans 2^31 elements or more
+  kEntryStateVec = 8,   // state and bf16 copy reach a boundary together, after adamw_head
+  kEntryVecScale = 16,  // 16 bytes of the gradient (after g_head) meet an aligned place in the output
+  kEntryVecAdamw = 32,  // and in state and bf16 copy
 };
 
 // A run of elements of one tensor, the work of one warp: [start, start + n), `head` of them before
@@ -55,7 +58,7 @@ struct alignas(16) Segment {
   int64_t start;
   uint32_t n;
   int32_t tensor;               // -1: no work
-  uint8_t dtype, head, flags, pos;  // flags: the kEntryVec* bits that hold; pos: kSeg* bits
+  uint8_t dtype, head, flags, pos;  // flags: the entry's; pos: kSeg* bits
   int32_t more, next, pad;
 };
 enum { kSegBegins = 1, kSegEnds = 2 };  // the first / last segment of its tensor
@@ -153,49 +156,57 @@ __device__ __forceinline__ void with_type(int dtype, F&& f) {
     f(TF16{});
 }
 
-// Walks the elements start + i0, start + i0 + step, ... of a view: `offset()` of the current one,
-// `next()` to the one `step` further.  One division at the beginning, none on the way.
+// Walks the elements first, first + step, ... of a view: `at` is the offset of the current one from
+// `base`, next() goes `step` further.  One division at the beginning, none on the way; in 32 bits
+// (I) where what is walked spans less than 2^31 elements.
+template <typename I>
 struct Walk {
-  int64_t off, step_off, wrap_off;
+  int64_t base;
+  I at, step_at, wrap_at;
   uint32_t col, step_col, row;
-  __device__ __forceinline__ int64_t offset() const { return off; }
   __device__ __forceinline__ void next() {
-    off += step_off;
+    at += step_at;
     col += step_col;
     if (col >= row) {
       col -= row;
-      off += wrap_off;
+      at += wrap_at;
     }
   }
 };
-__device__ __forceinline__ Walk make_walk(int64_t first, uint32_t step, bool rows, uint32_t row,
-                                          int64_t stride, int64_t col_stride) {
-  if (!rows) return Walk{first, step, 0, 0, 0, 1};
+template <typename I>
+__device__ __forceinline__ Walk<I> make_walk(int64_t first, uint32_t step, bool rows, uint32_t row,
+                                             int64_t stride, int64_t col_stride) {
+  if (!rows) return Walk<I>{first, 0, static_cast<I>(step), 0, 0, 0, 1};
   const int64_t r = first / row;
   const uint32_t c = static_cast<uint32_t>(first - r * row);
   const uint32_t dr = step / row, dc = step - dr * row;
-  return Walk{r * stride + c * col_stride, dr * stride + dc * col_stride,
-              stride - static_cast<int64_t>(row) * col_stride, c, dc, row};
+  return Walk<I>{r * stride + c * col_stride,
+                 0,
+                 static_cast<I>(dr * stride + dc * col_stride),
+                 static_cast<I>(stride - static_cast<int64_t>(row) * col_stride),
+                 c,
+                 dc,
+                 row};
 }
-__device__ __forceinline__ Walk grad_walk(const TensorEntry& e, int64_t first, uint32_t step) {
-  return make_walk(first, step, e.flags & kEntryRowsG, e.g_row, e.g_stride, e.g_col);
+template <typename I>
+__device__ __forceinline__ Walk<I> grad_walk(const TensorEntry& e, int64_t first, uint32_t step) {
+  return make_walk<I>(first, step, e.flags & kEntryRowsG, e.g_row, e.g_stride, e.g_col);
 }
-__device__ __forceinline__ Walk out_walk(const TensorEntry& e, int64_t first, uint32_t step) {
-  return make_walk(first, step, e.flags & kEntryRowsOut, e.out_row, e.out_stride, e.out_col);
+__device__ __forceinline__ Walk<int64_t> out_walk(const TensorEntry& e, int64_t first, uint32_t step) {
+  return make_walk<int64_t>(first, step, e.flags & kEntryRowsOut, e.out_row, e.out_stride, e.out_col);
 }
 
 // The elements [start, start + n) of unit k of a tensor; unit 0 also holds the head.
 struct UnitRange {
   int64_t start;
-  uint32_t n, head;
+  uint32_t n;
 };
-__device__ __forceinline__ UnitRange unit_range(const TensorEntry& e, int k, int unit) {
+__device__ __forceinline__ UnitRange unit_range(const TensorEntry& e, int k, int unit, int head) {
   UnitRange r;
-  r.start = k ? e.head + static_cast<int64_t>(k) * unit : 0;
-  int64_t end = e.head + static_cast<int64_t>(k + 1) * unit;
+  r.start = k ? head + static_cast<int64_t>(k) * unit : 0;
+  int64_t end = head + static_cast<int64_t>(k + 1) * unit;
   if (end > e.numel) end = e.numel;
   r.n = static_cast<uint32_t>(end - r.start);
-  r.head = k ? 0u : (e.head < r.n ? e.head : r.n);
   return r;
 }
 
@@ -268,7 +279,13 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
     acc.bits |= __float_as_uint(x);
     acc.template add<1>(&x);
   };
-  if (s.flags & kEntryVecG) {
+  auto vec = [&](const uint4& raw) {
+    float x[T::kVec];
+    T::unpack(raw, x);
+    acc.bits |= raw.x | raw.y | raw.z | raw.w;
+    acc.template add<T::kVec>(x);
+  };
+  if (!(s.flags & kEntryRowsG)) {
     const S* g = static_cast<const S*>(s.g);
     if (lane < s.head) one(g[lane]);
     const uint32_t nv = (s.n - s.head) / T::kVec;
@@ -282,38 +299,45 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
       }
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        float x[T::kVec];
-        T::unpack(raw[j], x);
-        acc.bits |= raw[j].x | raw[j].y | raw[j].z | raw[j].w;
-        acc.template add<T::kVec>(x);
+        vec(raw[j]);
         if (KEEP && v0 + j * 32 < nv) keep[v0 - lane + j * 32] = raw[j];
       }
     }
     const uint32_t i = s.head + nv * T::kVec + lane;
     if (i < s.n) one(g[i]);
   } else {
-    constexpr int kWalk = 16;
+    // a view with rows; a segment of it is a few hundred kilobytes at most unless it is far apart
     const TensorEntry& e = prm.entries[s.tensor];
     const S* g = static_cast<const S*>(e.g);
-    Walk w = grad_walk(e, s.start + lane, 32);
-    for (uint32_t i0 = lane; i0 < s.n; i0 += kWalk * 32) {
-      S raw[kWalk];
+    const auto walk = [&](auto index) {
+      constexpr int kWalk = 16;
+      Walk<decltype(index)> w = grad_walk<decltype(index)>(e, s.start + lane, 32);
+      g += w.base;
+      uint32_t i0 = lane;
+      for (; i0 + (kWalk - 1) * 32 < s.n; i0 += kWalk * 32) {
+        S raw[kWalk];
 #pragma unroll
-      for (int j = 0; j < kWalk; ++j) {
-        raw[j] = i0 + j * 32 < s.n ? g[w.offset()] : S(0);
-        w.next();
-      }
-#pragma unroll
-      for (int j = 0; j < kWalk; j += 8) {
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          x[k] = T::to_float(raw[j + k]);
-          acc.bits |= __float_as_uint(x[k]);
+        for (int j = 0; j < kWalk; ++j) {
+          raw[j] = g[w.at];
+          w.next();
         }
-        acc.template add<8>(x);
+#pragma unroll
+        for (int j = 0; j < kWalk; j += 8) {
+          float x[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            x[k] = T::to_float(raw[j + k]);
+            acc.bits |= __float_as_uint(x[k]);
+          }
+          acc.template add<8>(x);
+        }
       }
-    }
+      for (; i0 < s.n; i0 += 32, w.next()) one(g[w.at]);
+    };
+    if (e.flags & kEntryFar)
+      walk(int64_t{});
+    else
+      walk(int32_t{});
   }
   return acc;
 }
@@ -324,11 +348,11 @@ __device__ __forceinline__ double segment_acc_wide(const TensorsParams& prm, con
                                                    uint32_t lane) {
   const TensorEntry& e = prm.entries[s.tensor];
   const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
-  Walk w = grad_walk(e, s.start + lane, 32);
+  Walk<int64_t> w = grad_walk<int64_t>(e, s.start + lane, 32);
   double sum = 0.0;
 #pragma unroll 1
   for (uint32_t i = lane; i < s.n; i += 32, w.next()) {
-    const double x = T::to_float(g[w.offset()]);
+    const double x = T::to_float(g[w.base + w.at]);
     sum += NORM == kNorm2 ? x * x : fabs(x);
   }
   return sum;
@@ -412,7 +436,7 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
       Segment next = s;
       if (k < opening.more) next = prm.further[opening.next + k];
       const double y = segment_sum<NORM, KEEP>(prm, s, lane, keep);
-      if (KEEP && (s.flags & kEntryVecG))
+      if (KEEP && !(s.flags & kEntryRowsG))
         keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
       sum = norm_join<NORM>(sum, y);
       x = norm_join<NORM>(x, y);
@@ -592,29 +616,28 @@ __device__ __forceinline__ void store_scaled(const uint4& raw, int in, void* p, 
       __stcs(reinterpret_cast<uint4*>(y), make_uint4(w[0], w[1], w[2], w[3]));
   }
 }
-// n elements from `first` on, every step-th of them by this thread.
+// n elements from `first` on, every step-th of them by this thread, from and to any view.
 __device__ __forceinline__ void scale_walk(const TensorEntry& e, int64_t first, uint32_t i0,
                                            uint32_t n, uint32_t step, float factor, bool in_place) {
   constexpr int kBatch = 8;
-  Walk wi = grad_walk(e, first + i0, step);
-  Walk wo = in_place ? wi : out_walk(e, first + i0, step);
+  Walk<int64_t> wi = grad_walk<int64_t>(e, first + i0, step);
+  Walk<int64_t> wo = in_place ? wi : out_walk(e, first + i0, step);
   void* y = in_place ? const_cast<void*>(e.g) : e.out;
   const int in = e.g_dtype, out = in_place ? e.g_dtype : e.out_dtype;
   for (; i0 < n; i0 += kBatch * step) {
     float x[kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (i0 + j * step < n) x[j] = load_any(e.g, wi.offset(), in);
+      if (i0 + j * step < n) x[j] = load_any(e.g, wi.base + wi.at, in);
       wi.next();
     }
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (i0 + j * step < n) store_any(y, wo.offset(), out, factor * x[j]);
+      if (i0 + j * step < n) store_any(y, wo.base + wo.at, out, factor * x[j]);
       wo.next();
     }
   }
 }
-
 
 // Eight consecutive values, 16- or 32-byte aligned.
 template <typename T>
@@ -647,63 +670,161 @@ __device__ __forceinline__ void store8(typename T::scalar* p, const float* x) {
   }
 }
 
+// Eight consecutive values that begin `o` bytes after a 16-byte boundary (o > 0): the 16-byte pieces
+// that hold them, and the values out of those.
+template <typename T>
+struct Shifted8 {
+  uint4 r[8 / T::kVec + 1];
+};
+template <typename T>
+__device__ __forceinline__ Shifted8<T> load_shifted8(const typename T::scalar* p, uint32_t o) {
+  const uint4* c = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) - o);
+  Shifted8<T> x;
+#pragma unroll
+  for (int i = 0; i < 8 / T::kVec + 1; ++i) x.r[i] = c[i];  // a neighbour reads them too: L1
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ void unpack_shifted8(const Shifted8<T>& v, uint32_t o, float* x) {
+  constexpr int kWords = 4 * (8 / T::kVec) + 4;
+  uint32_t w[kWords];
+#pragma unroll
+  for (int i = 0; i < 8 / T::kVec + 1; ++i)
+    w[4 * i] = v.r[i].x, w[4 * i + 1] = v.r[i].y, w[4 * i + 2] = v.r[i].z, w[4 * i + 3] = v.r[i].w;
+  if (o & 8) {
+#pragma unroll
+    for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
+  }
+  if (o & 4) {
+#pragma unroll
+    for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
+  }
+  if (T::kVec == 8 && (o & 2)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  }
+  Vec8<T> y;
+#pragma unroll
+  for (int i = 0; i < 8 / T::kVec; ++i)
+    y.r[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  unpack8<T>(y, x);
+}
+
+// A run of n elements at g whose vectors of 8 begin at `head`: how far those lie behind a 16-byte
+// boundary, with the head and the number of vectors such that no piece reaches out of [lo, hi).
+struct Run {
+  uint32_t head, nv, o;
+};
+template <typename S>
+__device__ __forceinline__ Run make_run(const S* g, uint32_t n, uint32_t head, const S* lo,
+                                        const S* hi) {
+  Run r{head, 0, static_cast<uint32_t>(reinterpret_cast<uintptr_t>(g + head)) & 15u};
+  if (r.o && reinterpret_cast<const char*>(g + head) - r.o < reinterpret_cast<const char*>(lo))
+    r.head = min(head + 8, n);
+  r.nv = (n - r.head) / 8;
+  if (r.o && r.nv &&
+      reinterpret_cast<const char*>(g + r.head + 8 * r.nv) + (16 - r.o) >
+          reinterpret_cast<const char*>(hi))
+    --r.nv;
+  return r;
+}
+
 template <typename TI, typename TO>
 __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange& r, float factor,
                                            void* out, bool in_place) {
-  const typename TI::scalar* g = static_cast<const typename TI::scalar*>(e.g);
-  typename TO::scalar* y = static_cast<typename TO::scalar*>(out);
+  using SI = typename TI::scalar;
+  using SO = typename TO::scalar;
+  const SI* g = static_cast<const SI*>(e.g);
+  SO* y = static_cast<SO*>(out);
   const uint32_t tid = threadIdx.x;
-  if (e.flags & kEntryVecClip) {
-    // rows are whole vectors here, and there is no head then: the walk goes by vectors
-    constexpr int kBatch = 4;
-    const uint32_t nv = (r.n - r.head) / 8;
-    const int64_t first = r.start + r.head + tid * 8;
-    Walk wi = grad_walk(e, first, 8 * kTensorThreads);
-    Walk wo = in_place ? wi : out_walk(e, first, 8 * kTensorThreads);
-    for (uint32_t v0 = tid; v0 < nv; v0 += kBatch * kTensorThreads) {
-      Vec8<TI> raw[kBatch];
+  if (!(e.flags & (in_place ? kEntryRowsG : kEntryRowsG | kEntryRowsOut))) {
+    const SI *lo = g, *hi = g + e.numel;
+    g += r.start;
+    y += r.start;
+    const Run run = make_run(g, r.n, r.start ? 0u : min(uint32_t{e.scale_head}, r.n), lo, hi);
+    const auto one = [&](uint32_t k) { y[k] = TO::from_float(factor * TI::to_float(g[k])); };
+    const auto store = [&](uint32_t v, float* x) {
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (v0 + j * kTensorThreads < nv) raw[j] = load8<TI>(g + wi.offset());
-        wi.next();
-      }
-#pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (v0 + j * kTensorThreads < nv) {
-          float x[8];
-          unpack8<TI>(raw[j], x);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= factor;
-          store8<TO>(y + wo.offset(), x);
-        }
-        wo.next();
-      }
-    }
-    // head and rest of a tensor without rows: the elements of a view with rows are whole vectors
-    const auto one = [&](uint32_t i) {
-      y[r.start + i] = TO::from_float(factor * TI::to_float(g[r.start + i]));
+      for (int k = 0; k < 8; ++k) x[k] *= factor;
+      store8<TO>(y + run.head + v * 8, x);
     };
-    if (tid < r.head) one(tid);
-    const uint32_t rest = r.head + nv * 8 + tid;
-    if (rest < r.n) one(rest);
-  } else {
-    constexpr int kBatch = 16;
-    Walk wi = grad_walk(e, r.start + tid, kTensorThreads);
-    Walk wo = in_place ? wi : out_walk(e, r.start + tid, kTensorThreads);
-    for (uint32_t i0 = tid; i0 < r.n; i0 += kBatch * kTensorThreads) {
-      typename TI::scalar x[kBatch];
+    if (run.o == 0) {
+      constexpr int kBatch = 4;
+      for (uint32_t v0 = tid; v0 < run.nv; v0 += kBatch * kTensorThreads) {
+        Vec8<TI> raw[kBatch];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (i0 + j * kTensorThreads < r.n) x[j] = g[wi.offset()];
-        wi.next();
+        for (int j = 0; j < kBatch; ++j)
+          if (v0 + j * kTensorThreads < run.nv)
+            raw[j] = load8<TI>(g + run.head + (v0 + j * kTensorThreads) * 8);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (v0 + j * kTensorThreads < run.nv) {
+            float x[8];
+            unpack8<TI>(raw[j], x);
+            store(v0 + j * kTensorThreads, x);
+          }
       }
+    } else {
+      constexpr int kBatch = 2;
+      for (uint32_t v0 = tid; v0 < run.nv; v0 += kBatch * kTensorThreads) {
+        Shifted8<TI> raw[kBatch];
 #pragma unroll
-      for (int j = 0; j < kBatch; ++j) {
-        if (i0 + j * kTensorThreads < r.n)
-          y[wo.offset()] = TO::from_float(factor * TI::to_float(x[j]));
-        wo.next();
+        for (int j = 0; j < kBatch; ++j)
+          if (v0 + j * kTensorThreads < run.nv)
+            raw[j] = load_shifted8<TI>(g + run.head + (v0 + j * kTensorThreads) * 8, run.o);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (v0 + j * kTensorThreads < run.nv) {
+            float x[8];
+            unpack_shifted8<TI>(raw[j], run.o, x);
+            store(v0 + j * kTensorThreads, x);
+          }
       }
     }
+    // head and rest, at most 15 elements each
+    const uint32_t rest = run.head + run.nv * 8 + tid;
+    if (tid < run.head) one(tid);
+    if (rest < r.n) one(rest);
+  } else if (!(e.flags & kEntryFar) && (in_place || !(e.flags & kEntryRowsOut))) {
+    // rows into one run, or in place: one walk, and whole batches without a bound
+    constexpr int kBatch = 16;
+    Walk<int32_t> w = grad_walk<int32_t>(e, r.start + tid, kTensorThreads);
+    g += w.base;
+    y += in_place ? w.base : r.start + tid;
+    uint32_t i0 = tid;
+    for (; i0 + (kBatch - 1) * kTensorThreads < r.n; i0 += kBatch * kTensorThreads) {
+      SI x[kBatch];
+      Walk<int32_t> again = w;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        x[j] = g[w.at];
+        w.next();
+      }
+      if (in_place) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          y[again.at] = TO::from_float(factor * TI::to_float(x[j]));
+          again.next();
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          y[j * kTensorThreads] = TO::from_float(factor * TI::to_float(x[j]));
+        y += kBatch * kTensorThreads;
+      }
+    }
+    for (; i0 < r.n; i0 += kTensorThreads) {
+      const SO x = TO::from_float(factor * TI::to_float(g[w.at]));
+      if (in_place) {
+        y[w.at] = x;
+      } else {
+        *y = x;
+        y += kTensorThreads;
+      }
+      w.next();
+    }
+  } else {
+    scale_walk(e, r.start, tid, r.n, kTensorThreads, factor, in_place);
   }
 }
 
@@ -712,7 +833,7 @@ __global__ void __launch_bounds__(kTensorThreads, 3)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
   const int u = prm.n_scale - 1 - blockIdx.x;
   const TensorEntry& e = prm.entries[prm.scale_tensor[u]];
-  const UnitRange r = unit_range(e, u - e.first_scale, prm.scale_unit);
+  const UnitRange r = unit_range(e, u - e.first_scale, prm.scale_unit, e.scale_head);
   grid_dependency_wait();
   float factor = __ldcg(prm.factor);
   if (factor != factor) factor = static_cast<float>(prm.scale);  // not finite: not clipped
@@ -762,14 +883,15 @@ __device__ __forceinline__ void adamw_walk(const AdamScalars& a, const StateArra
                                            uint32_t n, uint32_t step, float factor) {
   constexpr int kBatch = 4;
   const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
-  Walk wg = grad_walk(e, first + i0, step);
+  Walk<int64_t> wg = grad_walk<int64_t>(e, first + i0, step);
+  g += wg.base;
   for (; i0 < n; i0 += kBatch * step) {
     typename T::scalar x[kBatch];
     float w[kBatch], m[kBatch], v[kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int64_t i = first + i0 + j * step;
-      if (i0 + j * step < n) x[j] = g[wg.offset()], w[j] = s.p[i], m[j] = s.m[i], v[j] = s.v[i];
+      if (i0 + j * step < n) x[j] = g[wg.at], w[j] = s.p[i], m[j] = s.m[i], v[j] = s.v[i];
       wg.next();
     }
 #pragma unroll
@@ -794,38 +916,31 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
   if (!after_norm) grid_dependency_wait();
   const int u = prm.n_adamw - 1 - blockIdx.x;
   const TensorEntry& e = prm.entries[prm.adamw_tensor[u]];
-  const UnitRange r = unit_range(e, u - e.first_adamw, kAdamwUnit);
+  const UnitRange r = unit_range(e, u - e.first_adamw, kAdamwUnit, e.adamw_head);
   const AdamScalars& a = groups.a[e.group];
   const StateArrays state{e.p, e.m, e.v, e.p16};
   const uint32_t tid = threadIdx.x;
   float factor = static_cast<float>(prm.scale);
   with_type(e.g_dtype, [&](auto type) {
     using T = decltype(type);
-    const typename T::scalar* g = static_cast<const typename T::scalar*>(e.g);
-    if (!(e.flags & kEntryVecAdam)) {
-      if (after_norm) grid_dependency_wait();
-      if (clipped) factor = __ldcg(prm.factor);
-      if (factor != factor) return;  // no update from a gradient that is not finite
-      adamw_walk<T>(a, state, e, r.start, tid, r.n, kTensorThreads, factor);
-      return;
-    }
-    const uint32_t nv = (r.n - r.head) / 8;
-    const int64_t first = r.start + r.head;
-    float *p = e.p + first, *m = e.m + first, *v = e.v + first;
-    Walk wg = grad_walk(e, first + tid * 8, 8 * kTensorThreads);
+    using S = typename T::scalar;
     bool have = false;
-    for (uint32_t q = tid; q < nv; q += kTensorThreads, wg.next()) {
-      const uint32_t i = q * 8;
-      const Vec8<T> raw = load8<T>(g + wg.offset());
-      Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
+    const auto skip = [&]() {  // gets the factor; true: no update, the gradient is not finite
       if (!have) {
         if (after_norm) grid_dependency_wait();
         if (clipped) factor = __ldcg(prm.factor);
-        if (factor != factor) return;
         have = true;
       }
-      float x[8];
-      unpack8<T>(raw, x);
+      return factor != factor;
+    };
+    if ((e.flags & kEntryRowsG) || !(e.flags & kEntryStateVec)) {
+      if (!skip()) adamw_walk<T>(a, state, e, r.start, tid, r.n, kTensorThreads, factor);
+      return;
+    }
+    const S *lo = static_cast<const S*>(e.g), *hi = lo + e.numel, *g = lo + r.start;
+    float *p = e.p + r.start, *m = e.m + r.start, *v = e.v + r.start;
+    const Run run = make_run(g, r.n, r.start ? 0u : min(uint32_t{e.adamw_head}, r.n), lo, hi);
+    const auto update = [&](uint32_t i, const float* x, Float8& w, Float8& mm, Float8& vv) {
       const float2 g0 = make_float2(factor * x[0], factor * x[1]);
       const float2 g1 = make_float2(factor * x[2], factor * x[3]);
       const float2 g2 = make_float2(factor * x[4], factor * x[5]);
@@ -835,18 +950,35 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
       st_stream_32(p + i, w.lo, w.hi);
       st_stream_32(m + i, mm.lo, mm.hi);
       st_stream_32(v + i, vv.lo, vv.hi);
-      if (e.p16) st_bf16x8(e.p16 + first + i, w.lo, w.hi);
-    }
-    // head and rest of a tensor whose gradient has no rows
-    const uint32_t rest = r.head + nv * 8 + tid;
-    if (tid < r.head || rest < r.n) {
-      if (!have) {
-        if (after_norm) grid_dependency_wait();
-        if (clipped) factor = __ldcg(prm.factor);
-        if (factor != factor) return;
+      if (e.p16) st_bf16x8(e.p16 + r.start + i, w.lo, w.hi);
+    };
+    if (run.o == 0) {
+      for (uint32_t q = tid; q < run.nv; q += kTensorThreads) {
+        const uint32_t i = run.head + q * 8;
+        const Vec8<T> raw = load8<T>(g + i);
+        Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
+        if (skip()) return;
+        float x[8];
+        unpack8<T>(raw, x);
+        update(i, x, w, mm, vv);
       }
-      if (tid < r.head) adamw_one(a, state, r.start + tid, factor * T::to_float(g[r.start + tid]));
-      if (rest < r.n) adamw_one(a, state, r.start + rest, factor * T::to_float(g[r.start + rest]));
+    } else {
+      for (uint32_t q = tid; q < run.nv; q += kTensorThreads) {
+        const uint32_t i = run.head + q * 8;
+        const Shifted8<T> raw = load_shifted8<T>(g + i, run.o);
+        Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
+        if (skip()) return;
+        float x[8];
+        unpack_shifted8<T>(raw, run.o, x);
+        update(i, x, w, mm, vv);
+      }
+    }
+    // head and rest, at most 15 elements each
+    const uint32_t rest = run.head + run.nv * 8 + tid;
+    if (tid < run.head || rest < r.n) {
+      if (skip()) return;
+      if (tid < run.head) adamw_one(a, state, r.start + tid, factor * T::to_float(g[tid]));
+      if (rest < r.n) adamw_one(a, state, r.start + rest, factor * T::to_float(g[rest]));
     }
   });
 }
@@ -884,7 +1016,7 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
   if constexpr (OP == kOpScale) {
     const int out = prm.in_place ? in : e.out_dtype;
     void* y = prm.in_place ? const_cast<void*>(e.g) : e.out;
-    if (!(s.flags & kEntryVecClip)) {
+    if (!(s.flags & kEntryVecScale)) {
       scale_walk(e, s.start, lane, s.n, 32, factor, prm.in_place);
       return;
     }
@@ -899,7 +1031,7 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
   } else {
     const AdamScalars& a = groups.a[e.group];
     const StateArrays state{e.p, e.m, e.v, e.p16};
-    if (!(s.flags & kEntryVecAdam)) {
+    if (!(s.flags & kEntryVecAdamw)) {
       with_type(in, [&](auto type) {
         adamw_walk<decltype(type)>(a, state, e, s.start, lane, s.n, 32, factor);
       });
@@ -981,7 +1113,7 @@ __global__ void __launch_bounds__(kClusterWarps * 32)
       Segment s = opening;
       for (int k = 0;; ++k) {
         segment_apply<OP>(prm, groups, s, lane, clip.factor, keep);
-        if (s.flags & kEntryVecG)
+        if (!(s.flags & kEntryRowsG))
           keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
         if (k == opening.more) break;
         s = prm.further[opening.next + k];

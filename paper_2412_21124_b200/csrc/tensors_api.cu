@@ -138,10 +138,19 @@ int view_of(const abs_tensor& t, View* v) {
   return ABS_OK;
 }
 
-// Whether elements [head, ...) of a view can be taken in groups of `vec`, each aligned.
-bool vector_ok(const View& v, int head, int vec) {
-  if (v.rows() && (head || v.col != 1 || v.row % vec || v.stride % vec)) return false;
-  return (reinterpret_cast<uintptr_t>(v.data) + head * v.esz) % (vec * v.esz) == 0;
+// Elements of a contiguous view before the first one on a boundary of `bytes` bytes.
+int head_of(const View& v, size_t bytes) {
+  const size_t a = reinterpret_cast<uintptr_t>(v.data) % bytes;
+  return v.rows() || !a ? 0 : static_cast<int>((bytes - a) / v.esz);
+}
+// Whether element `i` of a contiguous view lies on a boundary of `bytes` bytes.
+bool aligned_at(const View& v, int i, size_t bytes) {
+  return !v.rows() && (reinterpret_cast<uintptr_t>(v.data) + i * v.esz) % bytes == 0;
+}
+// Whether offsets within a run of `most` elements of a view may need more than 31 bits.
+bool spans_far(const View& v, int64_t most) {
+  const int64_t rows = std::min(v.numel / v.row, most / v.row + 2);
+  return rows > (int64_t{1} << 30) / v.stride || v.row > (int64_t{1} << 30) / v.col;
 }
 
 // Two views share an element.  Rows of the same stride that interleave do not.
@@ -400,29 +409,35 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
       all.push_back({g, false});
       grads_written.push_back({g, true});
     }
-    // the head that aligns most: the update's arrays before the output before the gradient alone
-    int best = -1;
-    for (int head = 0; head < 8; ++head) {
-      int flags = 0;
-      if (vector_ok(g, head, static_cast<int>(16 / g.esz))) flags |= kEntryVecG;
-      const bool g8 = vector_ok(g, head, 8);
-      if (g8 && (!outs || vector_ok(out, head, 8))) flags |= kEntryVecClip;
-      if (params && g8 && vector_ok(state[0], head, 8) && vector_ok(state[1], head, 8) &&
-          vector_ok(state[2], head, 8) && (!params_bf16 || vector_ok(b16, head, 8)))
-        flags |= kEntryVecAdam;
-      if (flags > best) {
-        best = flags;
-        e.head = static_cast<uint8_t>(flags ? head : 0);
+    const size_t per = 16 / g.esz;  // values in 16 bytes of the gradient
+    e.g_head = static_cast<uint8_t>(head_of(g, 16));
+    const int64_t longest = std::max<int64_t>(h.scale_unit, deal.rows * (kRowBytes / 2));
+    if (rows_g && spans_far(g, longest)) e.flags |= kEntryFar;
+    const View& y = outs ? out : g;
+    e.scale_head = static_cast<uint8_t>(head_of(y, 8 * y.esz));
+    if (!rows_g && aligned_at(y, e.g_head, std::min<size_t>(16, per * y.esz)))
+      e.flags |= kEntryVecScale;
+    if (params) {
+      e.adamw_head = static_cast<uint8_t>(head_of(state[0], 32));
+      bool together = true, vec = !rows_g;
+      for (int i = 0; i < 3; ++i) {
+        together = together && aligned_at(state[i], e.adamw_head, 32);
+        vec = vec && aligned_at(state[i], e.g_head, 16);
       }
+      if (params_bf16) {
+        together = together && aligned_at(b16, e.adamw_head, 16);
+        vec = vec && aligned_at(b16, e.g_head, 8);
+      }
+      if (together) e.flags |= kEntryStateVec;
+      if (vec) e.flags |= kEntryVecAdamw;
     }
-    e.flags |= static_cast<uint8_t>(best);
     if (e.numel) {
       e.first_scale = static_cast<int32_t>(scale_tensor.size());
       e.first_adamw = static_cast<int32_t>(adamw_tensor.size());
-      const int64_t k = units_of(e.numel, e.head, kAdamwUnit);
+      const int64_t k = units_of(e.numel, e.adamw_head, kAdamwUnit);
       if (k > kMaxUnits - static_cast<int64_t>(adamw_tensor.size())) return ABS_ERR_RANGE;
       scale_tensor.insert(scale_tensor.end(),
-                          static_cast<size_t>(units_of(e.numel, e.head, h.scale_unit)), t);
+                          static_cast<size_t>(units_of(e.numel, e.scale_head, h.scale_unit)), t);
       if (params) adamw_tensor.insert(adamw_tensor.end(), static_cast<size_t>(k), t);
     }
     entries[t] = e;
@@ -446,7 +461,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     }
     const size_t esz = element_size(e.g_dtype);
     const int64_t per_row = kRowBytes / static_cast<int64_t>(esz);
-    const int head = (e.flags & kEntryVecG) ? e.head : 0;
+    const int head = e.g_head;
     int64_t rows = rows_of(e.numel, esz), start = 0, first_block = 0;
     while (start < e.numel) {
       const bool opens = left == 0;
@@ -461,7 +476,6 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
       int64_t end = rows ? start + take * per_row + (start ? 0 : head) : e.numel;
       if (end >= e.numel) {  // perhaps the head has taken the last, short row
         end = e.numel;
-        left += rows;
         rows = 0;
       }
       Segment s;
@@ -472,9 +486,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
       s.tensor = t;
       s.dtype = e.g_dtype;
       s.head = static_cast<uint8_t>(start ? 0 : std::min<int64_t>(head, s.n));
-      // vectors in one run of bytes only: a view with rows is walked
-      if (!(e.flags & kEntryRowsG)) s.flags = e.flags & (kEntryVecG | kEntryVecClip | kEntryVecAdam);
-      if (e.flags & kEntryRowsOut) s.flags &= ~kEntryVecClip;
+      s.flags = e.flags;
       s.pos = (start ? 0 : kSegBegins) | (end == e.numel ? kSegEnds : 0);
       if (opens) {
         s.next = static_cast<int32_t>(further.size());

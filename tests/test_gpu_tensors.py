@@ -186,6 +186,89 @@ def test_interleaved_slices_in_place():
     assert torch.equal(parent[:, 97:], before[:, 97:])
 
 
+@pytest.mark.parametrize("n", (127, 128, 129, 130, 257))
+@pytest.mark.parametrize("many", (40, 700))
+def test_short_last_rows(n, many):
+    """Tensors whose last 512-byte row is short or taken by the head before the first 16-byte
+    boundary, as many as a small list's warps and several to a warp."""
+    g = gen(17)
+    grads = [make((n,), F32, "odd", g, 1.0 + i) for i in range(many)]
+    outs = [torch.empty(n, device=DEV) for _ in grads]
+    st = state_like([(n,)] * many, g)
+    before = [[x.clone() for x in t] for t in st]
+    ts = absnt.GradTensors(grads, out=outs, params=st[0], m=st[1], v=st[2])
+    absnt.abs_grad_clip(ts, 1.0)
+    total = check_norms(ts, grads, 2)
+    for x, y in zip(grads, outs):
+        check_scaled(y, x, 1.0 / (total + 1e-6), F32)
+    absnt.abs_grad_adamw(ts, HP, 3, 1.0)
+    check_norms(ts, grads, 2)
+    for i in range(0, many, 13):
+        w, m1, v1, e_p, e_m, e_v = adamw_ref(*(b[i].double() for b in before),
+                                             grads[i].double() / (total + 1e-6), HP, 3)
+        for got, ref, tol in zip((t[i] for t in st), (w, m1, v1), (e_p, e_m, e_v)):
+            assert ((got.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16, F16))
+@pytest.mark.parametrize("out_dtype", (F32, BF16))
+def test_every_alignment(dtype, out_dtype):
+    """Gradient, output and state at every distance from a boundary, runs of every length up to a few
+    vectors and one beyond a unit; nothing beside the output is touched."""
+    g = gen(18)
+    room = 32
+    sizes = list(range(1, 40)) + [63, 64, 65, 4095, 4097, 40_000]
+    for shift in range(8):
+        grads, outs, guards, ps = [], [], [], []
+        for k, n in enumerate(sizes):
+            a, b = (shift + k) % 8, (3 * shift + 5 * k) % 8
+            grads.append(make((n + a,), dtype, "dense", g)[a:])
+            whole = torch.full((n + b + room,), 7.0, device=DEV, dtype=out_dtype)
+            guards.append((whole, b))
+            outs.append(whole[b:b + n])
+            ps.append([make((n + b,), F32, "dense", g, 0.02)[b:] for _ in range(3)])
+        p, m, v = (list(x) for x in zip(*ps))
+        for x in v:
+            x.copy_(x.square() + 1e-6)
+        before = [[x.clone() for x in t] for t in (p, m, v)]
+        ts = absnt.GradTensors(grads, out=outs, params=p, m=m, v=v)
+        # with a sum given the second pass runs as a kernel of its own, whatever the list's size
+        absnt.abs_grad_norm(ts)
+        total = check_norms(ts, grads, 2)
+        absnt.abs_grad_clip(ts, 1.0, sum_in=ts.header)
+        absnt.abs_grad_adamw(ts, HP, 3, 1.0, sum_in=ts.header)
+        for i, n in enumerate(sizes):
+            check_scaled(outs[i], grads[i], 1.0 / (total + 1e-6), out_dtype)
+            whole, b = guards[i]
+            assert (whole[:b] == 7).all() and (whole[b + n:] == 7).all()
+            w, m1, v1, e_p, e_m, e_v = adamw_ref(*(t[i].double() for t in before),
+                                                 grads[i].double() / (total + 1e-6), HP, 3)
+            for got, ref, tol in zip((p[i], m[i], v[i]), (w, m1, v1), (e_p, e_m, e_v)):
+                assert ((got.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("width", (1, 3, 63, 64, 65, 200, 4099))
+@pytest.mark.parametrize("dtype", (F32, BF16))
+def test_rows_of_every_width(width, dtype):
+    """Column slices whose rows begin at changing distances from a boundary, in place and into a
+    dense and a sliced output."""
+    g = gen(19)
+    rows = max(3, 30_000 // width)
+    parent = make((rows, 2 * width + 5), dtype, "dense", g)
+    keep = parent.clone()
+    grad, ref = parent[:, 3:3 + width], keep[:, 3:3 + width]
+    for out in (torch.empty(rows, width, device=DEV),
+                torch.empty(rows, width + 3, device=DEV)[:, 1:1 + width], None):
+        ts = absnt.GradTensors([grad], out=None if out is None else [out])
+        absnt.abs_grad_norm(ts)
+        total = check_norms(ts, [ref], 2)
+        absnt.abs_grad_clip(ts, 1.0, sum_in=ts.header)
+        check_scaled(grad if out is None else out, ref, 1.0 / (total + 1e-6),
+                     dtype if out is None else F32)
+    assert torch.equal(parent[:, :3], keep[:, :3])
+    assert torch.equal(parent[:, 3 + width:], keep[:, 3 + width:])
+
+
 def adamw_ref(p, m, v, g, hp, step):
     hp = {k: float(torch.tensor(x, dtype=F32)) for k, x in hp.items()}  # the C struct holds floats
     b1, b2 = hp["beta1"], hp["beta2"]
