@@ -10,6 +10,7 @@
 #include <cuda_fp16.h>
 
 #include "abs_device.cuh"
+#include "normtest_bulk.cuh"
 
 namespace absnt {
 
@@ -224,7 +225,7 @@ template <int NORM>
 struct NormAcc {
   double s = 0.0;
   float mx = 0.f;
-  uint32_t bits = 0;  // any bit set: not every value is +0
+  uint32_t bits = 0;  // all values or-ed
   template <int N>
   __device__ __forceinline__ void add(const float* x) {
     if constexpr (NORM == kNormMax) {
@@ -370,8 +371,10 @@ __device__ __forceinline__ double segment_sum(const TensorsParams& prm, const Se
     if constexpr (NORM != kNormMax) {
       // fp32 squares overflow above 1.8e19 and lose bits below 1e-19; sums of |x| overflow
       // near the largest float.  A segment whose sum says so is taken again in fp64.
-      const bool wide = !(x < 0x1p120) || (NORM == kNorm2 && x < 0x1p-90);
-      if (wide && __any_sync(0xffffffffu, acc.bits != 0))
+      // (below 2^-100 a sum of 2^24 squares may be off by 2^-24 of itself: each loses up to 2^-150)
+      const bool wide = !(x < 0x1p120) || (NORM == kNorm2 && x < 0x1p-100);
+      constexpr uint32_t kSigns = T::kVec == 8 ? 0x80008000u : 0x80000000u;  // zeros have either
+      if (wide && __any_sync(0xffffffffu, (acc.bits & ~kSigns) != 0))
         x = warp_join<NORM>(segment_acc_wide<T, NORM>(prm, s, lane));
     }
   });
@@ -470,28 +473,29 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
 // Joins the parts of a block's warps, each tensor by the warp in which it begins (by warp 0, if it
 // began before the block); `edge[0]` and `edge[1]` receive the parts of a tensor that the block
 // shares with the one before and the one after it.  After a __syncthreads.
+// Returns the tensor whose sum is now known to this warp (in `x`; to be written by the caller), or -1.
 template <int NORM, int WARPS>
-__device__ __forceinline__ void join_parts(const TensorsParams& prm, const BlockParts<WARPS>& parts,
-                                          double* edge) {
+__device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockParts<WARPS>& parts,
+                                          double* edge, double& x) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int state = lane < WARPS ? parts.state[lane] : 0;
   const uint32_t heads = __ballot_sync(0xffffffffu, state & kHead);
   const uint32_t throughs = __ballot_sync(0xffffffffu, state & kThrough);
   const int mine = parts.state[warp];
   if (warp == 0 && lane == 0 && (mine & kHead)) edge[0] = parts.head[0];
-  if (!((mine & kTail) || (warp == 0 && (mine & kThrough)))) return;
+  if (!((mine & kTail) || (warp == 0 && (mine & kThrough)))) return -1;
   const uint32_t stop = ~throughs & ~((2u << warp) - 1u);  // warps after this one that end it
   const uint32_t u = stop ? static_cast<uint32_t>(__ffs(stop)) - 1u : 32u;
   const bool ends = u < 32 && ((heads >> u) & 1u);
-  double x = lane == warp || (lane > warp && lane < u && lane < WARPS) ? parts.open[lane]
-             : lane == u && ends                                       ? parts.head[lane]
-                                                                       : 0.0;
+  x = lane == warp || (lane > warp && lane < u && lane < WARPS) ? parts.open[lane]
+      : lane == u && ends                                       ? parts.head[lane]
+                                                                : 0.0;
   x = warp_join<NORM>(x);
   if (lane == 0) {
-    if ((mine & kTail) && ends) write_norm<NORM>(prm, parts.tensor[warp], x);
     if (!(mine & kTail)) edge[0] = x;
     if (!ends) edge[1] = x;
   }
+  return (mine & kTail) && ends ? parts.tensor[warp] : -1;
 }
 
 // The sum of a block from those of its warps, in every lane.  After a __syncthreads.
@@ -541,7 +545,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   if (lane == 0) parts.sum[warp] = sum;
   grid_launch_dependents();
   __syncthreads();
-  join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x);
+  double x;
+  const int known = join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x, x);
+  if (known >= 0 && lane == 0) write_norm<NORM>(prm, known, x);
   if (warp == 0) {
     sum = join_warps<NORM, WARPS>(parts.sum);
     if (lane == 0) prm.block_sum[blockIdx.x] = sum;
@@ -985,142 +991,245 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
 
 // ---- small lists: everything in one cluster -------------------------------------------------
 // Norm and second pass in one launch.  Up to kClusterBlocks blocks, launched as one cluster, hold
-// the whole list in shared memory; the cluster's barrier takes the place of tickets, and sums are
-// read from the other blocks' shared memory.
+// the whole list in shared memory, and every block sends its sums into the shared memory of all
+// (asynchronous stores counted on a barrier there): no ticket, no round trip to L2.
 enum { kOpNone = 0, kOpScale = 1, kOpAdamw = 2 };
 
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+// What a block has for the others: its sum, and its parts of the tensors that it shares.
+struct BlockSums {
+  double sum, edge[2], pad;
+};
+
+// The address in block `rank`'s shared memory of what lies at `p` in this block's.
+__device__ __forceinline__ uint32_t block_addr(const void* p, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+  return a;
 }
-__device__ __forceinline__ void cluster_wait() {
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+__device__ __forceinline__ void send_double(uint32_t to, double x, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to),
+               "l"(__double_as_longlong(x)), "r"(bar)
+               : "memory");
 }
-// A double in another block's shared memory, at the place where `p` points to in this one's.
-__device__ __forceinline__ double ld_block(const double* p, int block) {
-  uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(p));
-  double x;
-  asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(a) : "r"(block));
-  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(x) : "r"(a) : "memory");
-  return x;
+// The bits of a value of a type known at run time, and the value.
+__device__ __forceinline__ uint32_t load_bits(const char* p, bool wide) {
+  return wide ? *reinterpret_cast<const uint32_t*>(p) : *reinterpret_cast<const uint16_t*>(p);
+}
+__device__ __forceinline__ float value_of(uint32_t bits, int dtype) {
+  return dtype == ABS_F32    ? __uint_as_float(bits)
+         : dtype == ABS_BF16 ? __uint_as_float(bits << 16)
+                             : TF16::to_float(static_cast<uint16_t>(bits));
+}
+
+// AdamW on n elements, this lane's i0, i0 + 32, ...; bits(i) are those of element i's gradient.
+template <typename F>
+__device__ __forceinline__ void adamw_elements(const AdamScalars& a, const StateArrays& s,
+                                               uint32_t i0, uint32_t n, float factor, int dtype,
+                                               F&& bits) {
+  constexpr int kBatch = 4;
+#pragma unroll 1
+  for (; i0 < n; i0 += kBatch * 32) {
+    uint32_t x[kBatch];
+    float p[kBatch], m[kBatch], v[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const uint32_t i = i0 + j * 32;
+      if (i < n) p[j] = s.p[i], m[j] = s.m[i], v[j] = s.v[i], x[j] = bits(i);
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const uint32_t i = i0 + j * 32;
+      if (i < n) {
+        adamw_elem(a, a.omb1, a.omb2, factor * value_of(x[j], dtype), p[j], m[j], v[j]);
+        s.p[i] = p[j], s.m[i] = m[j], s.v[i] = v[j];
+        if (s.p16) s.p16[i] = to_bf16(p[j]);
+      }
+    }
+  }
+}
+
+// Where the second pass of a segment goes, out of its tensor's entry.
+struct Target {
+  const void* g;
+  void* out;
+  StateArrays state;
+  int out_dtype, group;
+};
+__device__ __forceinline__ Target target_of(const TensorEntry& e) {
+  return Target{e.g, e.out, {e.p, e.m, e.v, e.p16}, e.out_dtype, e.group};
 }
 
 template <int OP>
 __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const GroupScalars& groups,
-                                              const Segment& s, uint32_t lane, float factor,
-                                              const uint4* keep) {
-  const TensorEntry& e = prm.entries[s.tensor];
+                                              const Target& e, const Segment& s, uint32_t lane,
+                                              float factor, const uint4* keep) {
   const int in = s.dtype;
-  const uint32_t per = in == ABS_F32 ? 4 : 8;
-  const uint32_t nv = (s.n - s.head) / per;
+  const bool rows = s.flags & kEntryRowsG, wide = in == ABS_F32;
+  const uint32_t per = wide ? 4 : 8, esz = wide ? 4 : 2;
+  const uint32_t nv = rows ? 0 : (s.n - s.head) / per, body = nv * per;
   const int64_t first = s.start + s.head;
+  // a gradient in one run: its body lies in shared memory, head and rest (at most 7 elements each)
+  // in global memory
+  const char* kept = reinterpret_cast<const char*>(keep - lane);
+  const auto bits = [&](uint32_t i) {
+    const char* p = i - s.head < body ? kept + (i - s.head) * esz
+                                      : static_cast<const char*>(s.g) + static_cast<size_t>(i) * esz;
+    return load_bits(p, wide);
+  };
   if constexpr (OP == kOpScale) {
     const int out = prm.in_place ? in : e.out_dtype;
     void* y = prm.in_place ? const_cast<void*>(e.g) : e.out;
-    if (!(s.flags & kEntryVecScale)) {
-      scale_walk(e, s.start, lane, s.n, 32, factor, prm.in_place);
+    if (rows || (!prm.in_place && (s.flags & kEntryRowsOut))) {
+      scale_walk(prm.entries[s.tensor], s.start, lane, s.n, 32, factor, prm.in_place);
       return;
     }
-    for (uint32_t v = lane; v < nv; v += 32)
-      store_scaled(keep[v - lane], in, y, first + static_cast<int64_t>(v) * per, out, factor);
-    const auto one = [&](uint32_t i) {
-      store_any(y, s.start + i, out, factor * load_any(e.g, s.start + i, in));
-    };
-    if (lane < s.head) one(lane);
-    const uint32_t i = s.head + nv * per + lane;
-    if (i < s.n) one(i);
+    uint32_t i0 = lane, end = s.n;  // what is taken element by element
+    if (s.flags & kEntryVecScale) {
+      for (uint32_t v = lane; v < nv; v += 32)
+        store_scaled(keep[v - lane], in, y, first + static_cast<int64_t>(v) * per, out, factor);
+      i0 = lane < 8 ? (lane < s.head ? lane : s.n) : s.head + body + lane - 8;
+      end = i0 < s.n && lane < 16 ? i0 + 1 : i0;
+    }
+    with_type(in, [&](auto type) {
+      using T = decltype(type);
+      using S = typename T::scalar;
+      const S *g = static_cast<const S*>(s.g), *k = reinterpret_cast<const S*>(kept) - s.head;
+#pragma unroll 4
+      for (; i0 < end; i0 += 32) {
+        const S* p = (i0 - s.head < body ? k : g) + i0;
+        store_any(y, s.start + i0, out, factor * T::to_float(*p));
+      }
+    });
   } else {
     const AdamScalars& a = groups.a[e.group];
-    const StateArrays state{e.p, e.m, e.v, e.p16};
-    if (!(s.flags & kEntryVecAdamw)) {
-      with_type(in, [&](auto type) {
-        adamw_walk<decltype(type)>(a, state, e, s.start, lane, s.n, 32, factor);
+    const StateArrays at{e.state.p + s.start, e.state.m + s.start, e.state.v + s.start,
+                         e.state.p16 ? e.state.p16 + s.start : nullptr};
+    if (rows) {
+      const TensorEntry& full = prm.entries[s.tensor];
+      Walk<int64_t> w = grad_walk<int64_t>(full, s.start + lane, 32);
+      const char* g = static_cast<const char*>(e.g) + w.base * esz;
+      adamw_elements(a, at, lane, s.n, factor, in, [&](uint32_t) {
+        const uint32_t x = load_bits(g + w.at * esz, wide);
+        w.next();
+        return x;
       });
       return;
     }
-    for (uint32_t v = lane; v < nv; v += 32) {
-      const int64_t i = first + static_cast<int64_t>(v) * per;
-      float x[8] = {};
-      const uint4 raw = keep[v - lane];
-      if (in == ABS_F32)
-        TF32::unpack(raw, x);
-      else if (in == ABS_BF16)
-        TBF16::unpack(raw, x);
-      else
-        TF16::unpack(raw, x);
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (k == 1 && in == ABS_F32) break;
-        const int64_t j = i + 4 * k;
-        float4 w = ld_state_16(e.p + j), m = ld_state_16(e.m + j), q = ld_state_16(e.v + j);
-        adamw_quad(a, make_float2(factor * x[4 * k], factor * x[4 * k + 1]),
-                   make_float2(factor * x[4 * k + 2], factor * x[4 * k + 3]), w, m, q);
-        st_stream_16(e.p + j, w);
-        st_stream_16(e.m + j, m);
-        st_stream_16(e.v + j, q);
-        if (e.p16) st_bf16x4(e.p16 + j, w);
+    uint32_t i0 = lane, end = s.n;
+    if (s.flags & kEntryVecAdamw) {
+#pragma unroll 1
+      for (uint32_t v = lane; v < nv; v += 32) {
+        const uint32_t i = s.head + v * per;
+        const uint4 raw = keep[v - lane];
+        float4 w = ld_state_16(at.p + i), m = ld_state_16(at.m + i), q = ld_state_16(at.v + i);
+        float4 w1, m1, q1;
+        if (!wide)
+          w1 = ld_state_16(at.p + i + 4), m1 = ld_state_16(at.m + i + 4), q1 = ld_state_16(at.v + i + 4);
+        float x[8] = {};
+        if (wide)
+          TF32::unpack(raw, x);
+        else if (in == ABS_BF16)
+          TBF16::unpack(raw, x);
+        else
+          TF16::unpack(raw, x);
+        const auto store = [&](uint32_t k, const float4& p, const float4& mm, const float4& vv) {
+          st_stream_16(at.p + k, p);
+          st_stream_16(at.m + k, mm);
+          st_stream_16(at.v + k, vv);
+          if (at.p16) st_bf16x4(at.p16 + k, p);
+        };
+        adamw_quad(a, make_float2(factor * x[0], factor * x[1]),
+                   make_float2(factor * x[2], factor * x[3]), w, m, q);
+        store(i, w, m, q);
+        if (!wide) {
+          adamw_quad(a, make_float2(factor * x[4], factor * x[5]),
+                     make_float2(factor * x[6], factor * x[7]), w1, m1, q1);
+          store(i + 4, w1, m1, q1);
+        }
       }
+      // head and rest in one go: lanes 0..7 and 8..15
+      i0 = lane < 8 ? (lane < s.head ? lane : s.n) : s.head + body + lane - 8;
+      end = i0 < s.n && lane < 16 ? i0 + 1 : i0;
     }
-    const auto one = [&](uint32_t i) {
-      adamw_one(a, state, s.start + i, factor * load_any(e.g, s.start + i, in));
-    };
-    if (lane < s.head) one(lane);
-    const uint32_t i = s.head + nv * per + lane;
-    if (i < s.n) one(i);
+    adamw_elements(a, at, i0, end, factor, in, bits);
   }
 }
 
 template <int NORM, int OP>
-__global__ void __launch_bounds__(kClusterWarps * 32)
+__global__ void __launch_bounds__(kClusterWarps * 32, 1)
     tensors_cluster_kernel(const __grid_constant__ TensorsParams prm,
                            const __grid_constant__ GroupScalars groups, int rows) {
   extern __shared__ uint4 kept[];  // `rows` rows for each warp
   __shared__ BlockParts<kClusterWarps> parts;
-  __shared__ double s_edge[2], s_sum;
+  __shared__ BlockSums mine, all[kClusterBlocks];
+  __shared__ uint64_t bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int blocks = gridDim.x;
+  if (threadIdx.x == 0) {
+    mine.edge[0] = mine.edge[1] = 0.0;
+    mbar_init(&bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_expect_tx(&bar, blocks * 3 * sizeof(double));
+  }
+  __syncwarp();
+  // the others' shared memory may be written once all blocks have come here
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  // the tables were there before any kernel of the stream
   const Segment opening = prm.opening[blockIdx.x * kClusterWarps + warp];
+  Target target{};
+  if (OP != kOpNone && opening.tensor >= 0) target = target_of(prm.entries[opening.tensor]);
+  // tensors that several blocks share (at most blocks - 1), dealt out to the warps of the cluster
+  const int w = blockIdx.x + blocks * warp;
+  Spanning span{-1, 0, 0, 0};
+  if (w < prm.n_spanning) span = prm.spanning[w];
   uint4* keep = kept + warp * rows * 32 + lane;
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   grid_dependency_wait();
   double sum = warp_sum<NORM, OP != kOpNone>(prm, opening, parts, keep);
   if (lane == 0) parts.sum[warp] = sum;
   __syncthreads();
-  join_parts<NORM>(prm, parts, s_edge);
+  double x;
+  const int known = join_parts<NORM>(prm, parts, mine.edge, x);
+  __syncthreads();  // the edges are written
   if (warp == 0) {
     sum = join_warps<NORM, kClusterWarps>(parts.sum);
-    if (lane == 0) s_sum = sum;
+    if (lane < blocks) {
+      const uint32_t to = block_addr(&all[blockIdx.x], lane), at = block_addr(&bar, lane);
+      send_double(to, sum, at);
+      send_double(to + 8, mine.edge[0], at);
+      send_double(to + 16, mine.edge[1], at);
+    }
   }
-  cluster_arrive();
-  // tensors that several blocks share, dealt out to the warps of the cluster
-  const int w = blockIdx.x + blocks * warp;
-  Spanning span{-1, 0, 0, 0};
-  if (w < prm.n_spanning) span = prm.spanning[w];  // at most blocks - 1 of them
-  cluster_wait();
+  if (known >= 0 && lane == 0) write_norm<NORM>(prm, known, x);
+  const bool ok = mbar_wait_bounded(&bar, 0);
   grid_launch_dependents();
-  const double total = warp_join<NORM>(lane < blocks ? ld_block(&s_sum, lane) : 0.0);
-  if (span.tensor >= 0)
-    join_spanning<NORM>(prm, span, [&](int b, int k) { return ld_block(s_edge + k, b); });
-  cluster_arrive();  // nothing more is read from other blocks
+  const double total = ok ? warp_join<NORM>(lane < blocks ? all[lane].sum : 0.0)
+                          : __longlong_as_double(0x7ff8000000000000ll);
   const Clip clip = clip_of(total, NORM, prm.scale, prm.max_norm);
+  const bool skip = !ok || OP == kOpNone || (OP == kOpAdamw && !clip.finite) ||
+                    (OP == kOpScale && prm.in_place && clip.factor == 1.f);
+  if (!skip && opening.tensor >= 0) {
+    if constexpr (OP != kOpNone) {
+      Segment s = opening;
+#pragma unroll 1
+      for (int k = 0;; ++k) {
+        segment_apply<OP>(prm, groups, target, s, lane, clip.factor, keep);
+        if (k == opening.more) break;
+        if (!(s.flags & kEntryRowsG))
+          keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
+        s = prm.further[opening.next + k];
+        target = target_of(prm.entries[s.tensor]);
+      }
+    }
+  }
+  if (ok && span.tensor >= 0)
+    join_spanning<NORM>(prm, span, [&](int b, int k) { return all[b].edge[k]; });
   if (blockIdx.x == 0) {
     if (threadIdx.x == 0) write_clip(prm, total, clip);
     for (int i = threadIdx.x; i < prm.n_empty; i += kClusterWarps * 32)
       write_norm<NORM>(prm, prm.empty[i], 0.0);
   }
-  const bool skip = OP == kOpNone || (OP == kOpAdamw && !clip.finite) ||
-                    (OP == kOpScale && prm.in_place && clip.factor == 1.f);
-  if (!skip && opening.tensor >= 0) {
-    if constexpr (OP != kOpNone) {
-      Segment s = opening;
-      for (int k = 0;; ++k) {
-        segment_apply<OP>(prm, groups, s, lane, clip.factor, keep);
-        if (!(s.flags & kEntryRowsG))
-          keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
-        if (k == opening.more) break;
-        s = prm.further[opening.next + k];
-      }
-    }
-  }
-  cluster_wait();
 }
 
 }  // namespace absnt

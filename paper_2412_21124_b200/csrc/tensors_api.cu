@@ -17,7 +17,7 @@ namespace {
 constexpr uint64_t kPlanMagic = 0x6e616c7054534241ull;  // "ABSTplan"
 constexpr int64_t kMaxRow = int64_t{1} << 30;
 // Most elements that AdamW takes in one cluster: above, the state's traffic wants all SMs.
-constexpr int64_t kClusterAdamw = 128 * 1024;
+constexpr int64_t kClusterAdamw = 96 * 1024;
 constexpr size_t kKeepBytes = size_t{kClusterWarps} * 512;  // one row of each warp of a block
 constexpr int64_t kMaxElements = int64_t{1} << 46;
 constexpr int64_t kMaxUnits = int64_t{1} << 30;
