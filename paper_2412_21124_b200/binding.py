@@ -729,16 +729,24 @@ class GradTensors:
 
     def _groups(self, hparams):
         """The hyper-parameters of all groups as a C array, kept while they are the same values."""
-        if isinstance(hparams, (dict, abs_adamw_hparams)):
-            hparams = [hparams]
-        key = [tuple(h.values()) if isinstance(h, dict) else
-               (h.lr, h.beta1, h.beta2, h.eps, h.weight_decay) for h in hparams]
-        if key != self._hparams_of:
-            if len(hparams) < self.n_groups:
+        if hparams != self._hparams_of:
+            if isinstance(hparams, (dict, abs_adamw_hparams)):
+                array = (abs_adamw_hparams * self.n_groups)(*[_hparams(hparams)] * self.n_groups)
+            elif len(hparams) < self.n_groups:
                 raise ValueError("hparams for %d groups are needed" % self.n_groups)
-            self._hparams = (abs_adamw_hparams * len(hparams))(*[_hparams(h) for h in hparams])
-            self._hparams_of = key
+            else:
+                array = (abs_adamw_hparams * len(hparams))(*[_hparams(h) for h in hparams])
+            self._hparams, self._hparams_of = array, _copied(hparams)
         return self._hparams
+
+
+def _copied(hparams):
+    """A copy that compares equal while the values are the same; None for what is not plain dicts."""
+    if isinstance(hparams, dict):
+        return dict(hparams)
+    if isinstance(hparams, (list, tuple)) and all(isinstance(h, dict) for h in hparams):
+        return type(hparams)(dict(h) for h in hparams)
+    return None
 
 
 def _norm_type(norm_type):
@@ -782,7 +790,7 @@ def abs_grad_clip(tensors, max_norm, norm_type=2, grad_scale=1.0, sum_in=None, s
 def abs_grad_adamw(tensors, hparams, step, max_norm=0.0, norm_type=2, grad_scale=1.0, sum_in=None,
                    stream=None):
     """AdamW on the gradients scaled by grad_scale and, with max_norm > 0, clipped by their global
-    norm.  `hparams`: one dict for all tensors or a list with one per group.  An update whose norm
+    norm.  `hparams`: one dict for all tensors, or a list with one per group.  An update whose norm
     is not finite is left out.  Returns the global norm, a view of the object's results (not
     written when max_norm is 0)."""
     hp = tensors._groups(hparams)

@@ -9,6 +9,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "abs_device.cuh"
 #include "normtest_bulk.cuh"
 
@@ -307,38 +309,45 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
     const uint32_t i = s.head + nv * T::kVec + lane;
     if (i < s.n) one(g[i]);
   } else {
-    // a view with rows; a segment of it is a few hundred kilobytes at most unless it is far apart
+    // a view with rows
     const TensorEntry& e = prm.entries[s.tensor];
     const S* g = static_cast<const S*>(e.g);
-    const auto walk = [&](auto index) {
-      constexpr int kWalk = 16;
-      Walk<decltype(index)> w = grad_walk<decltype(index)>(e, s.start + lane, 32);
-      g += w.base;
-      uint32_t i0 = lane;
-      for (; i0 + (kWalk - 1) * 32 < s.n; i0 += kWalk * 32) {
-        S raw[kWalk];
-#pragma unroll
-        for (int j = 0; j < kWalk; ++j) {
-          raw[j] = g[w.at];
-          w.next();
-        }
-#pragma unroll
-        for (int j = 0; j < kWalk; j += 8) {
-          float x[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            x[k] = T::to_float(raw[j + k]);
-            acc.bits |= __float_as_uint(x[k]);
-          }
-          acc.template add<8>(x);
-        }
+    S* kept = reinterpret_cast<S*>(keep - lane);
+    if (e.flags & kEntryFar) {
+      Walk<int64_t> w = grad_walk<int64_t>(e, s.start + lane, 32);
+      for (uint32_t i = lane; i < s.n; i += 32, w.next()) {
+        const S raw = g[w.base + w.at];
+        one(raw);
+        if (KEEP) kept[i] = raw;
       }
-      for (; i0 < s.n; i0 += 32, w.next()) one(g[w.at]);
+      return acc;
+    }
+    constexpr int kWalk = 16;
+    Walk<int32_t> w = grad_walk<int32_t>(e, s.start + lane, 32);
+    g += w.base;
+    const auto batch = [&](uint32_t i0, auto whole) {
+      S raw[kWalk];
+#pragma unroll
+      for (int j = 0; j < kWalk; ++j) {
+        raw[j] = decltype(whole)::value || i0 + j * 32 < s.n ? g[w.at] : S(0);
+        w.next();
+      }
+#pragma unroll
+      for (int j = 0; j < kWalk; j += 8) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = T::to_float(raw[j + k]);
+          acc.bits |= __float_as_uint(x[k]);
+          if (KEEP && (decltype(whole)::value || i0 + (j + k) * 32 < s.n))
+            kept[i0 + (j + k) * 32] = raw[j + k];
+        }
+        acc.template add<8>(x);
+      }
     };
-    if (e.flags & kEntryFar)
-      walk(int64_t{});
-    else
-      walk(int32_t{});
+    uint32_t i0 = lane;
+    for (; i0 - lane + kWalk * 32 <= s.n; i0 += kWalk * 32) batch(i0, std::true_type{});
+    if (i0 < s.n) batch(i0, std::false_type{});
   }
   return acc;
 }
@@ -425,6 +434,14 @@ struct BlockParts {
   int tensor[WARPS], state[WARPS];
 };
 
+// Rows of 512 bytes that a segment leaves in shared memory: all vectors of one run of elements
+// (head and rest are not kept), all elements of a view with rows.
+__device__ __forceinline__ uint32_t kept_rows(const Segment& s) {
+  const uint32_t n = (s.flags & kEntryRowsG) ? s.n : s.n - s.head;
+  const uint32_t per_row = s.dtype == ABS_F32 ? 128 : 256, per = per_row / 32;
+  return (s.flags & kEntryRowsG) ? (n + per_row - 1) / per_row : (n / per + 31) / 32;
+}
+
 // One warp's rows; returns their sum.
 template <int NORM, bool KEEP, int WARPS>
 __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segment& opening,
@@ -439,8 +456,7 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
       Segment next = s;
       if (k < opening.more) next = prm.further[opening.next + k];
       const double y = segment_sum<NORM, KEEP>(prm, s, lane, keep);
-      if (KEEP && !(s.flags & kEntryRowsG))
-        keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
+      if (KEEP) keep += kept_rows(s) * 32;
       sum = norm_join<NORM>(sum, y);
       x = norm_join<NORM>(x, y);
       begun |= (s.pos & kSegBegins) != 0;
@@ -735,8 +751,9 @@ __device__ __forceinline__ Run make_run(const S* g, uint32_t n, uint32_t head, c
   return r;
 }
 
-template <typename TI, typename TO>
-__device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange& r, float factor,
+// `factor()` gives the factor, waiting for it the first time; a NaN: nothing is to be written.
+template <typename TI, typename TO, typename F>
+__device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange& r, F&& factor,
                                            void* out, bool in_place) {
   using SI = typename TI::scalar;
   using SO = typename TO::scalar;
@@ -748,10 +765,9 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
     g += r.start;
     y += r.start;
     const Run run = make_run(g, r.n, r.start ? 0u : min(uint32_t{e.scale_head}, r.n), lo, hi);
-    const auto one = [&](uint32_t k) { y[k] = TO::from_float(factor * TI::to_float(g[k])); };
-    const auto store = [&](uint32_t v, float* x) {
+    const auto store = [&](uint32_t v, float* x, float f) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] *= factor;
+      for (int k = 0; k < 8; ++k) x[k] *= f;
       store8<TO>(y + run.head + v * 8, x);
     };
     if (run.o == 0) {
@@ -762,12 +778,14 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
         for (int j = 0; j < kBatch; ++j)
           if (v0 + j * kTensorThreads < run.nv)
             raw[j] = load8<TI>(g + run.head + (v0 + j * kTensorThreads) * 8);
+        const float f = factor();
+        if (f != f) return;
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
           if (v0 + j * kTensorThreads < run.nv) {
             float x[8];
             unpack8<TI>(raw[j], x);
-            store(v0 + j * kTensorThreads, x);
+            store(v0 + j * kTensorThreads, x, f);
           }
       }
     } else {
@@ -778,72 +796,81 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
         for (int j = 0; j < kBatch; ++j)
           if (v0 + j * kTensorThreads < run.nv)
             raw[j] = load_shifted8<TI>(g + run.head + (v0 + j * kTensorThreads) * 8, run.o);
+        const float f = factor();
+        if (f != f) return;
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
           if (v0 + j * kTensorThreads < run.nv) {
             float x[8];
             unpack_shifted8<TI>(raw[j], run.o, x);
-            store(v0 + j * kTensorThreads, x);
+            store(v0 + j * kTensorThreads, x, f);
           }
       }
     }
     // head and rest, at most 15 elements each
     const uint32_t rest = run.head + run.nv * 8 + tid;
-    if (tid < run.head) one(tid);
-    if (rest < r.n) one(rest);
-  } else if (!(e.flags & kEntryFar) && (in_place || !(e.flags & kEntryRowsOut))) {
-    // rows into one run, or in place: one walk, and whole batches without a bound
+    if (tid < run.head || rest < r.n) {
+      const float f = factor();
+      if (f != f) return;
+      if (tid < run.head) y[tid] = TO::from_float(f * TI::to_float(g[tid]));
+      if (rest < r.n) y[rest] = TO::from_float(f * TI::to_float(g[rest]));
+    }
+    return;
+  }
+  const float f = factor();
+  if (f != f) return;
+  if (!(e.flags & kEntryFar) && (in_place || !(e.flags & kEntryRowsOut))) {
+    // rows into one run, or in place: one walk
     constexpr int kBatch = 16;
     Walk<int32_t> w = grad_walk<int32_t>(e, r.start + tid, kTensorThreads);
     g += w.base;
     y += in_place ? w.base : r.start + tid;
-    uint32_t i0 = tid;
-    for (; i0 + (kBatch - 1) * kTensorThreads < r.n; i0 += kBatch * kTensorThreads) {
+    const auto batch = [&](uint32_t i0, auto whole) {
       SI x[kBatch];
       Walk<int32_t> again = w;
 #pragma unroll
       for (int j = 0; j < kBatch; ++j) {
-        x[j] = g[w.at];
+        if (decltype(whole)::value || i0 + j * kTensorThreads < r.n) x[j] = g[w.at];
         w.next();
       }
-      if (in_place) {
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          y[again.at] = TO::from_float(factor * TI::to_float(x[j]));
-          again.next();
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j)
-          y[j * kTensorThreads] = TO::from_float(factor * TI::to_float(x[j]));
-        y += kBatch * kTensorThreads;
+      for (int j = 0; j < kBatch; ++j) {
+        if (decltype(whole)::value || i0 + j * kTensorThreads < r.n)
+          y[in_place ? again.at : j * kTensorThreads] = TO::from_float(f * TI::to_float(x[j]));
+        if (in_place) again.next();
       }
-    }
-    for (; i0 < r.n; i0 += kTensorThreads) {
-      const SO x = TO::from_float(factor * TI::to_float(g[w.at]));
-      if (in_place) {
-        y[w.at] = x;
-      } else {
-        *y = x;
-        y += kTensorThreads;
-      }
-      w.next();
-    }
+      if (!in_place) y += kBatch * kTensorThreads;
+    };
+    uint32_t i0 = tid;
+    for (; i0 - tid + kBatch * kTensorThreads <= r.n; i0 += kBatch * kTensorThreads)
+      batch(i0, std::true_type{});
+    if (i0 < r.n) batch(i0, std::false_type{});
   } else {
-    scale_walk(e, r.start, tid, r.n, kTensorThreads, factor, in_place);
+    scale_walk(e, r.start, tid, r.n, kTensorThreads, f, in_place);
   }
 }
 
-// One CTA per unit, the last unit of the list first.
+// One CTA per unit, the last unit of the list first.  After this call's norm kernel the first loads
+// are made before the factor is waited for: that kernel lets this one start only after its own wait,
+// so whatever wrote the tensors before is done.
 __global__ void __launch_bounds__(kTensorThreads, 3)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
   const int u = prm.n_scale - 1 - blockIdx.x;
   const TensorEntry& e = prm.entries[prm.scale_tensor[u]];
   const UnitRange r = unit_range(e, u - e.first_scale, prm.scale_unit, e.scale_head);
-  grid_dependency_wait();
-  float factor = __ldcg(prm.factor);
-  if (factor != factor) factor = static_cast<float>(prm.scale);  // not finite: not clipped
-  if (prm.in_place && factor == 1.f) return;                     // x * 1 is x
+  bool have = false;
+  if (!prm.after_norm) grid_dependency_wait();
+  float value = 0.f;
+  const auto factor = [&]() {
+    if (!have) {
+      if (prm.after_norm) grid_dependency_wait();
+      value = __ldcg(prm.factor);
+      if (value != value) value = static_cast<float>(prm.scale);  // not finite: not clipped
+      if (prm.in_place && value == 1.f) value = __int_as_float(0x7fc00000);  // x * 1 is x
+      have = true;
+    }
+    return value;
+  };
   with_type(e.g_dtype, [&](auto ti) {
     using TI = decltype(ti);
     if (prm.in_place)
@@ -1066,21 +1093,27 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
   const int in = s.dtype;
   const bool rows = s.flags & kEntryRowsG, wide = in == ABS_F32;
   const uint32_t per = wide ? 4 : 8, esz = wide ? 4 : 2;
-  const uint32_t nv = rows ? 0 : (s.n - s.head) / per, body = nv * per;
-  const int64_t first = s.start + s.head;
-  // a gradient in one run: its body lies in shared memory, head and rest (at most 7 elements each)
-  // in global memory
+  // what lies in shared memory: the body of one run (head and rest, at most 7 elements each, are in
+  // global memory), or a view with rows whole
+  const uint32_t head = rows ? 0 : s.head, nv = rows ? 0 : (s.n - s.head) / per;
+  const uint32_t body = rows ? s.n : nv * per;
+  const int64_t first = s.start + head;
   const char* kept = reinterpret_cast<const char*>(keep - lane);
   const auto bits = [&](uint32_t i) {
-    const char* p = i - s.head < body ? kept + (i - s.head) * esz
-                                      : static_cast<const char*>(s.g) + static_cast<size_t>(i) * esz;
+    const char* p = i - head < body ? kept + (i - head) * esz
+                                    : static_cast<const char*>(s.g) + static_cast<size_t>(i) * esz;
     return load_bits(p, wide);
   };
   if constexpr (OP == kOpScale) {
     const int out = prm.in_place ? in : e.out_dtype;
     void* y = prm.in_place ? const_cast<void*>(e.g) : e.out;
-    if (rows || (!prm.in_place && (s.flags & kEntryRowsOut))) {
-      scale_walk(prm.entries[s.tensor], s.start, lane, s.n, 32, factor, prm.in_place);
+    if (prm.in_place ? rows : (s.flags & kEntryRowsOut) != 0) {
+      const TensorEntry& full = prm.entries[s.tensor];
+      Walk<int64_t> w = prm.in_place ? grad_walk<int64_t>(full, s.start + lane, 32)
+                                     : out_walk(full, s.start + lane, 32);
+#pragma unroll 4
+      for (uint32_t i = lane; i < s.n; i += 32, w.next())
+        store_any(y, w.base + w.at, out, factor * value_of(bits(i), in));
       return;
     }
     uint32_t i0 = lane, end = s.n;  // what is taken element by element
@@ -1093,10 +1126,10 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
     with_type(in, [&](auto type) {
       using T = decltype(type);
       using S = typename T::scalar;
-      const S *g = static_cast<const S*>(s.g), *k = reinterpret_cast<const S*>(kept) - s.head;
+      const S *g = static_cast<const S*>(s.g), *k = reinterpret_cast<const S*>(kept) - head;
 #pragma unroll 4
       for (; i0 < end; i0 += 32) {
-        const S* p = (i0 - s.head < body ? k : g) + i0;
+        const S* p = (i0 - head < body ? k : g) + i0;
         store_any(y, s.start + i0, out, factor * T::to_float(*p));
       }
     });
@@ -1104,17 +1137,6 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
     const AdamScalars& a = groups.a[e.group];
     const StateArrays at{e.state.p + s.start, e.state.m + s.start, e.state.v + s.start,
                          e.state.p16 ? e.state.p16 + s.start : nullptr};
-    if (rows) {
-      const TensorEntry& full = prm.entries[s.tensor];
-      Walk<int64_t> w = grad_walk<int64_t>(full, s.start + lane, 32);
-      const char* g = static_cast<const char*>(e.g) + w.base * esz;
-      adamw_elements(a, at, lane, s.n, factor, in, [&](uint32_t) {
-        const uint32_t x = load_bits(g + w.at * esz, wide);
-        w.next();
-        return x;
-      });
-      return;
-    }
     uint32_t i0 = lane, end = s.n;
     if (s.flags & kEntryVecAdamw) {
 #pragma unroll 1
@@ -1216,8 +1238,7 @@ __global__ void __launch_bounds__(kClusterWarps * 32, 1)
       for (int k = 0;; ++k) {
         segment_apply<OP>(prm, groups, target, s, lane, clip.factor, keep);
         if (k == opening.more) break;
-        if (!(s.flags & kEntryRowsG))
-          keep += ((s.n - s.head) / (s.dtype == ABS_F32 ? 4 : 8) + 31) / 32 * 32;
+        keep += kept_rows(s) * 32;
         s = prm.further[opening.next + k];
         target = target_of(prm.entries[s.tensor]);
       }
