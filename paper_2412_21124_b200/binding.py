@@ -9,6 +9,7 @@ import ctypes
 import math
 import os
 
+import numpy as np
 import torch
 
 from . import build as _build
@@ -587,6 +588,10 @@ def abs_persample_norm_test_coordwise(G, eta, stats_out, gbar_out, b_next_out, s
 
 # ---------------------------------------------------------------------- lists of tensors
 _TENSOR_DTYPES = {torch.float32: ABS_F32, torch.bfloat16: ABS_BF16, torch.float16: ABS_F16}
+# abs_tensor with its three row fields in one
+_TENSOR_FIELDS = np.dtype([("data", np.uint64), ("numel", np.int64), ("rows", np.int64, 3),
+                           ("dtype", np.int32), ("group", np.int32)])
+assert _TENSOR_FIELDS.itemsize == ctypes.sizeof(abs_tensor)
 _NORM_TYPES = {2: ABS_NORM_2, 1: ABS_NORM_1, math.inf: ABS_NORM_MAX}
 
 
@@ -613,18 +618,26 @@ def _rows(t, order, name):
 
 
 def _tensor_array(tensors, orders, name, dtypes, groups=None, dense=False):
-    """The abs_tensor array of one role."""
-    arr = (abs_tensor * max(len(tensors), 1))()
-    for i, t in enumerate(tensors):
-        code = _TENSOR_DTYPES.get(t.dtype)
+    """The abs_tensor array of one role (a numpy array of its fields, or None for no tensors)."""
+    n = len(tensors)
+    arr = np.zeros(max(n, 1), dtype=_TENSOR_FIELDS)
+    if not n:
+        return arr
+    codes = [_TENSOR_DTYPES.get(t.dtype) for t in tensors]
+    for i, code in enumerate(codes):
         if code not in dtypes:
-            raise TypeError("%s[%d] must not be %s" % (name, i, t.dtype))
-        rows = (0, 0, 0)
-        if t.numel() and not (orders[i] is None and t.is_contiguous()):
+            raise TypeError("%s[%d] must not be %s" % (name, i, tensors[i].dtype))
+    arr["data"] = [t.data_ptr() for t in tensors]
+    arr["numel"] = [t.numel() for t in tensors]
+    arr["dtype"] = codes
+    if groups is not None:
+        arr["group"] = groups
+    for i, t in enumerate(tensors):
+        if not (orders[i] is None and t.is_contiguous()) and t.numel():
             rows = _rows(t, orders[i] or range(t.dim()), "%s[%d]" % (name, i))
             if dense and rows[0]:
                 raise TypeError("%s[%d] must be dense, in the order of params[%d]" % (name, i, i))
-        arr[i] = abs_tensor(t.data_ptr() or None, t.numel(), *rows, code, groups[i] if groups else 0)
+            arr["rows"][i] = rows
     return arr
 
 
@@ -656,20 +669,22 @@ class GradTensors:
         given = [roles[k] is not None for k in ("params", "m", "v")]
         if any(given) != all(given) or (roles["params_bf16"] is not None and not given[0]):
             raise ValueError("params, m and v go together, params_bf16 with them")
+        shapes = [g.shape for g in grads]
         for name, x in roles.items():
             if x is None:
                 continue
             if len(x) != n:
                 raise ValueError("%s: %d tensors for %d gradients" % (name, len(x), n))
-            for i, (t, g) in enumerate(zip(x, grads)):
-                if t.shape != g.shape:
-                    raise ValueError("%s[%d] has shape %s, its gradient %s"
-                                     % (name, i, tuple(t.shape), tuple(g.shape)))
+            if [t.shape for t in x] != shapes:
+                raise ValueError("%s: shapes must be those of the gradients" % name)
         groups = [0] * n if groups is None else [int(k) for k in groups]
         if len(groups) != n or any(not 0 <= k < ABS_MAX_GROUPS for k in groups):
             raise ValueError("groups: one number in 0..%d per tensor" % (ABS_MAX_GROUPS - 1))
         self._keep = (grads, roles)
-        _check_one_device(*grads, *(t for x in roles.values() if x is not None for t in x))
+        here = torch.device("cuda", torch.cuda.current_device())
+        for x in (grads, *roles.values()):
+            if x is not None and any(t.device != here for t in x):
+                _check_one_device(*x)  # says which one
         # the order in which a tensor's dimensions are walked: the parameter's own, else the
         # gradient's, largest stride first (None: the order of the shape)
         orders = [None if x.is_contiguous() else
@@ -682,13 +697,13 @@ class GradTensors:
                                     ("params_bf16", (ABS_BF16,), True)):
             x = roles[name]
             arrays[name] = None if x is None else _tensor_array(x, orders, name, dtypes, None, dense)
-        nbytes = lib().abs_tensors_plan_bytes(arrays["grads"], n)
+        where = {k: None if a is None else a.ctypes.data for k, a in arrays.items()}
+        nbytes = lib().abs_tensors_plan_bytes(where["grads"], n)
         self._plan = (ctypes.c_uint64 * (nbytes // 8 + 1))()
-        rc = lib().abs_tensors_plan(*(arrays[k] for k in ("grads", "out", "params", "m", "v",
-                                                          "params_bf16")), n, self._plan, nbytes)
+        rc = lib().abs_tensors_plan(*(where[k] for k in ("grads", "out", "params", "m", "v",
+                                                         "params_bf16")), n, self._plan, nbytes)
         if rc != ABS_OK:
             raise AbsError(rc, "abs_tensors_plan")
-        self._adam = roles["params"] is not None
         self.n_groups = max(groups, default=0) + 1
         self._device = torch.cuda.current_device()
         self._plan_ptr = ctypes.addressof(self._plan)
