@@ -19,6 +19,10 @@ cross the wire.  This module holds that small host-side logic:
                       peers; rank r then runs the fused call on index range r of all ranks'
                       buffers, so the gradient exchange is the kernel's own loads over NVLink
                       (no all-reduce of d elements, no second all-reduce for the variance)
+  join_power_sums, sharded_grad_clip, sharded_grad_adamw
+                      global-norm clipping when the ranks hold different tensors (or ranges of
+                      them): one double per rank is gathered, joined in rank order, and the second
+                      pass takes the result from device memory
   max_over_ranks      max-reduction used for timing
 """
 import os
@@ -180,6 +184,47 @@ def ddp_normtest_adamw(peer_grads, eta, b_cur, stats_out, b_next_out, params, m_
                 dist.broadcast(params[r_lo:r_hi], src=dist.get_global_rank(group, r)
                                if group is not None else r, group=group)
     return out
+
+
+def join_power_sums(local, norm_type=2, group=None):
+    """The power sum of all ranks' gradients from each rank's own (`local`: one float64 element, a
+    GradTensors' header[ABS_GRAD_SUM]): added in rank order, for the largest magnitude the
+    maximum, so that every rank has the same bits.  A new tensor on the device of `local`; under
+    NCCL the host does not wait."""
+    local = local.reshape(1)
+    if not (dist.is_initialized() and dist.get_world_size(group) > 1):
+        return local.clone()
+    on_gpu = dist.get_backend(group) == "nccl"
+    mine = local.clone() if on_gpu == local.is_cuda else (local.cuda() if on_gpu else local.cpu())
+    parts = [torch.empty_like(mine) for _ in range(dist.get_world_size(group))]
+    dist.all_gather(parts, mine, group=group)
+    total = parts[0]
+    for part in parts[1:]:  # torch.maximum keeps a NaN
+        total = torch.maximum(total, part) if norm_type == float("inf") else total + part
+    return total.to(local.device)
+
+
+def sharded_grad_clip(tensors, max_norm, norm_type=2, grad_scale=1.0, group=None):
+    """abs_grad_clip where each rank's GradTensors holds its own part of the gradients (FSDP
+    shards, pipeline stages): the norm is that of all ranks' parts together.  Collective.  A tensor
+    that several ranks hold has to be in one rank's list only, or its norm counts twice."""
+    if not (dist.is_initialized() and dist.get_world_size(group) > 1):
+        return binding.abs_grad_clip(tensors, max_norm, norm_type, grad_scale)
+    binding.abs_grad_norm(tensors, norm_type, grad_scale)
+    total = join_power_sums(tensors.header[binding.ABS_GRAD_SUM], norm_type, group)
+    return binding.abs_grad_clip(tensors, max_norm, norm_type, grad_scale, sum_in=total)
+
+
+def sharded_grad_adamw(tensors, hparams, step, max_norm, norm_type=2, grad_scale=1.0, group=None):
+    """abs_grad_adamw where each rank's GradTensors holds its own part of gradients, parameters and
+    moments; as sharded_grad_clip.  A gradient that is not finite on one rank leaves the update out
+    on all of them."""
+    if not (dist.is_initialized() and dist.get_world_size(group) > 1):
+        return binding.abs_grad_adamw(tensors, hparams, step, max_norm, norm_type, grad_scale)
+    binding.abs_grad_norm(tensors, norm_type, grad_scale)
+    total = join_power_sums(tensors.header[binding.ABS_GRAD_SUM], norm_type, group)
+    return binding.abs_grad_adamw(tensors, hparams, step, max_norm, norm_type, grad_scale,
+                                  sum_in=total)
 
 
 def barrier(device=None):
