@@ -771,7 +771,7 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
       store8<TO>(y + run.head + v * 8, x);
     };
     if (run.o == 0) {
-      constexpr int kBatch = 4;
+      constexpr int kBatch = TI::kVec == 8 ? 8 : 4;  // 128 bytes in flight per thread
       for (uint32_t v0 = tid; v0 < run.nv; v0 += kBatch * kTensorThreads) {
         Vec8<TI> raw[kBatch];
 #pragma unroll
