@@ -19,10 +19,9 @@ namespace absnt {
 constexpr int kTensorThreads = 256;
 constexpr int kMaxGroups = ABS_MAX_GROUPS;
 constexpr int kListBlocks = 148;     // blocks of the norm kernel, one for each SM
-constexpr int kListWarps = 32;       // their warps
 constexpr int kClusterBlocks = 16;   // blocks of the one-cluster kernel
-constexpr int kClusterWarps = 16;
 constexpr int kClusterRows = 16;     // most rows that one of its warps takes
+constexpr int kListWarps = 16;       // warps of a block of either
 constexpr int kAdamwUnit = 4096;     // elements of a unit of AdamW
 
 // One tensor of the list.  A view with rows has `row` elements in each row, `stride` elements from
@@ -428,10 +427,9 @@ __device__ __forceinline__ void write_norm(const TensorsParams& prm, int t, doub
 // with there.  There may be one at the front that began before them (kHead: and ends in them), and
 // one at the back that goes on after them (kTail: and begins in them; kThrough: began before them).
 enum { kHead = 1, kTail = 2, kThrough = 4 };
-template <int WARPS>
 struct BlockParts {
-  double head[WARPS], open[WARPS], sum[WARPS];
-  int tensor[WARPS], state[WARPS];
+  double head[kListWarps], open[kListWarps], sum[kListWarps];
+  int tensor[kListWarps], state[kListWarps];
 };
 
 // Rows of 512 bytes that a segment leaves in shared memory: all vectors of one run of elements
@@ -443,9 +441,9 @@ __device__ __forceinline__ uint32_t kept_rows(const Segment& s) {
 }
 
 // One warp's rows; returns their sum.
-template <int NORM, bool KEEP, int WARPS>
+template <int NORM, bool KEEP>
 __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segment& opening,
-                                           BlockParts<WARPS>& parts, uint4* keep) {
+                                           BlockParts& parts, uint4* keep) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   double sum = 0.0, x = 0.0, head = 0.0;
   int state = 0, tensor = -1;
@@ -490,11 +488,11 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
 // began before the block); `edge[0]` and `edge[1]` receive the parts of a tensor that the block
 // shares with the one before and the one after it.  After a __syncthreads.
 // Returns the tensor whose sum is now known to this warp (in `x`; to be written by the caller), or -1.
-template <int NORM, int WARPS>
-__device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockParts<WARPS>& parts,
+template <int NORM>
+__device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockParts& parts,
                                           double* edge, double& x) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int state = lane < WARPS ? parts.state[lane] : 0;
+  const int state = lane < kListWarps ? parts.state[lane] : 0;
   const uint32_t heads = __ballot_sync(0xffffffffu, state & kHead);
   const uint32_t throughs = __ballot_sync(0xffffffffu, state & kThrough);
   const int mine = parts.state[warp];
@@ -503,7 +501,7 @@ __device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockP
   const uint32_t stop = ~throughs & ~((2u << warp) - 1u);  // warps after this one that end it
   const uint32_t u = stop ? static_cast<uint32_t>(__ffs(stop)) - 1u : 32u;
   const bool ends = u < 32 && ((heads >> u) & 1u);
-  x = lane == warp || (lane > warp && lane < u && lane < WARPS) ? parts.open[lane]
+  x = lane == warp || (lane > warp && lane < u && lane < kListWarps) ? parts.open[lane]
       : lane == u && ends                                       ? parts.head[lane]
                                                                 : 0.0;
   x = warp_join<NORM>(x);
@@ -515,10 +513,10 @@ __device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockP
 }
 
 // The sum of a block from those of its warps, in every lane.  After a __syncthreads.
-template <int NORM, int WARPS>
+template <int NORM>
 __device__ __forceinline__ double join_warps(const double* sums) {
   const uint32_t lane = threadIdx.x & 31;
-  return warp_join<NORM>(lane < WARPS ? sums[lane] : 0.0);
+  return warp_join<NORM>(lane < kListWarps ? sums[lane] : 0.0);
 }
 
 // The norm of a tensor that several blocks share, by one warp.  edge(b, i): edge i of block b.
@@ -547,13 +545,13 @@ __device__ __forceinline__ bool last_of(unsigned int* ticket, unsigned int of) {
 // Every warp sums its rows, every block its warps; the block that finishes last joins the blocks,
 // and of the blocks that share a tensor the last one joins that tensor: one launch, and no order of
 // finishing shows in a sum.
-template <int NORM, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32, 1)
+template <int NORM>
+__global__ void __launch_bounds__(kListWarps * 32, 1)
     tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
-  __shared__ BlockParts<WARPS> parts;
+  __shared__ BlockParts parts;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the tables were there before any kernel of the stream
-  const Segment opening = prm.opening[blockIdx.x * WARPS + warp];
+  const Segment opening = prm.opening[blockIdx.x * kListWarps + warp];
   Shared2 shared{-1, -1};
   if (warp == 1 || warp == 2) shared = prm.shared[blockIdx.x];
   grid_dependency_wait();
@@ -565,7 +563,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   const int known = join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x, x);
   if (known >= 0 && lane == 0) write_norm<NORM>(prm, known, x);
   if (warp == 0) {
-    sum = join_warps<NORM, WARPS>(parts.sum);
+    sum = join_warps<NORM>(parts.sum);
     if (lane == 0) prm.block_sum[blockIdx.x] = sum;
   }
   const int i = warp == 1 ? shared.before : warp == 2 ? shared.after : -1;
@@ -582,7 +580,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   if (i >= 0 && last_of(prm.tickets + 1 + i, span.last - span.first + 1))
     join_spanning<NORM>(prm, span, [&](int b, int k) { return __ldcg(prm.edge_sum + 2 * b + k); });
   if (blockIdx.x == 0)
-    for (int k = threadIdx.x; k < prm.n_empty; k += WARPS * 32)
+    for (int k = threadIdx.x; k < prm.n_empty; k += kListWarps * 32)
       write_norm<NORM>(prm, prm.empty[k], 0.0);
 }
 
@@ -1178,11 +1176,11 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
 }
 
 template <int NORM, int OP>
-__global__ void __launch_bounds__(kClusterWarps * 32, 1)
+__global__ void __launch_bounds__(kListWarps * 32, 1)
     tensors_cluster_kernel(const __grid_constant__ TensorsParams prm,
                            const __grid_constant__ GroupScalars groups, int rows) {
   extern __shared__ uint4 kept[];  // `rows` rows for each warp
-  __shared__ BlockParts<kClusterWarps> parts;
+  __shared__ BlockParts parts;
   __shared__ BlockSums mine, all[kClusterBlocks];
   __shared__ uint64_t bar;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -1197,7 +1195,7 @@ __global__ void __launch_bounds__(kClusterWarps * 32, 1)
   // the others' shared memory may be written once all blocks have come here
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   // the tables were there before any kernel of the stream
-  const Segment opening = prm.opening[blockIdx.x * kClusterWarps + warp];
+  const Segment opening = prm.opening[blockIdx.x * kListWarps + warp];
   Target target{};
   if (OP != kOpNone && opening.tensor >= 0) target = target_of(prm.entries[opening.tensor]);
   // tensors that several blocks share (at most blocks - 1), dealt out to the warps of the cluster
@@ -1215,7 +1213,7 @@ __global__ void __launch_bounds__(kClusterWarps * 32, 1)
   const int known = join_parts<NORM>(prm, parts, mine.edge, x);
   __syncthreads();  // the edges are written
   if (warp == 0) {
-    sum = join_warps<NORM, kClusterWarps>(parts.sum);
+    sum = join_warps<NORM>(parts.sum);
     if (lane < blocks) {
       const uint32_t to = block_addr(&all[blockIdx.x], lane), at = block_addr(&bar, lane);
       send_double(to, sum, at);
@@ -1248,7 +1246,7 @@ __global__ void __launch_bounds__(kClusterWarps * 32, 1)
     join_spanning<NORM>(prm, span, [&](int b, int k) { return all[b].edge[k]; });
   if (blockIdx.x == 0) {
     if (threadIdx.x == 0) write_clip(prm, total, clip);
-    for (int i = threadIdx.x; i < prm.n_empty; i += kClusterWarps * 32)
+    for (int i = threadIdx.x; i < prm.n_empty; i += kListWarps * 32)
       write_norm<NORM>(prm, prm.empty[i], 0.0);
   }
 }

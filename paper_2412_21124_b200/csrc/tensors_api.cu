@@ -19,7 +19,7 @@ constexpr int64_t kMaxRow = int64_t{1} << 30;
 // Most elements that AdamW takes in one cluster: above, the state's traffic wants all SMs (fp32, us,
 // cluster against norm and AdamW kernel: 60k 6.6 / 7.8, 100k 7.5 / 7.5, 240k 14.1 / 8.3).
 constexpr int64_t kClusterAdamw = 96 * 1024;
-constexpr size_t kKeepBytes = size_t{kClusterWarps} * 512;  // one row of each warp of a block
+constexpr size_t kKeepBytes = size_t{kListWarps} * 512;  // one row of each warp of a block
 constexpr int64_t kMaxElements = int64_t{1} << 46;
 constexpr int64_t kMaxUnits = int64_t{1} << 30;
 enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
@@ -28,17 +28,16 @@ enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
 struct PlanHeader {
   uint64_t magic;
   int32_t n, n_scale, n_adamw, n_further, n_spanning, n_empty, scale_unit;
-  int32_t blocks, warps, rows;  // rows: of each warp
+  int32_t blocks, rows, cluster;  // rows: of each warp; cluster: the blocks make up one
   int32_t roles, n_groups;
   int64_t total;  // elements
-  bool cluster() const { return warps == kClusterWarps; }
 };
 // Offsets of the tables in the image (which the device holds as well).
 struct Image {
   size_t opening, further, spanning, shared, scale_tensor, adamw_tensor, empty, bytes;
   explicit Image(const PlanHeader& h) {
     opening = (static_cast<size_t>(h.n) * sizeof(TensorEntry) + 15) / 16 * 16;
-    further = opening + sizeof(Segment) * static_cast<size_t>(h.blocks) * h.warps;
+    further = opening + sizeof(Segment) * static_cast<size_t>(h.blocks) * kListWarps;
     spanning = further + sizeof(Segment) * static_cast<size_t>(h.n_further);
     shared = spanning + sizeof(Spanning) * static_cast<size_t>(h.n_spanning);
     scale_tensor = shared + sizeof(Shared2) * static_cast<size_t>(h.blocks);
@@ -71,18 +70,17 @@ struct WorkLayout {
 constexpr int kClusterTensors = 384;
 constexpr int64_t kRowBytes = 512;
 struct Deal {
-  int blocks, warps;
+  bool cluster;
+  int blocks;
   int64_t rows;  // of each warp
 };
 Deal deal_of(int64_t rows, int tensors) {
   Deal d;
-  const bool small = rows <= int64_t{kClusterBlocks} * kClusterWarps * kClusterRows &&
-                     tensors <= kClusterTensors;
-  d.warps = small ? kClusterWarps : kListWarps;
-  const int64_t most = static_cast<int64_t>(small ? kClusterBlocks : kListBlocks) * d.warps;
+  d.cluster = rows <= int64_t{kClusterBlocks} * kListWarps * kClusterRows && tensors <= kClusterTensors;
+  const int64_t most = static_cast<int64_t>(d.cluster ? kClusterBlocks : kListBlocks) * kListWarps;
   d.rows = std::max<int64_t>(1, (rows + most - 1) / most);
   const int64_t slots = std::max<int64_t>(1, (rows + d.rows - 1) / d.rows);
-  d.blocks = static_cast<int>((slots + d.warps - 1) / d.warps);
+  d.blocks = static_cast<int>((slots + kListWarps - 1) / kListWarps);
   return d;
 }
 // Rows of a tensor, the last one short.
@@ -268,7 +266,7 @@ bool cluster_runs() {
   if (yes) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kClusterBlocks);
-    cfg.blockDim = dim3(kClusterWarps * 32);
+    cfg.blockDim = dim3(kListWarps * 32);
     cfg.dynamicSmemBytes = kKeepBytes * kClusterRows;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -290,7 +288,7 @@ cudaError_t launch_cluster(const PlanHeader& h, const TensorsParams& prm, const 
                            cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(h.blocks);
-  cfg.blockDim = dim3(kClusterWarps * 32);
+  cfg.blockDim = dim3(kListWarps * 32);
   cfg.dynamicSmemBytes = OP == kOpNone ? 0 : kKeepBytes * h.rows;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -310,18 +308,11 @@ cudaError_t launch_cluster(const PlanHeader& h, const TensorsParams& prm, const 
              : cudaLaunchKernelEx(&cfg, tensors_cluster_kernel<kNormMax, OP>, prm, groups, rows);
 }
 
-template <int WARPS>
-cudaError_t launch_norm_blocks(int blocks, const TensorsParams& prm, cudaStream_t st) {
-  const dim3 grid(blocks), block(WARPS * 32);
-  return prm.norm_type == ABS_NORM_2
-             ? launch_pdl(tensors_norm_kernel<kNorm2, WARPS>, grid, block, st, prm)
-         : prm.norm_type == ABS_NORM_1
-             ? launch_pdl(tensors_norm_kernel<kNorm1, WARPS>, grid, block, st, prm)
-             : launch_pdl(tensors_norm_kernel<kNormMax, WARPS>, grid, block, st, prm);
-}
 cudaError_t launch_norm(const PlanHeader& h, const TensorsParams& prm, cudaStream_t st) {
-  return h.cluster() ? launch_norm_blocks<kClusterWarps>(h.blocks, prm, st)
-                     : launch_norm_blocks<kListWarps>(h.blocks, prm, st);
+  const dim3 grid(h.blocks), block(kListWarps * 32);
+  return prm.norm_type == ABS_NORM_2   ? launch_pdl(tensors_norm_kernel<kNorm2>, grid, block, st, prm)
+         : prm.norm_type == ABS_NORM_1 ? launch_pdl(tensors_norm_kernel<kNorm1>, grid, block, st, prm)
+                                       : launch_pdl(tensors_norm_kernel<kNormMax>, grid, block, st, prm);
 }
 
 // The factor of a call: from the list's own norm, or from the sum that it is given.
@@ -357,7 +348,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   h.scale_unit = scale_unit_for(total);
   const Deal deal = deal_of(total_rows, nonempty);
   h.blocks = deal.blocks;
-  h.warps = deal.warps;
+  h.cluster = deal.cluster;
   h.rows = static_cast<int32_t>(deal.rows);
   std::vector<TensorEntry> entries(n);
   std::vector<int32_t> scale_tensor, adamw_tensor;
@@ -457,7 +448,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   Segment idle;
   std::memset(&idle, 0, sizeof idle);
   idle.tensor = -1;
-  std::vector<Segment> opening(static_cast<size_t>(deal.blocks) * deal.warps, idle), further;
+  std::vector<Segment> opening(static_cast<size_t>(deal.blocks) * kListWarps, idle), further;
   std::vector<Spanning> spanning;
   std::vector<int32_t> empty;
   int64_t slot = -1, left = 0;  // the warp that is dealt to, and the rows that it still takes
@@ -503,7 +494,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
         ++opening[slot].more;
         further.push_back(s);
       }
-      const int64_t block = slot / deal.warps;
+      const int64_t block = slot / kListWarps;
       if (!start) first_block = block;
       if (end == e.numel && block != first_block)
         spanning.push_back({t, static_cast<int32_t>(first_block), static_cast<int32_t>(block), 0});
@@ -568,7 +559,6 @@ size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n) {
   h.n_scale = static_cast<int32_t>(scale);
   h.n_adamw = static_cast<int32_t>(adamw);
   h.blocks = deal.blocks;
-  h.warps = deal.warps;
   h.n_spanning = std::min(n, deal.blocks);
   return sizeof h + Image(h).bytes;
 }
@@ -617,7 +607,7 @@ int abs_grad_norm(const void* plan, void* work, int norm_type, double grad_scale
   if (!norms_out) return ABS_ERR_NULL;
   const PlanHeader& h = *plan_of(plan);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = h.cluster() && cluster_runs()
+  const cudaError_t e = h.cluster && cluster_runs()
                             ? launch_cluster<kOpNone>(h, prm, GroupScalars{}, st)
                             : launch_norm(h, prm, st);
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
@@ -634,7 +624,7 @@ int abs_grad_clip(const void* plan, void* work, int norm_type, double grad_scale
   if (prm.in_place && (h.roles & kGradsOverlap)) return ABS_ERR_ALIAS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (!sum_in && h.cluster() && cluster_runs()) {
+  if (!sum_in && h.cluster && cluster_runs()) {
     e = launch_cluster<kOpScale>(h, prm, GroupScalars{}, st);
   } else {
     e = launch_norm_or_clip(h, prm, st);
@@ -665,7 +655,7 @@ int abs_grad_adamw(const void* plan, void* work, const abs_adamw_hparams* hparam
   }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (clipped && !sum_in && h->cluster() && h->total <= kClusterAdamw && cluster_runs()) {
+  if (clipped && !sum_in && h->cluster && h->total <= kClusterAdamw && cluster_runs()) {
     e = launch_cluster<kOpAdamw>(*h, prm, groups, st);
   } else {
     e = clipped ? launch_norm_or_clip(*h, prm, st) : cudaSuccess;
