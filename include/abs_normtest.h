@@ -500,6 +500,7 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  * of the caller) that the plan is uploaded to; then each call is one or two launches.  Both hold
  * the addresses of the tensors, which must stay where they are while the plan is in use.  One
  * work area serves one call at a time: calls on it have to be ordered (one stream, or events).
+ * Make the first call on a device outside of any stream capture; later ones may be captured.
  *
  * Range and accuracy: sums are held in fp64 (fp32 within 16 bytes of input); the norm of finite
  * gradients is right also where their fp32 squares overflow or vanish.  Results do not depend on

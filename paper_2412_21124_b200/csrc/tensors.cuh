@@ -269,12 +269,13 @@ __device__ __forceinline__ uint4 ld_grad_16(const void* p) {
 }
 
 // One lane's share of a segment.  KEEP: its rows are also left in shared memory, at `keep` (this
-// lane's place in row 0), one after the other.
-template <typename T, int NORM, bool KEEP>
+// lane's place in row 0), one after the other.  SMALL: fewer loads at once, for lists of a few rows a
+// warp, where fetching the instructions of a larger body is what shows (60k elements: 3.5 -> 3.4 us).
+template <typename T, int NORM, bool KEEP, bool SMALL>
 __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, const Segment& s,
                                                      uint32_t lane, uint4* keep) {
   using S = typename T::scalar;
-  constexpr int kBatch = 8;
+  constexpr int kBatch = SMALL ? 4 : 8;
   NormAcc<NORM> acc;
   auto one = [&](S raw) {
     const float x = T::to_float(raw);
@@ -321,7 +322,7 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
       }
       return acc;
     }
-    constexpr int kWalk = 16;
+    constexpr int kWalk = SMALL ? 8 : 16;
     Walk<int32_t> w = grad_walk<int32_t>(e, s.start + lane, 32);
     g += w.base;
     const auto batch = [&](uint32_t i0, auto whole) {
@@ -368,13 +369,13 @@ __device__ __forceinline__ double segment_acc_wide(const TensorsParams& prm, con
 }
 
 // The sum of a segment, in every lane of its warp.
-template <int NORM, bool KEEP>
+template <int NORM, bool KEEP, bool SMALL>
 __device__ __forceinline__ double segment_sum(const TensorsParams& prm, const Segment& s,
                                               uint32_t lane, uint4* keep) {
   double x = 0.0;
   with_type(s.dtype, [&](auto type) {
     using T = decltype(type);
-    const NormAcc<NORM> acc = segment_acc<T, NORM, KEEP>(prm, s, lane, keep);
+    const NormAcc<NORM> acc = segment_acc<T, NORM, KEEP, SMALL>(prm, s, lane, keep);
     x = warp_join<NORM>(NORM == kNormMax ? static_cast<double>(acc.mx) : acc.s);
     if constexpr (NORM != kNormMax) {
       // fp32 squares overflow above 1.8e19 and lose bits below 1e-19; sums of |x| overflow
@@ -441,7 +442,7 @@ __device__ __forceinline__ uint32_t kept_rows(const Segment& s) {
 }
 
 // One warp's rows; returns their sum.
-template <int NORM, bool KEEP>
+template <int NORM, bool KEEP, bool SMALL>
 __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segment& opening,
                                            BlockParts& parts, uint4* keep) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -453,7 +454,7 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
     for (int k = 0;; ++k) {
       Segment next = s;
       if (k < opening.more) next = prm.further[opening.next + k];
-      const double y = segment_sum<NORM, KEEP>(prm, s, lane, keep);
+      const double y = segment_sum<NORM, KEEP, SMALL>(prm, s, lane, keep);
       if (KEEP) keep += kept_rows(s) * 32;
       sum = norm_join<NORM>(sum, y);
       x = norm_join<NORM>(x, y);
@@ -542,9 +543,16 @@ __device__ __forceinline__ bool last_of(unsigned int* ticket, unsigned int of) {
   return __shfl_sync(0xffffffffu, before, 0) == of - 1;
 }
 
-// Every warp sums its rows, every block its warps; the block that finishes last joins the blocks,
-// and of the blocks that share a tensor the last one joins that tensor: one launch, and no order of
-// finishing shows in a sum.
+// sum |x|^p (or max |x|) of each tensor and of the list.  Every warp sums its rows, every block its
+// warps; the block that finishes last joins the blocks, and of the blocks that share a tensor the last
+// one joins that tensor: one launch, and no order of finishing shows in a sum.
+//
+// Bound by reading the gradients once.  Each warp reads one run of the list, eight 16-byte loads per
+// lane at a time, and meets another warp only at the end, so that the tensors' boundaries cost
+// nothing on the way: 1.24G bf16 (2.47 GB) 355 us = 7.0 TB/s, 124M fp32 (498 MB) 76 us = 6.5 TB/s, against
+// 405 and 79.5 us with one CTA per 32768 elements of a tensor and a ticket each.  16 warps a block:
+// 32 of half the registers take 358 and 78.4 us.  Below 50 MB what shows is the chain launch, table,
+// data, join, ticket, join: 4.9 us for an empty list.
 template <int NORM>
 __global__ void __launch_bounds__(kListWarps * 32, 1)
     tensors_norm_kernel(const __grid_constant__ TensorsParams prm) {
@@ -555,7 +563,7 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
   Shared2 shared{-1, -1};
   if (warp == 1 || warp == 2) shared = prm.shared[blockIdx.x];
   grid_dependency_wait();
-  double sum = warp_sum<NORM, false>(prm, opening, parts, nullptr);
+  double sum = warp_sum<NORM, false, false>(prm, opening, parts, nullptr);
   if (lane == 0) parts.sum[warp] = sum;
   grid_launch_dependents();
   __syncthreads();
@@ -848,9 +856,15 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
   }
 }
 
-// One CTA per unit, the last unit of the list first.  After this call's norm kernel the first loads
-// are made before the factor is waited for: that kernel lets this one start only after its own wait,
-// so whatever wrote the tensors before is done.
+// y = factor * x, rounded once to y's type.  Bound by reading x again and writing y: a list that is
+// larger than what stays on chip is read twice, since the factor needs the whole norm.  One CTA per
+// unit, the last unit of the list first.  After this call's norm kernel the first loads are made before
+// the factor is waited for: that kernel lets this one start only after its own wait, so whatever wrote
+// the tensors before is done.
+// Norm and scaling of 124M bf16 into bf16: 121 us = 6.2 TB/s of the 747 MB that they move; 1.24G fp32
+// into bf16: 1.84 ms = 6.7 TB/s of 12.4 GB.  Measured and dropped: one cooperative kernel in which each
+// warp scales what it read itself, with its last rows kept in shared memory (167 us and 2.5 ms: the
+// reads and writes of thousands of warps lie too far apart).
 __global__ void __launch_bounds__(kTensorThreads, 3)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
   const int u = prm.n_scale - 1 - blockIdx.x;
@@ -937,9 +951,11 @@ __device__ __forceinline__ void adamw_walk(const AdamScalars& a, const StateArra
   }
 }
 
-// One CTA per unit, the last unit of the list first.  After this call's norm kernel the first loads
-// are made before the factor is waited for: that kernel lets this one start only after its own wait,
-// so whatever wrote the tensors before is done.
+// AdamW on factor * g (adamw_elem), the gradient read and never written.  Bound by its traffic: g once,
+// p, m and v read and written, the bf16 copy.  Units and early loads as in the scaling kernel; units of
+// 4096 elements (two vectors of 8 per thread) so that CTAs of 115 KB each fill the last wave: 1.24G bf16
+// gradients with the copy 5.48 ms after the norm = 6.8 TB/s of the 37.1 GB that both move (2048: 5.53,
+// 8192: 5.52, 32768: 5.68 ms); 124M 564 us; 1200 adapters of 24M fp32 together 124 us.
 __global__ void __launch_bounds__(kTensorThreads, 4)
     tensors_adamw_kernel(const __grid_constant__ TensorsParams prm,
                          const __grid_constant__ GroupScalars groups, int clipped) {
@@ -1175,6 +1191,10 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
   }
 }
 
+// Bound by a chain of latencies: launch, table (read before the predecessor's
+// end is waited for), rows, join, one store into the other blocks, the factor, the second
+// pass out of shared memory.  20 tensors of 60k fp32 together: norm 3.4 us, clip 4.9, AdamW 6.4; with
+// the kernels above 5.0, 7.6 and 7.8.
 template <int NORM, int OP>
 __global__ void __launch_bounds__(kListWarps * 32, 1)
     tensors_cluster_kernel(const __grid_constant__ TensorsParams prm,
@@ -1206,7 +1226,7 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
   __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   grid_dependency_wait();
-  double sum = warp_sum<NORM, OP != kOpNone>(prm, opening, parts, keep);
+  double sum = warp_sum<NORM, OP != kOpNone, true>(prm, opening, parts, keep);
   if (lane == 0) parts.sum[warp] = sum;
   __syncthreads();
   double x;
