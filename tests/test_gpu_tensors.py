@@ -68,16 +68,19 @@ def check_scaled(got, x, factor, dtype):
     assert ((got.double() - ref).abs() <= tol).all()
 
 
-SHAPES = [(1,), (0,), (7,), (64, 48), (33, 129), (1000,), (300, 257), (5, 1), (1, 4096), (40_009,)]
+SHAPES = [(1,), (0,), (7,), (64, 50), (33, 129), (1000,), (300, 257), (5, 1), (1, 4096), (40_009,)]
+# beside them: nothing (the list fits one cluster), or a tensor that makes it one for all SMs
+MORE = ([], [(1500, 1100)])
 LAYOUTS = ("dense", "odd", "columns", "columns_odd", "swapped")
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
 @pytest.mark.parametrize("order", ORDERS)
-def test_norm(order, dtype, layout):
+@pytest.mark.parametrize("more", MORE)
+def test_norm(more, order, dtype, layout):
     g = gen(1)
-    grads = [make(s, dtype, layout, g, 0.01 * (i + 1)) for i, s in enumerate(SHAPES)]
+    grads = [make(s, dtype, layout, g, 0.01 * (i + 1)) for i, s in enumerate(SHAPES + more)]
     ts = absnt.GradTensors(grads)
     for scale in (1.0, 0.125, -3.0):  # the same object, called again
         absnt.abs_grad_norm(ts, norm_type=order, grad_scale=scale)
@@ -117,9 +120,10 @@ def test_types_mixed_in_one_list():
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
 @pytest.mark.parametrize("order", ORDERS)
-def test_clip_in_place(order, dtype, layout):
+@pytest.mark.parametrize("more", MORE)
+def test_clip_in_place(more, order, dtype, layout):
     g = gen(5)
-    grads = [make(s, dtype, layout, g, 0.1) for s in SHAPES]
+    grads = [make(s, dtype, layout, g, 0.1) for s in SHAPES + more]
     before = [x.clone() for x in grads]
     total, _ = ref_norms(grads, order, 1.0)
     total = float(total)
@@ -141,9 +145,10 @@ def test_clip_in_place(order, dtype, layout):
                                      ("columns", "dense"), ("dense", "columns"),
                                      ("columns_odd", "columns"), ("swapped", "swapped"),
                                      ("dense", "swapped"), ("swapped", "columns")])
-def test_clip_into(layouts, dtype, out_dtype):
+@pytest.mark.parametrize("more", MORE)
+def test_clip_into(more, layouts, dtype, out_dtype):
     g = gen(6)
-    shapes = SHAPES + [(600, 520)]
+    shapes = SHAPES + [(600, 520)] + more
     grads = [make(s, dtype, layouts[0], g, 0.1) for s in shapes]
     outs = [make(s, out_dtype, layouts[1], g) for s in shapes]
     before = [x.clone() for x in grads]
@@ -298,9 +303,10 @@ def state_like(shapes, g, layout="dense"):
                                      ("columns", "swapped")])
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
 @pytest.mark.parametrize("clip", (True, False))
-def test_adamw(clip, dtype, layouts):
+@pytest.mark.parametrize("shapes", (SHAPES[:6] + SHAPES[7:9], SHAPES, SHAPES + [(1500, 1100)]))
+def test_adamw(shapes, clip, dtype, layouts):
+    """Lists whose update is part of the cluster kernel, whose norm is, and for all SMs."""
     g = gen(8)
-    shapes = SHAPES + [(600, 520)]
     grads = [make(s, dtype, layouts[0], g, 0.1) for s in shapes]
     p, m, v = state_like(shapes, g, layouts[1])
     p16 = [make(s, BF16, layouts[1], g) for s in shapes]
@@ -313,8 +319,8 @@ def test_adamw(clip, dtype, layouts):
     factor = 0.5
     if clip:
         total = check_norms(ts, grads, 2, 0.5)
-        factor *= min(1.0, 1.0 / (total + 1e-6))
-        assert factor < 0.4
+        factor *= 1.0 / (total + 1e-6)
+        assert total > 2.0
     for i, k in enumerate(groups):
         p0, m0, v0, g0 = (b[i].double() for b in before)
         w, m1, v1, e_p, e_m, e_v = adamw_ref(p0, m0, v0, g0 * factor, hps[k], step)
@@ -386,11 +392,12 @@ def test_empty_lists():
 @pytest.mark.parametrize("bad", (math.nan, math.inf, -math.inf))
 @pytest.mark.parametrize("order", ORDERS)
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
-def test_not_finite(dtype, order, bad):
+@pytest.mark.parametrize("more", MORE)
+def test_not_finite(more, dtype, order, bad):
     """One such value: the flag is raised, nothing is clipped, AdamW leaves its state alone; the next
     call on mended gradients is an ordinary one."""
     g = gen(11)
-    shapes = [(1000,), (70_001,), (30, 30)]
+    shapes = [(1000,), (70_001,), (30, 30)] + more
     grads = [make(s, dtype, "dense", g) for s in shapes]
     p, m, v = state_like(shapes, g)
     before = [[x.clone() for x in t] for t in (grads, p, m, v)]
@@ -461,9 +468,10 @@ def test_sum_for_the_flat_calls():
     assert ((p.double() - w).abs() <= 2 * e_p).all()
 
 
-def test_other_streams_and_graphs():
+@pytest.mark.parametrize("more", MORE)
+def test_other_streams_and_graphs(more):
     g = gen(15)
-    shapes = [(100, 100), (33_333,)]
+    shapes = [(100, 100), (33_333,)] + more
     grads = [make(s, BF16, "dense", g, 0.1) for s in shapes]
     p, m, v = state_like(shapes, g)
     q = [[x.clone() for x in t] for t in (p, m, v)]
