@@ -491,7 +491,7 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  * "Gradient clipping 1.0" in the hyper-parameter tables of Appendix C).
  *
  *   x_t,i        element i of tensor t, and s = grad_scale, a factor known before the call
- *                (1/micro-batches, 1/loss scale; finite, not 0)
+ *                (1/micro-batches, 1/loss scale; a float, not 0)
  *   N_t          the norm of s*x_t:  (sum_i |s x_t,i|^p)^(1/p) for p = 1, 2, or max_i |s x_t,i|
  *   N            the same norm over all tensors, (sum_t N_t^p)^(1/p) or max_t N_t
  *   c            min(1, max_norm / (N + 1e-6)), the clipping coefficient
@@ -504,7 +504,8 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  *
  * Range and accuracy: sums are held in fp64 (fp32 within 16 bytes of input); the norm of finite
  * gradients is right also where their fp32 squares overflow or vanish.  Results do not depend on
- * the order in which blocks run.  A norm that is not finite (a NaN or infinite gradient) raises
+ * the order in which blocks run.  s c is rounded to float once (below 2^-126, for norms above 1e38
+ * max_norm, with fewer bits).  A norm that is not finite (a NaN or infinite gradient) raises
  * ABS_FLAG_NONFINITE in the header; c is then 1 and AdamW leaves params, m and v as they are.
  */
 typedef struct {

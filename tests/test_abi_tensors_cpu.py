@@ -177,7 +177,7 @@ def test_launching_calls_refuse(L):
         assert call(norms=work + 16) == B.ABS_ERR_ALIAS
         for kind in (-1, 3):
             assert call(kind=kind) == B.ABS_ERR_RANGE
-        for scale in (0.0, nan, inf):
+        for scale in (0.0, nan, inf, 1e39, -1e300):
             assert call(scale=scale) == B.ABS_ERR_RANGE
         for max_norm in (-1.0, nan, inf):
             assert call(max_norm=max_norm) == B.ABS_ERR_RANGE

@@ -348,11 +348,12 @@ def test_adamw_is_the_flat_call():
 @pytest.mark.parametrize("dtype", (F32, BF16))
 @pytest.mark.parametrize("order", (2, 1))
 @pytest.mark.parametrize("size", (1e-42, 1e-30, 1e-21, 1e25, 1e37))
-def test_range(size, order, dtype):
+@pytest.mark.parametrize("more", ([], [(1_700_000,)]))
+def test_range(more, size, order, dtype):
     """Squares and sums that leave the range of fp32: the norm is still that of the values."""
     g = gen(10)
     grads = [(torch.randn(s, device=DEV, generator=g).clamp(-3, 3) * size).to(dtype)
-             for s in ((5,), (300, 70), (50_000,))]
+             for s in [(5,), (300, 70), (50_000,)] + more]
     grads.append(torch.randn(1000, device=DEV, generator=g))  # one of ordinary size
     ts = absnt.GradTensors(grads)
     absnt.abs_grad_norm(ts, norm_type=order, max_norm=1.0)
@@ -496,6 +497,45 @@ def test_other_streams_and_graphs(more):
     absnt.abs_grad_clip(rs, 1.0)
     for a, b in zip((p, m, v, grads), (*q, then)):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("columns", (1, 2))
+@pytest.mark.parametrize("more", ([], [(2_000_000,)]))
+def test_far_apart_rows(more, columns):
+    """Views whose rows lie so far apart that offsets within one unit pass 31 bits."""
+    g = gen(20)
+    rows, pitch = 40_000, 70_000
+    parent = torch.zeros(rows, pitch, device=DEV, dtype=BF16)
+    target = torch.zeros(rows, pitch, device=DEV, dtype=BF16)
+    at = slice(pitch - 7, pitch - 7 + columns)
+    view = parent[:, at]
+    view.copy_(torch.randn(rows, columns, device=DEV, generator=g))
+    rest = [make(s, F32, "dense", g, 0.01) for s in more]
+    before = [x.clone() for x in [view] + rest]
+    p, m, v = state_like([x.shape for x in before], g)
+    st = [[x.clone() for x in t] for t in (p, m, v)]
+    ts = absnt.GradTensors([view] + rest, out=[target[:, at]] + [torch.empty_like(x) for x in rest],
+                           params=p, m=m, v=v)
+    for order in ORDERS:
+        absnt.abs_grad_norm(ts, norm_type=order)
+        check_norms(ts, before, order)
+    for sums in (None, ts.header):
+        absnt.abs_grad_norm(ts)
+        absnt.abs_grad_clip(ts, 1.0, sum_in=sums)
+        total = check_norms(ts, before, 2)
+        check_scaled(target[:, at], before[0], 1.0 / (total + 1e-6), BF16)
+        assert int(torch.count_nonzero(target)) == int(torch.count_nonzero(target[:, at]))
+        target.zero_()
+    absnt.abs_grad_adamw(ts, HP, 3, 1.0)
+    w, m1, v1, e_p, e_m, e_v = adamw_ref(*(t[0].double() for t in st),
+                                         before[0].double() / (total + 1e-6), HP, 3)
+    for got, ref, tol in zip((p[0], m[0], v[0]), (w, m1, v1), (e_p, e_m, e_v)):
+        assert ((got.double() - ref).abs() <= tol).all()
+    del target
+    ts = absnt.GradTensors([view] + rest)  # in place
+    absnt.abs_grad_clip(ts, 1.0)
+    check_scaled(view, before[0], 1.0 / (total + 1e-6), BF16)
+    assert int(torch.count_nonzero(parent)) == int(torch.count_nonzero(view))
 
 
 def test_beyond_32_bits():
