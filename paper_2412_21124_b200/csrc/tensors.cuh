@@ -92,7 +92,7 @@ struct TensorsParams {
   double* block_sum;        // blocks
   double* edge_sum;         // 2 * blocks: a block's parts of the tensors it shares
   float* norms_out;         // 2 + n
-  int n, n_scale, n_adamw, n_spanning, n_empty;
+  int n_scale, n_adamw, n_spanning, n_empty;
   int scale_unit;  // elements of a unit for scaling
   int norm_type;
   double scale, max_norm;
@@ -600,8 +600,7 @@ __global__ void tensors_clip_kernel(const __grid_constant__ TensorsParams prm) {
 }
 
 // ---- scaling -------------------------------------------------------------------------
-// Values of a type known at run time.  A list mixes types, and nine loops for the pairs of them take
-// more registers than one loop with uniform branches takes time.
+// Values of a type known at run time: where there are few of them, or any pair of types may meet.
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int dtype) {
   if (dtype == ABS_F32) return static_cast<const float*>(p)[i];
   const uint16_t x = static_cast<const uint16_t*>(p)[i];
@@ -613,7 +612,8 @@ __device__ __forceinline__ void store_any(void* p, int64_t i, int dtype, float x
   else
     static_cast<uint16_t*>(p)[i] = dtype == ABS_BF16 ? TBF16::from_float(x) : TF16::from_float(x);
 }
-// The 4 (fp32) or 8 values of 16 bytes of input, scaled, to an output whose groups of 8 are aligned.
+// The 4 (fp32) or 8 values of 16 bytes of input, scaled, to an output that is aligned for 16-byte stores
+// (8-byte ones from fp32 to 16 bits).
 __device__ __forceinline__ void store_scaled(const uint4& raw, int in, void* p, int64_t i, int out,
                                              float factor) {
   float x[8] = {};
