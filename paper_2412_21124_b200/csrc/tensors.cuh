@@ -563,9 +563,9 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
   Shared2 shared{-1, -1};
   if (warp == 1 || warp == 2) shared = prm.shared[blockIdx.x];
   grid_dependency_wait();
+  grid_launch_dependents();  // see tensors_scale_kernel
   double sum = warp_sum<NORM, false, false>(prm, opening, parts, nullptr);
   if (lane == 0) parts.sum[warp] = sum;
-  grid_launch_dependents();
   __syncthreads();
   double x;
   const int known = join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x, x);
@@ -860,12 +860,14 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
 // larger than what stays on chip is read twice, since the factor needs the whole norm.  One CTA per
 // unit, the last unit of the list first.  After this call's norm kernel the first loads are made before
 // the factor is waited for: that kernel lets this one start only after its own wait, so whatever wrote
-// the tensors before is done.
+// the tensors before is done.  At 64 registers one CTA fits beside a block of the norm kernel and has
+// its loads under way when that ends (4M bf16 11.3 -> 10.5 us, 50M fp16 34.8 -> 33.4; three CTAs of 80
+// registers are 1% faster beyond 100M).
 // Norm and scaling of 124M bf16 into bf16: 121 us = 6.2 TB/s of the 747 MB that they move; 1.24G fp32
 // into bf16: 1.84 ms = 6.7 TB/s of 12.4 GB.  Measured and dropped: one cooperative kernel in which each
 // warp scales what it read itself, with its last rows kept in shared memory (167 us and 2.5 ms: the
 // reads and writes of thousands of warps lie too far apart).
-__global__ void __launch_bounds__(kTensorThreads, 3)
+__global__ void __launch_bounds__(kTensorThreads, 4)
     tensors_scale_kernel(const __grid_constant__ TensorsParams prm) {
   const int u = prm.n_scale - 1 - blockIdx.x;
   const TensorEntry& e = prm.entries[prm.scale_tensor[u]];
