@@ -50,6 +50,7 @@ enum {
   kEntryStateVec = 8,   // state and bf16 copy reach a boundary together, after adamw_head
   kEntryVecScale = 16,  // 16 bytes of the gradient (after g_head) meet an aligned place in the output
   kEntryVecAdamw = 32,  // and in state and bf16 copy
+  kEntryRuns = 64,      // the gradient's rows are runs of 16 elements or more, none of them far
 };
 
 // A run of elements of one tensor, the work of one warp: [start, start + n), `head` of them before
@@ -896,6 +897,45 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
   });
 }
 
+// Eight values of a view whose rows are runs, from the place of a walk by vectors of 8: the aligned
+// 16-byte pieces that hold them, or one by one where they reach into the next row or a piece would
+// reach out of the view, [lo, hi).  (A piece may hold what lies between two rows.)
+template <typename T>
+struct Gathered8 {
+  Shifted8<T> v;
+  uint32_t o;  // as for Shifted8, or 0
+};
+template <typename T>
+__device__ __forceinline__ Gathered8<T> gather8(const typename T::scalar* p, uint32_t col, uint32_t row,
+                                                int32_t gap, const typename T::scalar* lo,
+                                                const typename T::scalar* hi) {
+  using S = typename T::scalar;
+  constexpr int kPieces = 8 / T::kVec;
+  Gathered8<T> x;
+  x.o = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 15u;
+  const S* c = p - x.o / sizeof(S);
+  if (col + 8 <= row && c >= lo && c + T::kVec * (kPieces + 1) <= hi) {
+#pragma unroll
+    for (int i = 0; i < kPieces + 1; ++i) x.v.r[i] = reinterpret_cast<const uint4*>(c)[i];
+  } else {
+    x.o = 0;
+    uint32_t w[4 * kPieces];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const S b = p[k + (col + k >= row ? gap : 0)];
+      if constexpr (T::kVec == 4)
+        w[k] = __float_as_uint(b);
+      else
+        w[k / 2] = k % 2 ? w[k / 2] | static_cast<uint32_t>(b) << 16 : b;
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+      x.v.r[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    x.v.r[kPieces] = make_uint4(0, 0, 0, 0);
+  }
+  return x;
+}
+
 // ---- AdamW ---------------------------------------------------------------------------
 // Four neighbouring coordinates.
 __device__ __forceinline__ void adamw_quad(const AdamScalars& a, float2 g0, float2 g1, float4& w,
@@ -958,6 +998,10 @@ __device__ __forceinline__ void adamw_walk(const AdamScalars& a, const StateArra
 // 4096 elements (two vectors of 8 per thread) so that CTAs of 115 KB each fill the last wave: 1.24G bf16
 // gradients with the copy 5.48 ms after the norm = 6.8 TB/s of the 37.1 GB that both move (2048: 5.53,
 // 8192: 5.52, 32768: 5.68 ms); 124M 564 us; 1200 adapters of 24M fp32 together 124 us.
+// Gradients that are views take vectors of 8 of the state as well, if their rows are runs of 16 or more
+// (24M fp16 in rows of 333, norm and update: 131 us element by element, 120 so; fp32 137 and 130; rows
+// of 16, in the order of the tested alignments, fp16 146 / 133 and 139 / 122, fp32 157 / 144 and
+// 163 / 137; rows of 8 hardly ever hold a whole vector).
 __global__ void __launch_bounds__(kTensorThreads, 4)
     tensors_adamw_kernel(const __grid_constant__ TensorsParams prm,
                          const __grid_constant__ GroupScalars groups, int clipped) {
@@ -982,13 +1026,15 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
       }
       return factor != factor;
     };
-    if ((e.flags & kEntryRowsG) || !(e.flags & kEntryStateVec)) {
+    const bool runs = e.flags & kEntryRuns;
+    if (((e.flags & kEntryRowsG) && !runs) || !(e.flags & kEntryStateVec)) {
       if (!skip()) adamw_walk<T>(a, state, e, r.start, tid, r.n, kTensorThreads, factor);
       return;
     }
     const S *lo = static_cast<const S*>(e.g), *hi = lo + e.numel, *g = lo + r.start;
     float *p = e.p + r.start, *m = e.m + r.start, *v = e.v + r.start;
-    const Run run = make_run(g, r.n, r.start ? 0u : min(uint32_t{e.adamw_head}, r.n), lo, hi);
+    const uint32_t head = r.start ? 0u : min(uint32_t{e.adamw_head}, r.n);
+    const Run run = runs ? Run{head, (r.n - head) / 8, 0} : make_run(g, r.n, head, lo, hi);
     const auto update = [&](uint32_t i, const float* x, Float8& w, Float8& mm, Float8& vv) {
       const float2 g0 = make_float2(factor * x[0], factor * x[1]);
       const float2 g1 = make_float2(factor * x[2], factor * x[3]);
@@ -1001,7 +1047,21 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
       st_stream_32(v + i, vv.lo, vv.hi);
       if (e.p16) st_bf16x8(e.p16 + r.start + i, w.lo, w.hi);
     };
-    if (run.o == 0) {
+    if (runs) {
+      const S* end = lo + (e.numel / e.g_row - 1) * e.g_stride + e.g_row;
+      const int32_t gap = static_cast<int32_t>(e.g_stride - e.g_row);
+      Walk<int32_t> wg = grad_walk<int32_t>(e, r.start + head + tid * 8, 8 * kTensorThreads);
+      const S* from = lo + wg.base;
+      for (uint32_t q = tid; q < run.nv; q += kTensorThreads, wg.next()) {
+        const uint32_t i = run.head + q * 8;
+        const Gathered8<T> raw = gather8<T>(from + wg.at, wg.col, wg.row, gap, lo, end);
+        Float8 w = ld_state_32(p + i), mm = ld_state_32(m + i), vv = ld_state_32(v + i);
+        if (skip()) return;
+        float x[8];
+        unpack_shifted8<T>(raw.v, raw.o, x);
+        update(i, x, w, mm, vv);
+      }
+    } else if (run.o == 0) {
       for (uint32_t q = tid; q < run.nv; q += kTensorThreads) {
         const uint32_t i = run.head + q * 8;
         const Vec8<T> raw = load8<T>(g + i);
@@ -1026,8 +1086,12 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
     const uint32_t rest = run.head + run.nv * 8 + tid;
     if (tid < run.head || rest < r.n) {
       if (skip()) return;
-      if (tid < run.head) adamw_one(a, state, r.start + tid, factor * T::to_float(g[tid]));
-      if (rest < r.n) adamw_one(a, state, r.start + rest, factor * T::to_float(g[rest]));
+      const auto one = [&](uint32_t k) {
+        const S* at = runs ? lo + grad_walk<int64_t>(e, r.start + k, 1).base : g + k;
+        adamw_one(a, state, r.start + k, factor * T::to_float(*at));
+      };
+      if (tid < run.head) one(tid);
+      if (rest < r.n) one(rest);
     }
   });
 }

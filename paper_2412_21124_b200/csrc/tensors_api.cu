@@ -413,6 +413,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
     e.g_head = static_cast<uint8_t>(head_of(g, 16));
     const int64_t longest = std::max<int64_t>(h.scale_unit, deal.rows * (kRowBytes / 2));
     if (rows_g && spans_far(g, longest)) e.flags |= kEntryFar;
+    if (rows_g && g.col == 1 && g.row >= 16 && !(e.flags & kEntryFar)) e.flags |= kEntryRuns;
     const View& y = outs ? out : g;
     e.scale_head = static_cast<uint8_t>(head_of(y, 8 * y.esz));
     if (!rows_g && aligned_at(y, e.g_head, std::min<size_t>(16, per * y.esz)))

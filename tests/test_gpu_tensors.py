@@ -331,6 +331,32 @@ def test_adamw(shapes, clip, dtype, layouts):
         assert torch.equal(grads[i], before[3][i])
 
 
+@pytest.mark.parametrize("width", (1, 15, 16, 17, 24, 31, 64, 100, 513, 4100))
+@pytest.mark.parametrize("dtype", (F32, BF16, F16))
+@pytest.mark.parametrize("layout", ("dense", "odd"))
+def test_adamw_rows_of_every_width(width, dtype, layout):
+    """Column slices at every distance from a boundary, the first and last columns among them; what
+    lies between their rows is NaN."""
+    g = gen(width)
+    rows, grads = 40_000 // width, []
+    for gap in (1, 3, 8, 16):
+        for at in (0, gap):
+            parent = torch.full((rows, width + gap), math.nan, device=DEV, dtype=dtype)
+            grads.append(parent[:, at:at + width])
+            grads[-1].copy_(torch.randn(rows, width, device=DEV, generator=g) * 0.1)
+    p, m, v = state_like([x.shape for x in grads], g, layout)
+    half = [torch.empty(x.shape, device=DEV, dtype=BF16) for x in grads]
+    ref = [[x.double() for x in t] for t in (p, m, v)]
+    each = [adamw_ref(*z, x.double(), HP, 5) for *z, x in zip(*ref, grads)]
+    ts = absnt.GradTensors(grads, params=p, m=m, v=v, params_bf16=half)
+    absnt.abs_grad_adamw(ts, HP, 5)
+    for (rp, rm, rv, e_p, e_m, e_v), x, y, z, h in zip(each, p, m, v, half):
+        assert ((x.double() - rp).abs() <= e_p).all()
+        assert ((y.double() - rm).abs() <= e_m).all()
+        assert ((z.double() - rv).abs() <= e_v).all()
+        assert torch.equal(h, x.to(BF16))
+
+
 def test_adamw_is_the_flat_call():
     """On one dense fp32 tensor, without clipping: the update of abs_adamw_step, bit for bit."""
     g = gen(9)
