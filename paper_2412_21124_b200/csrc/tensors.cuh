@@ -863,9 +863,9 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
 // larger than what stays on chip is read twice, since the factor needs the whole norm.  One CTA per
 // unit, the last unit of the list first.  After this call's norm kernel the first loads are made before
 // the factor is waited for: that kernel lets this one start only after its own wait, so whatever wrote
-// the tensors before is done.  At 64 registers one CTA fits beside a block of the norm kernel and has
-// its loads under way when that ends (4M bf16 11.3 -> 10.5 us, 50M fp16 34.8 -> 33.4; three CTAs of 80
-// registers are 1% faster beyond 100M).
+// the tensors before is done.  Four CTAs of 64 registers to an SM, against three of 80, norm and scaling
+// (us): 4M bf16 9.7 / 10.6, 16M fp16 16 / 18, 50M fp16 48.1 / 49.0, 300M bf16 279.5 / 279.0, 1.24G fp32
+// into bf16 1832 / 1818.
 // Norm and scaling of 124M bf16 into bf16: 121 us = 6.2 TB/s of the 747 MB that they move; 1.24G fp32
 // into bf16: 1.84 ms = 6.7 TB/s of 12.4 GB.  Measured and dropped: one cooperative kernel in which each
 // warp scales what it read itself, with its last rows kept in shared memory (167 us and 2.5 ms: the
