@@ -213,6 +213,18 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
+def _stream_object(stream, device):
+    """What _stream gives the number of, as torch's stream.  0 is the default stream, but
+    torch.cuda.ExternalStream takes it for no number at all and hands out a stream of its pool."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    if int(stream) == 0:
+        return torch.cuda.default_stream(device)
+    return torch.cuda.ExternalStream(int(stream))
+
+
 def _grad_table(grads):
     K = len(grads)
     if K < 1:
@@ -736,7 +748,7 @@ class GradTensors:
         else:
             raw = _stream(stream).value or 0
         if raw != self._uploaded_on and not torch.cuda.is_current_stream_capturing():
-            other = torch.cuda.ExternalStream(raw)
+            other = _stream_object(stream, self._device)
             other.wait_event(self._uploaded)
             self._work.record_stream(other)
             self._results.record_stream(other)

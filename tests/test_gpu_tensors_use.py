@@ -157,3 +157,24 @@ def test_from_c(tmp_path):
     np.testing.assert_allclose(got[1], coef, rtol=7e-7)
     np.testing.assert_allclose(got[2:5], each, rtol=6e-7)
     np.testing.assert_allclose(got[5:], 0.5 * coef * x, rtol=8e-7)
+
+
+def test_built_on_a_side_stream(monkeypatch):
+    """Calls on the default stream after an upload on another one: it is the default stream that waits
+    for the upload, and the results are those of the list."""
+    import paper_2412_21124_b200 as absnt
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    grads = [torch.randn(n, device="cuda", generator=gen) for n in (5000, 33, 1_000_003)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ts = absnt.GradTensors(grads)
+    waits = []
+    wait_event = torch.cuda.Stream.wait_event
+    monkeypatch.setattr(torch.cuda.Stream, "wait_event",
+                        lambda self, event: (waits.append(self.cuda_stream), wait_event(self, event))[1])
+    expected = torch.cat(grads).double().norm()
+    for stream in (None, torch.cuda.default_stream(), 0):
+        norm = absnt.abs_grad_norm(ts, stream=stream)
+        assert waits.pop() == torch.cuda.default_stream().cuda_stream == 0 and not waits
+        assert abs(float(norm) - float(expected)) <= 6e-7 * float(expected)

@@ -1,0 +1,106 @@
+"""The Python side of the calls over a list of tensors, without a device: torch.cuda is replaced by a
+model of it with numbered streams."""
+
+import pytest
+import torch
+
+from paper_2412_21124_b200 import binding
+
+
+class Stream:
+    """A stream that writes down what is asked of it.  As in torch, a stream made for the number 0 is
+    not the default stream but one out of a pool."""
+    pool = 9000
+
+    def __init__(self, number):
+        self.cuda_stream, self.waits, self.capturing = number, [], False
+
+    def wait_event(self, event):
+        assert not self.capturing, "an event from outside would end the capture"
+        self.waits.append(event)
+
+
+class Cuda:
+    """The parts of torch.cuda that a call uses."""
+
+    def __init__(self):
+        self.default = Stream(0)
+        self.current = self.default
+        self.external = {}
+
+    def make_external(self, number, device=None):
+        if number == 0:
+            Stream.pool += 1
+            return Stream(Stream.pool)
+        return self.external.setdefault(number, Stream(number))
+
+    def stream(self, s):
+        cuda = self
+
+        class Context:
+            def __enter__(self):
+                self.before, cuda.current = cuda.current, s
+
+            def __exit__(self, *_):
+                cuda.current = self.before
+        return Context()
+
+
+class Buffer:
+    def __init__(self):
+        self.recorded = []
+
+    def record_stream(self, s):
+        self.recorded.append(s)
+
+
+@pytest.fixture
+def cuda(monkeypatch):
+    c = Cuda()
+    monkeypatch.setattr(torch.cuda, "Stream", Stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", c.make_external)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: c.default)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: c.current)
+    monkeypatch.setattr(torch.cuda, "stream", c.stream)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: c.current.capturing)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: c.current.cuda_stream,
+                        raising=False)
+    return c
+
+
+def tensors(uploaded_on=0, **more):
+    """A GradTensors as its construction on the stream of that number leaves it, with no tensors."""
+    ts = object.__new__(binding.GradTensors)
+    fields = dict(_device=0, _uploaded_on=uploaded_on, _uploaded=object(), _work=Buffer(),
+                  _results=Buffer(), _hparams=None, _hparams_of=None, n_groups=1)
+    ts.__dict__.update(fields, **more)
+    return ts
+
+
+def entered(ts, stream, on):
+    """The call on `stream` ran on `on`, which waited for the upload and keeps the buffers."""
+    number = ts._enter(stream)
+    assert number == on.cuda_stream
+    assert on.waits == [ts._uploaded]
+    assert ts._work.recorded == [on] and ts._results.recorded == [on]
+
+
+@pytest.mark.parametrize("given", ("nothing", "stream", "number"))
+def test_default_stream_waits_for_an_upload_elsewhere(cuda, given):
+    ts = tensors(uploaded_on=77)
+    entered(ts, {"nothing": None, "stream": cuda.default, "number": 0}[given], cuda.default)
+
+
+@pytest.mark.parametrize("given", ("nothing", "stream", "number"))
+def test_side_stream_waits_for_an_upload_on_the_default_one(cuda, given):
+    ts, side = tensors(uploaded_on=0), cuda.make_external(77)
+    if given == "nothing":
+        cuda.current = side
+    entered(ts, {"nothing": None, "stream": side, "number": 77}[given], side)
+
+
+def test_the_uploading_stream_waits_for_nothing(cuda):
+    ts = tensors(uploaded_on=0)
+    assert ts._enter(None) == 0 and ts._enter(cuda.default) == 0
+    assert not cuda.default.waits and not ts._work.recorded
