@@ -739,7 +739,8 @@ class GradTensors:
 
     def _enter(self, stream):
         """The stream of a call, as a number; a stream other than the one the plan was uploaded on
-        first waits for the upload."""
+        first waits for the upload, unless it is being captured: an event from outside cannot go into
+        a graph, so the upload has to be done before the capture begins."""
         if torch._C._cuda_getDevice() != self._device:
             raise ValueError("the tensors live on cuda:%d, which is not the current device"
                              % self._device)
@@ -747,11 +748,14 @@ class GradTensors:
             raw = torch._C._cuda_getCurrentRawStream(self._device)
         else:
             raw = _stream(stream).value or 0
-        if raw != self._uploaded_on and not torch.cuda.is_current_stream_capturing():
+        if raw != self._uploaded_on:
             other = _stream_object(stream, self._device)
-            other.wait_event(self._uploaded)
-            self._work.record_stream(other)
-            self._results.record_stream(other)
+            with torch.cuda.stream(other):  # the question is about the current stream
+                captured = torch.cuda.is_current_stream_capturing()
+            if not captured:
+                other.wait_event(self._uploaded)
+                self._work.record_stream(other)
+                self._results.record_stream(other)
         return raw
 
     def _groups(self, hparams):

@@ -178,3 +178,22 @@ def test_built_on_a_side_stream(monkeypatch):
         norm = absnt.abs_grad_norm(ts, stream=stream)
         assert waits.pop() == torch.cuda.default_stream().cuda_stream == 0 and not waits
         assert abs(float(norm) - float(expected)) <= 6e-7 * float(expected)
+
+
+def test_capture_of_a_given_stream():
+    """A call with `stream` on a stream under capture, while another one is current."""
+    import paper_2412_21124_b200 as absnt
+    grads = [torch.full((n,), 2.0, device="cuda") for n in (50, 9)]
+    ts = absnt.GradTensors(grads)
+    absnt.abs_grad_norm(ts)  # the first call on a device is made outside of captures
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin(capture_error_mode="thread_local")
+    absnt.abs_grad_norm(ts, norm_type=1, stream=side)
+    with torch.cuda.stream(side):
+        graph.capture_end()
+    assert float(ts.norm) == pytest.approx(2 * 59 ** 0.5)  # captured, not run
+    graph.replay()
+    torch.cuda.synchronize()
+    assert float(ts.norm) == 118.0

@@ -104,3 +104,22 @@ def test_the_uploading_stream_waits_for_nothing(cuda):
     ts = tensors(uploaded_on=0)
     assert ts._enter(None) == 0 and ts._enter(cuda.default) == 0
     assert not cuda.default.waits and not ts._work.recorded
+
+
+def test_capture_of_the_given_stream(cuda):
+    """No wait for an event from outside goes into a stream that is being captured, whatever stream is
+    the current one."""
+    ts, side = tensors(uploaded_on=0), cuda.make_external(77)
+    side.capturing = True
+    for stream in (side, 77):
+        assert ts._enter(stream) == 77
+    assert not side.waits and cuda.current is cuda.default
+
+
+def test_capture_of_another_stream(cuda):
+    """A given stream that is not captured waits, though the current one is being captured."""
+    ts, side, captured = tensors(uploaded_on=0), cuda.make_external(77), cuda.make_external(78)
+    captured.capturing = True
+    cuda.current = captured
+    entered(ts, side, side)
+    assert cuda.current is captured and not captured.waits
