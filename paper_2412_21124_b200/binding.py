@@ -772,12 +772,14 @@ class GradTensors:
 
 
 def _copied(hparams):
-    """A copy that compares equal while the values are the same; None for what is not plain dicts."""
-    if isinstance(hparams, dict):
-        return dict(hparams)
-    if isinstance(hparams, (list, tuple)) and all(isinstance(h, dict) for h in hparams):
-        return type(hparams)(dict(h) for h in hparams)
-    return None
+    """A copy that compares equal while the values are the same.  None for what is not plain dicts of
+    Python numbers: a tensor or an array may be changed in place, and its copy would change with it."""
+    groups = [hparams] if isinstance(hparams, dict) else hparams
+    if type(groups) not in (list, tuple) or not all(isinstance(h, dict) for h in groups):
+        return None
+    if not all(isinstance(x, (int, float)) for h in groups for x in h.values()):
+        return None
+    return dict(hparams) if isinstance(hparams, dict) else type(groups)(dict(h) for h in groups)
 
 
 def _norm_type(norm_type):

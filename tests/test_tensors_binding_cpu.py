@@ -1,6 +1,9 @@
 """The Python side of the calls over a list of tensors, without a device: torch.cuda is replaced by a
 model of it with numbered streams."""
 
+import collections
+
+import numpy as np
 import pytest
 import torch
 
@@ -123,3 +126,43 @@ def test_capture_of_another_stream(cuda):
     cuda.current = captured
     entered(ts, side, side)
     assert cuda.current is captured and not captured.waits
+
+
+HP = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.1)
+
+
+def lrs(ts, hparams):
+    return [pytest.approx(h.lr, rel=1e-6) for h in ts._groups(hparams)]
+
+
+@pytest.mark.parametrize("scalar", (lambda: torch.tensor(1e-3), lambda: np.array(1e-3)))
+@pytest.mark.parametrize("form", (lambda hp: hp, lambda hp: [hp], lambda hp: (hp,)))
+def test_a_learning_rate_that_is_changed_in_place(scalar, form):
+    ts, lr = tensors(), scalar()
+    hparams = form(dict(HP, lr=lr))
+    assert lrs(ts, hparams) == [1e-3]
+    lr *= 0.1
+    assert lrs(ts, hparams) == [1e-4]
+
+
+def test_hparams_that_change():
+    ts = tensors(n_groups=2)
+    hp = dict(HP)
+    assert lrs(ts, hp) == [1e-3, 1e-3]
+    hp["lr"] = 2e-3
+    assert lrs(ts, hp) == [2e-3, 2e-3]
+    pair = [hp, dict(HP)]
+    assert lrs(ts, pair) == [2e-3, 1e-3]
+    pair[1]["lr"] = 3e-3
+    assert lrs(ts, pair) == [2e-3, 3e-3]
+    struct = binding.abs_adamw_hparams(4e-3, 0.9, 0.999, 1e-8, 0.1)
+    assert lrs(ts, struct) == [4e-3, 4e-3]
+    struct.lr = 5e-3
+    assert lrs(ts, struct) == [5e-3, 5e-3]
+    kept = ts._groups(pair)
+    assert ts._groups([dict(h) for h in pair]) is kept  # the same values: not converted again
+
+
+def test_hparams_in_a_named_tuple():
+    Pair = collections.namedtuple("Pair", "matrices vectors")
+    assert lrs(tensors(n_groups=2), Pair(HP, dict(HP, lr=2e-3))) == [1e-3, 2e-3]
