@@ -760,7 +760,7 @@ class GradTensors:
 
     def _groups(self, hparams):
         """The hyper-parameters of all groups as a C array, kept while they are the same values."""
-        if hparams != self._hparams_of:
+        if self._hparams_of is None or hparams != self._hparams_of:
             if isinstance(hparams, (dict, abs_adamw_hparams)):
                 array = (abs_adamw_hparams * self.n_groups)(*[_hparams(hparams)] * self.n_groups)
             elif len(hparams) < self.n_groups:

@@ -166,3 +166,12 @@ def test_hparams_that_change():
 def test_hparams_in_a_named_tuple():
     Pair = collections.namedtuple("Pair", "matrices vectors")
     assert lrs(tensors(n_groups=2), Pair(HP, dict(HP, lr=2e-3))) == [1e-3, 2e-3]
+
+
+def test_no_hparams_after_others():
+    """None is refused, not taken for those of the call before."""
+    ts = tensors()
+    for before in (binding.abs_adamw_hparams(1e-3, 0.9, 0.999, 1e-8, 0.1), HP):
+        ts._groups(before)
+        with pytest.raises(TypeError):
+            ts._groups(None)
