@@ -506,7 +506,7 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  * gradients is right also where their fp32 squares overflow or vanish.  Results do not depend on
  * the order in which blocks run.  s c is rounded to float once (below 2^-126, for norms above 1e38
  * max_norm, with fewer bits).  A norm that is not finite (a NaN or infinite gradient) raises
- * ABS_FLAG_NONFINITE in the header; c is then 1 and AdamW leaves params, m and v as they are.
+ * ABS_FLAG_NONFINITE in the header; c is then 1 and a clipping AdamW leaves params, m and v as they are.
  */
 typedef struct {
   void* data;         /* device, aligned to its element size; may be NULL when numel = 0          */
@@ -581,8 +581,9 @@ int abs_grad_clip(const void* plan, void* work, int norm_type, double grad_scale
  * AdamW on clipped gradients: abs_adamw_step for every tensor with g = (s c) x, which stays in
  * registers; the gradients are not written.
  *   hparams    host, n_groups entries (1..ABS_MAX_GROUPS); tensor t uses entry grads[t].group
- *   max_norm   > 0: as abs_grad_clip, sum_in too; 0: no norm is computed, c = 1, sum_in and
- *              norms_out are left alone
+ *   max_norm   > 0: as abs_grad_clip, sum_in too; 0: no norm is computed, c = 1, sum_in,
+ *              norms_out and the header are left alone, and gradients that are not finite are
+ *              not noticed: they reach params, m and v
  */
 int abs_grad_adamw(const void* plan, void* work, const abs_adamw_hparams* hparams, int n_groups,
                    int64_t step, int norm_type, double grad_scale, double max_norm,

@@ -823,16 +823,20 @@ def abs_grad_clip(tensors, max_norm, norm_type=2, grad_scale=1.0, sum_in=None, s
 def abs_grad_adamw(tensors, hparams, step, max_norm=0.0, norm_type=2, grad_scale=1.0, sum_in=None,
                    stream=None):
     """AdamW on the gradients scaled by grad_scale and, with max_norm > 0, clipped by their global
-    norm.  `hparams`: one dict for all tensors, or a list with one per group.  An update whose norm
-    is not finite is left out.  Returns the global norm, a view of the object's results (not
-    written when max_norm is 0)."""
+    norm.  `hparams`: one dict for all tensors, or a list with one per group.  Returns the global norm,
+    a view of the object's results.
+
+    Only with max_norm > 0 is a norm computed, and an update whose norm is not finite left out (a very
+    large max_norm asks for that alone).  With max_norm = 0 a NaN or an infinity in the gradients
+    reaches params, m and v; norm, coef, norms and the header stay those of an earlier call, and
+    nothing is returned."""
     hp = tensors._groups(hparams)
     rc = lib().abs_grad_adamw(tensors._plan_ptr, tensors._work_ptr, hp, len(hp), step,
                               _norm_type(norm_type), grad_scale, max_norm, _sum_in(sum_in),
                               tensors._results_ptr, tensors._enter(stream))
     if rc != ABS_OK:
         raise AbsError(rc, "abs_grad_adamw")
-    return tensors.norm
+    return tensors.norm if max_norm else None
 
 
 def abs_decide(S, n2, norm, eta, b_cur):

@@ -218,8 +218,9 @@ def sharded_grad_clip(tensors, max_norm, norm_type=2, grad_scale=1.0, group=None
 def sharded_grad_adamw(tensors, hparams, step, max_norm, norm_type=2, grad_scale=1.0, group=None):
     """abs_grad_adamw where each rank's GradTensors holds its own part of gradients, parameters and
     moments; as sharded_grad_clip.  A gradient that is not finite on one rank leaves the update out
-    on all of them."""
-    if not (dist.is_initialized() and dist.get_world_size(group) > 1):
+    on all of them, if they clip: with max_norm = 0 (the same on all ranks) no norm is computed and
+    nothing exchanged, as in abs_grad_adamw."""
+    if not max_norm or not (dist.is_initialized() and dist.get_world_size(group) > 1):
         return binding.abs_grad_adamw(tensors, hparams, step, max_norm, norm_type, grad_scale)
     binding.abs_grad_norm(tensors, norm_type, grad_scale)
     total = join_power_sums(tensors.header[binding.ABS_GRAD_SUM], norm_type, group)

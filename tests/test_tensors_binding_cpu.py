@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2412_21124_b200 import binding
+from paper_2412_21124_b200 import binding, dist
 
 
 class Stream:
@@ -175,3 +175,39 @@ def test_no_hparams_after_others():
         ts._groups(before)
         with pytest.raises(TypeError):
             ts._groups(None)
+
+
+class Library:
+    """The three launching calls, always answering ABS_OK; writes down which were made."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        return lambda *arguments: self.made.append(name) or 0
+
+
+@pytest.fixture
+def library(monkeypatch):
+    calls = Library()
+    monkeypatch.setattr(binding, "_lib", calls)
+    return calls
+
+
+def test_adamw_without_clipping_returns_no_norm(cuda, library):
+    """No norm is computed then: what the object holds is that of an earlier call, or nothing at all."""
+    ts = tensors(norm=object(), _plan_ptr=0, _work_ptr=0, _results_ptr=0)
+    assert binding.abs_grad_adamw(ts, HP, 1) is None
+    assert binding.abs_grad_adamw(ts, HP, 1, max_norm=1.0) is ts.norm
+    assert library.made == ["abs_grad_adamw"] * 2
+
+
+def test_sharded_adamw_without_clipping(cuda, library, monkeypatch):
+    """Over ranks too: no norm, nothing exchanged."""
+    monkeypatch.setattr(dist.dist, "is_initialized", lambda: True)
+    monkeypatch.setattr(dist.dist, "get_world_size", lambda group=None: 2)
+    ts = tensors(norm=object(), header=torch.zeros(8, dtype=torch.float64), _plan_ptr=0, _work_ptr=0,
+                 _results_ptr=0)
+    monkeypatch.setattr(dist, "join_power_sums", None)  # not to be called
+    assert dist.sharded_grad_adamw(ts, HP, 1, 0.0) is None
+    assert library.made == ["abs_grad_adamw"]
