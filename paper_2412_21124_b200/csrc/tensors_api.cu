@@ -5,6 +5,7 @@
 #include <cfloat>
 #include <cstring>
 #include <mutex>
+#include <numeric>
 #include <vector>
 
 #include "host_checks.cuh"
@@ -159,17 +160,59 @@ bool spans_far(const View& v, int64_t most) {
   return rows > (int64_t{1} << 30) / v.stride || v.row > (int64_t{1} << 30) / v.col;
 }
 
-// Two views share an element.  Rows of the same stride that interleave do not.
+// The bytes of a view: `n` groups, `step` apart, of `pieces` runs of `width` bytes, `piece_step` apart.
+// Neither the groups nor the runs of a group reach into each other.
+struct Places {
+  uintptr_t at;
+  int64_t n, step, pieces, piece_step, width;
+  int64_t group() const { return (pieces - 1) * piece_step + width; }
+  explicit Places(const View& v) : at(reinterpret_cast<uintptr_t>(v.data)) {
+    const int64_t esz = static_cast<int64_t>(v.esz);
+    n = v.numel / v.row, step = v.stride * esz, pieces = v.row, piece_step = v.col * esz, width = esz;
+    if (step <= (pieces - 1) * piece_step) std::swap(n, pieces), std::swap(step, piece_step);
+    if (piece_step == width) width *= pieces, pieces = 1;
+    if (n == 1) n = pieces, step = piece_step, pieces = 1;
+  }
+};
+
+// Items of `ea` bytes at a, a + sa, .. (na of them) against such at b: whether f(place in a, place in b)
+// is true for two that share a byte.  No two of a meet, nor two of b, so those that share form one chain,
+// which is walked from its beginning.  What lies where repeats after the common multiple of sa and sb.
+template <typename F>
+bool any_pair(int64_t a, int64_t na, int64_t sa, int64_t ea, int64_t b, int64_t nb, int64_t sb, int64_t eb,
+              F&& f) {
+  int64_t period_a = na, period_b = nb;  // in items
+  if (na > 1 && nb > 1) {
+    const int64_t g = std::gcd(sa, sb);
+    period_a = std::min(na, sb / g);
+    period_b = std::min(nb, sa / g);
+  }
+  int64_t i = 0, k = 0;
+  while (true) {
+    // the first items that end after the other one begins
+    if (a + i * sa + ea <= b + k * sb) i = (b + k * sb - ea - a) / sa + 1;
+    if (i >= na) return false;
+    if (b + k * sb + eb <= a + i * sa) k = (a + i * sa - eb - b) / sb + 1;
+    if (k >= nb || (i >= period_a && k >= period_b)) return false;
+    const int64_t pa = a + i * sa, pb = b + k * sb;
+    if (pa + ea <= pb) continue;
+    if (f(pa, pb)) return true;
+    if (pa + ea <= pb + eb)
+      ++i;
+    else
+      ++k;
+  }
+}
+
+// Two views share an element.
 bool views_overlap(const View& a, const View& b) {
   if (!overlaps(a.data, a.extent(), b.data, b.extent())) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.data), pb = reinterpret_cast<uintptr_t>(b.data);
-  const View &lo = pa <= pb ? a : b, &hi = pa <= pb ? b : a;
-  const size_t s = static_cast<size_t>(lo.stride) * lo.esz;
-  if (lo.rows() && hi.rows() && lo.col == 1 && hi.col == 1 && s == static_cast<size_t>(hi.stride) * hi.esz) {
-    const size_t phase = (pa <= pb ? pb - pa : pa - pb) % s;
-    if (phase >= lo.row * lo.esz && phase + hi.row * hi.esz <= s) return false;
-  }
-  return true;
+  const Places p(a), q(b);
+  const int64_t from = static_cast<int64_t>(q.at - p.at);
+  return any_pair(0, p.n, p.step, p.group(), from, q.n, q.step, q.group(), [&](int64_t x, int64_t y) {
+    return any_pair(x, p.pieces, p.piece_step, p.width, y, q.pieces, q.piece_step, q.width,
+                    [](int64_t, int64_t) { return true; });
+  });
 }
 
 // Any pair of views of which at least one is written (`written`) that shares an element; pairs of

@@ -3,6 +3,7 @@ full; every refusal of the launching calls comes before the first CUDA call.  As
 test_abi_cpu.py, no device is visible while fabricated addresses are handed over."""
 import ctypes
 import os
+import random
 
 import pytest
 
@@ -194,3 +195,62 @@ def test_launching_calls_refuse(L):
     hp[1].eps = 1e-8
     assert adamw(plan=bare) == B.ABS_ERR_NULL
 
+
+
+def shared(L, a, b):
+    """Whether the plan of a list in which `a` is a gradient and `b` an output of another tensor finds
+    an element that both hold."""
+    rc, _ = plan(L, [a, T(far(200), b.numel)], outs=[T(far(220), a.numel), b])
+    assert rc in (B.ABS_OK, B.ABS_ERR_ALIAS)
+    return rc == B.ABS_ERR_ALIAS
+
+
+def test_views_that_interleave(L):
+    at = far(1)
+    # even and odd columns of a matrix of 10 x 20
+    even, odd = T(at, 100, 10, 20, 2), T(at + 4, 100, 10, 20, 2)
+    assert not shared(L, even, odd) and not shared(L, odd, even)
+    assert shared(L, even, T(at + 8, 90, 9, 20, 2))
+    # column slices of a transposed matrix, the columns walked first
+    left, right = T(at, 80, 10, 1, 20), T(at + 4 * 8, 120, 10, 1, 20)
+    assert not shared(L, left, right)
+    assert shared(L, left, T(at + 4 * 7, 120, 10, 1, 20))
+    # a contiguous tensor between two rows, and one that reaches into the second
+    rows = T(at, 40, 8, 20, 1)
+    assert not shared(L, rows, T(at + 32, 12)) and not shared(L, T(at + 32, 12), rows)
+    assert shared(L, rows, T(at + 32, 13)) and shared(L, rows, T(at + 28, 12))
+    # rows of different strides: every fourth, every third, every fourth of them in the gaps
+    assert not shared(L, T(at, 50, 1, 4, 1), T(at + 4, 25, 1, 8, 1))
+    assert shared(L, T(at, 50, 1, 4, 1), T(at + 4, 50, 1, 3, 1))
+    # 16-bit views between fp32 ones
+    assert not shared(L, T(at, 100, 10, 20, 2), T(at + 4, 100, 10, 40, 4, B.ABS_BF16))
+    assert not shared(L, T(at, 100, 10, 20, 2), T(at + 6, 100, 10, 40, 4, B.ABS_F16))
+    assert shared(L, T(at, 100, 10, 20, 2), T(at + 2, 100, 10, 40, 4, B.ABS_F16))
+    # a whole embedding's columns dealt out to two, far apart in a long matrix
+    assert not shared(L, T(at, 50_000 * 96, 96, 192, 2), T(at + 4, 50_000 * 96, 96, 192, 2))
+    assert shared(L, T(at, 50_000, 1, 1001, 1), T(at + 4 * 1001 * 40_000, 7000, 1, 997, 1))
+
+
+def test_views_share_an_element_or_not(L):
+    """Against the elements themselves, random pairs of views."""
+    rng = random.Random(7)
+
+    def view():
+        esz, dtype = rng.choice(((4, B.ABS_F32), (2, B.ABS_BF16)))
+        inner, outer = rng.choice((1, 1, 2, 3, 8)), rng.choice((1, 2, 5, 12))
+        step = rng.choice((1, 1, 2, 3, 5))
+        stride = (inner - 1) * step + 1 + rng.choice((0, 0, 1, 2, 7, 40))
+        if rng.random() < 0.3:  # the columns walked first
+            inner, outer, step, stride = outer, inner, stride, step
+        at = FAKE + esz * rng.randrange(0, 160)
+        held = {at + esz * (i * stride + j * step) + k for i in range(outer) for j in range(inner)
+                for k in range(esz)}
+        return T(at, inner * outer, inner, stride, step, dtype), held
+
+    found = [0, 0]
+    for _ in range(20_000):
+        (a, x), (b, y) = view(), view()
+        assert shared(L, a, b) == bool(x & y), (
+            [(t.data - FAKE, t.numel, t.row_len, t.row_stride, t.col_stride, t.dtype) for t in (a, b)])
+        found[bool(x & y)] += 1
+    assert min(found) > 2000

@@ -191,6 +191,25 @@ def test_interleaved_slices_in_place():
     assert torch.equal(parent[:, 97:], before[:, 97:])
 
 
+@pytest.mark.parametrize("dtype", (F32, BF16))
+@pytest.mark.parametrize("rows", (70, 9000))
+def test_interleaved_views_in_place(rows, dtype):
+    """Gradients in each other's gaps, in one list, scaled in place: even and odd columns, a contiguous
+    one between two rows of another, columns of a transposed matrix."""
+    g = gen(22)
+    parents = [make((rows, 90), dtype, "dense", g), make((rows, 64), dtype, "dense", g),
+               make((rows, 50), dtype, "swapped", g)]
+    views = lambda a, b, c: [a[:, ::2], a[:, 1::2], b[:, :20], b[3, 20:], c[:, 8:31], c[:, :8]]  # noqa: E731
+    before = [x.clone() for x in parents]
+    ts = absnt.GradTensors(views(*parents))
+    absnt.abs_grad_clip(ts, 1.0)
+    total = check_norms(ts, views(*before), 2)
+    for x, b in zip(views(*parents), views(*before)):
+        check_scaled(x, b, 1.0 / (total + 1e-6), dtype)
+    assert torch.equal(parents[1][4:, 20:], before[1][4:, 20:])
+    assert torch.equal(parents[2][:, 31:], before[2][:, 31:])
+
+
 @pytest.mark.parametrize("n", (127, 128, 129, 130, 257))
 @pytest.mark.parametrize("many", (40, 700))
 def test_short_last_rows(n, many):
