@@ -544,6 +544,8 @@ enum {
  * Elements correspond by their index i, whatever the rows.  n = 0 and empty tensors are allowed.
  * No output may share an element with a gradient or another output (ABS_ERR_ALIAS).  Gradients may
  * overlap each other unless abs_grad_clip is to scale them in place (it answers ABS_ERR_ALIAS).
+ * Neither the work area nor norms_out may share a byte with a tensor of the list, or with each other
+ * (ABS_ERR_ALIAS from the calls that take them).
  * ABS_ERR_TOO_LARGE: plan_bytes is too small, or the host is out of memory.
  */
 size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n);

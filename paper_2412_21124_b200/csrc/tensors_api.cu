@@ -26,12 +26,13 @@ constexpr int64_t kMaxElements = int64_t{1} << 46;
 constexpr int64_t kMaxUnits = int64_t{1} << 30;
 enum { kRoleOut = 1, kRoleAdam = 2, kRoleBf16 = 4, kGradsOverlap = 8 };
 
-// Host image of a plan: this header, then the tables in the order of `Image`.
+// Host image of a plan: this header, the tables in the order of `Image`, and the ranges of addresses that
+// the list's tensors take up.
 struct PlanHeader {
   uint64_t magic;
   int32_t n, n_scale, n_adamw, n_further, n_spanning, n_empty, scale_unit;
   int32_t blocks, rows, cluster;  // rows: of each warp; cluster: the blocks make up one
-  int32_t roles, n_groups;
+  int32_t roles, n_groups, n_taken;
   int64_t total;  // elements
 };
 // Offsets of the tables in the image (which the device holds as well).
@@ -49,6 +50,13 @@ struct Image {
   }
 };
 char* image_of(void* plan) { return static_cast<char*>(plan) + sizeof(PlanHeader); }
+const char* image_of(const void* plan) { return static_cast<const char*>(plan) + sizeof(PlanHeader); }
+
+// A range of addresses, from the first to the last element of a tensor or of several that touch.
+struct Taken {
+  uintptr_t begin, end;
+};
+size_t taken_offset(const Image& image) { return sizeof(PlanHeader) + (image.bytes + 7) / 8 * 8; }
 
 // Device work area: header, sums of the blocks, their edge sums, the factor, the tickets, the image
 // of the plan.
@@ -231,10 +239,53 @@ bool any_conflict(std::vector<std::pair<View, bool>>& list) {
   return false;
 }
 
+// The ranges that the views of a list take up, in order, those that touch as one.  Sorted by address.
+std::vector<Taken> taken_by(const std::vector<std::pair<View, bool>>& list) {
+  std::vector<Taken> all;
+  for (const auto& [v, written] : list) {
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(v.data), end = begin + v.extent();
+    if (!all.empty() && begin <= all.back().end)
+      all.back().end = std::max(all.back().end, end);
+    else
+      all.push_back({begin, end});
+  }
+  return all;
+}
+
 const PlanHeader* plan_of(const void* plan) {
   if (!plan || misaligned(plan, 8)) return nullptr;
   const PlanHeader* h = static_cast<const PlanHeader*>(plan);
   return h->magic == kPlanMagic ? h : nullptr;
+}
+
+// Whether `bytes` bytes at p hold an element of a tensor of the plan.  Outside of the ranges that the
+// tensors take up that is one search; inside (it may still be a gap between rows) every tensor is asked.
+bool over_tensors(const PlanHeader& h, const void* p, size_t bytes) {
+  const char* image = image_of(&h);
+  const Taken* taken = reinterpret_cast<const Taken*>(reinterpret_cast<const char*>(&h) + taken_offset(Image(h)));
+  const uintptr_t begin = reinterpret_cast<uintptr_t>(p);
+  const Taken* first = std::partition_point(taken, taken + h.n_taken, [&](const Taken& t) { return t.end <= begin; });
+  if (first == taken + h.n_taken || first->begin >= begin + bytes) return false;
+  const int64_t n = static_cast<int64_t>(bytes);
+  const View here{p, n, n, n, 1, 1};
+  const TensorEntry* entries = reinterpret_cast<const TensorEntry*>(image);
+  for (int t = 0; t < h.n; ++t) {
+    const TensorEntry& e = entries[t];
+    if (!e.numel) continue;
+    View g{e.g, e.numel, e.numel, e.numel, 1, element_size(e.g_dtype)};
+    if (e.flags & kEntryRowsG) g.row = e.g_row, g.stride = e.g_stride, g.col = e.g_col;
+    if (views_overlap(here, g)) return true;
+    if (e.out) {
+      View out{e.out, e.numel, e.numel, e.numel, 1, element_size(e.out_dtype)};
+      if (e.flags & kEntryRowsOut) out.row = e.out_row, out.stride = e.out_stride, out.col = e.out_col;
+      if (views_overlap(here, out)) return true;
+    }
+    const size_t numel = static_cast<size_t>(e.numel);
+    for (const float* s : {e.p, e.m, e.v})
+      if (s && overlaps(p, bytes, s, 4 * numel)) return true;
+    if (e.p16 && overlaps(p, bytes, e.p16, 2 * numel)) return true;
+  }
+  return false;
 }
 
 int fill_params(const void* plan, void* work, int norm_type, double scale, double max_norm,
@@ -250,7 +301,10 @@ int fill_params(const void* plan, void* work, int norm_type, double scale, doubl
     return ABS_ERR_ALIGN;
   const WorkLayout L(*h);
   char* w = static_cast<char*>(work);
-  if (norms_out && overlaps(norms_out, 4 * (static_cast<size_t>(h->n) + 2), work, L.bytes)) return ABS_ERR_ALIAS;
+  const size_t norms_bytes = 4 * (static_cast<size_t>(h->n) + 2);
+  if (norms_out && overlaps(norms_out, norms_bytes, work, L.bytes)) return ABS_ERR_ALIAS;
+  if ((norms_out && over_tensors(*h, norms_out, norms_bytes)) || over_tensors(*h, work, L.bytes))
+    return ABS_ERR_ALIAS;
   prm->header = reinterpret_cast<double*>(w);
   prm->block_sum = reinterpret_cast<double*>(w + L.block_sum);
   prm->edge_sum = reinterpret_cast<double*>(w + L.edge_sum);
@@ -488,6 +542,8 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   }
   if (any_conflict(all)) return ABS_ERR_ALIAS;
   if (any_conflict(grads_written)) h.roles |= kGradsOverlap;
+  const std::vector<Taken> taken = taken_by(all);  // which any_conflict has sorted
+  h.n_taken = static_cast<int32_t>(taken.size());
 
   // the segments: the rows of all tensors in order, dealt out warp by warp
   Segment idle;
@@ -560,7 +616,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   h.n_adamw = static_cast<int32_t>(adamw_tensor.size());
 
   const Image I(h);
-  if (plan_bytes < sizeof(PlanHeader) + I.bytes) return ABS_ERR_TOO_LARGE;
+  if (plan_bytes < taken_offset(I) + taken.size() * sizeof(Taken)) return ABS_ERR_TOO_LARGE;
   char* image = image_of(plan);
   const auto put = [](char* to, const void* from, size_t bytes) {
     if (bytes) std::memcpy(to, from, bytes);
@@ -573,6 +629,7 @@ int make_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor*
   put(image + I.scale_tensor, scale_tensor.data(), scale_tensor.size() * 4);
   put(image + I.adamw_tensor, adamw_tensor.data(), adamw_tensor.size() * 4);
   put(image + I.empty, empty.data(), empty.size() * 4);
+  put(static_cast<char*>(plan) + taken_offset(I), taken.data(), taken.size() * sizeof(Taken));
   std::memcpy(plan, &h, sizeof h);
   return ABS_OK;
 }
@@ -605,7 +662,7 @@ size_t abs_tensors_plan_bytes(const abs_tensor* grads, int n) {
   h.n_adamw = static_cast<int32_t>(adamw);
   h.blocks = deal.blocks;
   h.n_spanning = std::min(n, deal.blocks);
-  return sizeof h + Image(h).bytes;
+  return taken_offset(Image(h)) + 6 * static_cast<size_t>(n) * sizeof(Taken);  // six roles
 }
 
 int abs_tensors_plan(const abs_tensor* grads, const abs_tensor* outs, const abs_tensor* params,
@@ -635,6 +692,7 @@ int abs_tensors_upload(const void* plan, void* work, abs_stream_t stream) {
   if (!h) return ABS_ERR_RANGE;
   if (misaligned(work, 16)) return ABS_ERR_ALIGN;
   const WorkLayout L(*h);
+  if (over_tensors(*h, work, L.bytes)) return ABS_ERR_ALIAS;
   char* w = static_cast<char*>(work);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaMemsetAsync(w, 0, L.image, st);

@@ -254,3 +254,34 @@ def test_views_share_an_element_or_not(L):
             [(t.data - FAKE, t.numel, t.row_len, t.row_stride, t.col_stride, t.dtype) for t in (a, b)])
         found[bool(x & y)] += 1
     assert min(found) > 2000
+
+
+def test_results_and_work_area_over_the_lists_tensors(L):
+    """norms_out (n + 2 floats) and the work area share no byte with a tensor of the list.  (Clipping with
+    max_norm 0 is refused too, but after that.)"""
+    rows = T(far(1), 200, 20, 64, 1)  # ten rows of 20 floats, 64 apart
+    rc, buf = plan(L, [rows, T(far(2), 10, dtype=B.ABS_BF16)], outs=[T(far(3), 200), T(far(4), 10)],
+                   p16=[T(far(5), 200, dtype=B.ABS_BF16), T(far(6), 10, dtype=B.ABS_BF16)],
+                   **{k: [T(far(i), 200), T(far(i + 1), 10)] for k, i in (("p", 10), ("m", 40), ("v", 70))})
+    assert rc == B.ABS_OK
+    hp = (B.abs_adamw_hparams * 1)(B.abs_adamw_hparams(1e-3, 0.9, 0.999, 1e-8, 0.1))
+    size = L.abs_tensors_work_bytes(buf)
+    work, apart = far(100), far(101)
+    taken = [far(i) + 4 for i in (1, 3, 4, 5, 10, 11, 40, 41, 70, 71)]
+    taken += [far(2) + 16, far(6) + 16, far(3) + 796]       # the last elements
+    taken += [far(1) + 64 * 4 * 9 + 76, far(3) - 12]        # of the rows; norms_out reaches into it
+    free = [far(2) + 20, far(3) + 800, far(3) - 16, far(1) + 64 * 4 * 9 + 80]
+    free += [far(1) + 80, far(1) + 64 * 4 - 16]              # between two rows
+    for at in taken:
+        assert L.abs_grad_norm(buf, work, 2, 1.0, 0.0, at, None) == B.ABS_ERR_ALIAS
+        assert L.abs_grad_clip(buf, work, 2, 1.0, 0.0, None, at, None) == B.ABS_ERR_ALIAS
+        assert L.abs_grad_adamw(buf, work, hp, 1, 1, 2, 1.0, 1.0, None, at, None) == B.ABS_ERR_ALIAS
+    for at in free:
+        assert L.abs_grad_clip(buf, work, 2, 1.0, 0.0, None, at, None) == B.ABS_ERR_RANGE
+    for at in (far(1), far(2) - 16, (far(4) - size + 16) & ~15, (far(11) - size + 16) & ~15, far(70) + 32):
+        assert L.abs_tensors_upload(buf, at, None) == B.ABS_ERR_ALIAS
+        assert L.abs_grad_norm(buf, at, 2, 1.0, 0.0, apart, None) == B.ABS_ERR_ALIAS
+    assert L.abs_grad_clip(buf, far(4) - ((size + 15) & ~15), 2, 1.0, 0.0, None, apart, None) == B.ABS_ERR_RANGE
+    # none of it for an empty list
+    rc, buf = plan(L, [T(None, 0)])
+    assert rc == B.ABS_OK and L.abs_grad_clip(buf, work, 2, 1.0, 0.0, None, apart, None) == B.ABS_ERR_RANGE
