@@ -295,7 +295,7 @@ int fill_params(const void* plan, void* work, int norm_type, double scale, doubl
   if (!h) return ABS_ERR_RANGE;
   if (norm_type != ABS_NORM_2 && norm_type != ABS_NORM_1 && norm_type != ABS_NORM_MAX)
     return ABS_ERR_RANGE;
-  if (!(std::fabs(scale) <= FLT_MAX) || scale == 0.0) return ABS_ERR_RANGE;
+  if (!(std::fabs(scale) <= FLT_MAX) || static_cast<float>(scale) == 0.f) return ABS_ERR_RANGE;
   if (!std::isfinite(max_norm) || max_norm < 0.0) return ABS_ERR_RANGE;
   if (misaligned(work, 16) || misaligned(norms_out, 4) || misaligned(sum_in, 8))
     return ABS_ERR_ALIGN;

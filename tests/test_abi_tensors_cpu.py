@@ -285,3 +285,13 @@ def test_results_and_work_area_over_the_lists_tensors(L):
     # none of it for an empty list
     rc, buf = plan(L, [T(None, 0)])
     assert rc == B.ABS_OK and L.abs_grad_clip(buf, work, 2, 1.0, 0.0, None, apart, None) == B.ABS_ERR_RANGE
+
+
+def test_a_scale_that_is_zero_as_a_float(L):
+    """grad_scale is a float: below its range the norm would be scaled and the gradients be zeroed."""
+    rc, buf = plan(L, [T(far(1))], **state())
+    hp = (B.abs_adamw_hparams * 1)(B.abs_adamw_hparams(1e-3, 0.9, 0.999, 1e-8, 0.1))
+    for scale in (1e-60, -1e-60, 5e-324, 7e-46):
+        assert L.abs_grad_norm(buf, far(100), 2, scale, 0.0, far(101), None) == B.ABS_ERR_RANGE
+        assert L.abs_grad_clip(buf, far(100), 2, scale, 1.0, None, far(101), None) == B.ABS_ERR_RANGE
+        assert L.abs_grad_adamw(buf, far(100), hp, 1, 1, 2, scale, 1.0, None, far(101), None) == B.ABS_ERR_RANGE
