@@ -794,6 +794,7 @@ def _sum_in(sum_in):
         return None
     if not sum_in.is_cuda or sum_in.dtype != torch.float64 or sum_in.numel() < 1:
         raise TypeError("sum_in must be a CUDA float64 tensor")
+    _check_one_device(sum_in)
     return sum_in.data_ptr()
 
 

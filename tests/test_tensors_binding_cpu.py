@@ -211,3 +211,29 @@ def test_sharded_adamw_without_clipping(cuda, library, monkeypatch):
     monkeypatch.setattr(dist, "join_power_sums", None)  # not to be called
     assert dist.sharded_grad_adamw(ts, HP, 1, 0.0) is None
     assert library.made == ["abs_grad_adamw"]
+
+
+class Sum:
+    """A float64 tensor on a CUDA device."""
+    is_cuda, dtype = True, torch.float64
+
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+
+    def numel(self):
+        return 1
+
+    def data_ptr(self):
+        return 4096
+
+
+def test_a_sum_on_another_device(cuda, library, monkeypatch):
+    """Its address means nothing to the kernels of this one."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    ts = tensors(norm=object(), _plan_ptr=0, _work_ptr=0, _results_ptr=0)
+    for call in (lambda s: binding.abs_grad_clip(ts, 1.0, sum_in=s),
+                 lambda s: binding.abs_grad_adamw(ts, HP, 1, 1.0, sum_in=s)):
+        with pytest.raises(ValueError):
+            call(Sum(1))
+        assert call(Sum(0)) is ts.norm
+    assert library.made == ["abs_grad_clip", "abs_grad_adamw"]
