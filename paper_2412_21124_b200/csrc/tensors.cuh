@@ -543,7 +543,9 @@ __device__ __forceinline__ bool last_of(unsigned int* ticket, unsigned int of) {
     if (before == of - 1) *ticket = 0;
     __threadfence();
   }
-  return __shfl_sync(0xffffffffu, before, 0) == of - 1;
+  before = __shfl_sync(0xffffffffu, before, 0);
+  __syncwarp();  // a shuffle orders no memory: what lane 0 may see, the others may from here on
+  return before == of - 1;
 }
 
 // sum |x|^p (or max |x|) of each tensor and of the list.  Every warp sums its rows, every block its
