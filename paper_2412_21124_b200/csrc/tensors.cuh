@@ -489,18 +489,18 @@ __device__ __forceinline__ double warp_sum(const TensorsParams& prm, const Segme
 }
 
 // Joins the parts of a block's warps, each tensor by the warp in which it begins (by warp 0, if it
-// began before the block); `edge[0]` and `edge[1]` receive the parts of a tensor that the block
-// shares with the one before and the one after it.  After a __syncthreads.
+// began before the block); edge(0, x) and edge(1, x), called by a whole warp, receive the parts of a
+// tensor that the block shares with the one before and the one after it.  After a __syncthreads.
 // Returns the tensor whose sum is now known to this warp (in `x`; to be written by the caller), or -1.
-template <int NORM>
-__device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockParts& parts,
-                                          double* edge, double& x) {
+template <int NORM, typename F>
+__device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockParts& parts, F&& edge,
+                                          double& x) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int state = lane < kListWarps ? parts.state[lane] : 0;
   const uint32_t heads = __ballot_sync(0xffffffffu, state & kHead);
   const uint32_t throughs = __ballot_sync(0xffffffffu, state & kThrough);
   const int mine = parts.state[warp];
-  if (warp == 0 && lane == 0 && (mine & kHead)) edge[0] = parts.head[0];
+  if (warp == 0 && (mine & kHead)) edge(0, parts.head[0]);
   if (!((mine & kTail) || (warp == 0 && (mine & kThrough)))) return -1;
   const uint32_t stop = ~throughs & ~((2u << warp) - 1u);  // warps after this one that end it
   const uint32_t u = stop ? static_cast<uint32_t>(__ffs(stop)) - 1u : 32u;
@@ -509,10 +509,8 @@ __device__ __forceinline__ int join_parts(const TensorsParams& prm, const BlockP
       : lane == u && ends                                       ? parts.head[lane]
                                                                 : 0.0;
   x = warp_join<NORM>(x);
-  if (lane == 0) {
-    if (!(mine & kTail)) edge[0] = x;
-    if (!ends) edge[1] = x;
-  }
+  if (!(mine & kTail)) edge(0, x);
+  if (!ends) edge(1, x);
   return (mine & kTail) && ends ? parts.tensor[warp] : -1;
 }
 
@@ -573,7 +571,10 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
   if (lane == 0) parts.sum[warp] = sum;
   __syncthreads();
   double x;
-  const int known = join_parts<NORM>(prm, parts, prm.edge_sum + 2 * blockIdx.x, x);
+  const auto edge = [&](int k, double part) {
+    if (lane == 0) prm.edge_sum[2 * blockIdx.x + k] = part;
+  };
+  const int known = join_parts<NORM>(prm, parts, edge, x);
   if (known >= 0 && lane == 0) write_norm<NORM>(prm, known, x);
   if (warp == 0) {
     sum = join_warps<NORM>(parts.sum);
@@ -1102,25 +1103,29 @@ __global__ void __launch_bounds__(kTensorThreads, 4)
 
 // ---- small lists: everything in one cluster -------------------------------------------------
 // Norm and second pass in one launch.  Up to kClusterBlocks blocks, launched as one cluster, hold
-// the whole list in shared memory, and every block sends its sums into the shared memory of all
-// (asynchronous stores counted on a barrier there): no ticket, no round trip to L2.
+// the whole list in shared memory, and every block writes its sums into the shared memory of all before
+// the cluster's barrier: no ticket, no round trip to L2, and no wait that could run out in one block and
+// not in another (asynchronous stores counted on an mbarrier took 0.08 us less and had that).
 enum { kOpNone = 0, kOpScale = 1, kOpAdamw = 2 };
 
 // What a block has for the others: its sum, and its parts of the tensors that it shares.
 struct BlockSums {
-  double sum, edge[2], pad;
+  double sum, edge[2];
 };
 
-// The address in block `rank`'s shared memory of what lies at `p` in this block's.
-__device__ __forceinline__ uint32_t block_addr(const void* p, int rank) {
+// Writes x into the shared memory of block `rank`, to the place where `p` points in this one's.
+__device__ __forceinline__ void send_double(const double* p, int rank, double x) {
   uint32_t a;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
-  return a;
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(a), "d"(x) : "memory");
 }
-__device__ __forceinline__ void send_double(uint32_t to, double x, uint32_t bar) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(to),
-               "l"(__double_as_longlong(x)), "r"(bar)
-               : "memory");
+__device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // The bits of a value of a type known at run time, and the value.
 __device__ __forceinline__ uint32_t load_bits(const char* p, bool wide) {
@@ -1262,28 +1267,20 @@ __device__ __forceinline__ void segment_apply(const TensorsParams& prm, const Gr
 }
 
 // Bound by a chain of latencies: launch, table (read before the predecessor's
-// end is waited for), rows, join, one store into the other blocks, the factor, the second
-// pass out of shared memory.  20 tensors of 60k fp32 together: norm 3.4 us, clip 4.9, AdamW 6.4; with
-// the kernels above 5.0, 7.6 and 7.8.
+// end is waited for), rows, join, one store into the other blocks and their barrier, the factor, the
+// second pass out of shared memory.  20 tensors of 60k fp32 together: norm 3.6 us, clip 5.1, AdamW 6.6;
+// with the kernels above 5.0, 7.6 and 7.8.
 template <int NORM, int OP>
 __global__ void __launch_bounds__(kListWarps * 32, 1)
     tensors_cluster_kernel(const __grid_constant__ TensorsParams prm,
                            const __grid_constant__ GroupScalars groups, int rows) {
   extern __shared__ uint4 kept[];  // `rows` rows for each warp
   __shared__ BlockParts parts;
-  __shared__ BlockSums mine, all[kClusterBlocks];
-  __shared__ uint64_t bar;
+  __shared__ BlockSums all[kClusterBlocks];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int blocks = gridDim.x;
-  if (threadIdx.x == 0) {
-    mine.edge[0] = mine.edge[1] = 0.0;
-    mbar_init(&bar, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    mbar_expect_tx(&bar, blocks * 3 * sizeof(double));
-  }
-  __syncwarp();
   // the others' shared memory may be written once all blocks have come here
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  cluster_arrive();
   // the tables were there before any kernel of the stream
   const Segment opening = prm.opening[blockIdx.x * kListWarps + warp];
   Target target{};
@@ -1293,31 +1290,27 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
   Spanning span{-1, 0, 0, 0};
   if (w < prm.n_spanning) span = prm.spanning[w];
   uint4* keep = kept + warp * rows * 32 + lane;
-  __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_wait();
   grid_dependency_wait();
   double sum = warp_sum<NORM, OP != kOpNone, true>(prm, opening, parts, keep);
   if (lane == 0) parts.sum[warp] = sum;
   __syncthreads();
   double x;
-  const int known = join_parts<NORM>(prm, parts, mine.edge, x);
-  __syncthreads();  // the edges are written
+  const auto edge = [&](int k, double part) {
+    if (lane < blocks) send_double(&all[blockIdx.x].edge[k], lane, part);
+  };
+  const int known = join_parts<NORM>(prm, parts, edge, x);
   if (warp == 0) {
     sum = join_warps<NORM>(parts.sum);
-    if (lane < blocks) {
-      const uint32_t to = block_addr(&all[blockIdx.x], lane), at = block_addr(&bar, lane);
-      send_double(to, sum, at);
-      send_double(to + 8, mine.edge[0], at);
-      send_double(to + 16, mine.edge[1], at);
-    }
+    if (lane < blocks) send_double(&all[blockIdx.x].sum, lane, sum);
   }
+  cluster_arrive();
   if (known >= 0 && lane == 0) write_norm<NORM>(prm, known, x);
-  const bool ok = mbar_wait_bounded(&bar, 0);
+  cluster_wait();  // all sums are here, and nothing more is written into this block's shared memory
   grid_launch_dependents();
-  const double total = ok ? warp_join<NORM>(lane < blocks ? all[lane].sum : 0.0)
-                          : __longlong_as_double(0x7ff8000000000000ll);
+  const double total = warp_join<NORM>(lane < blocks ? all[lane].sum : 0.0);
   const Clip clip = clip_of(total, NORM, prm.scale, prm.max_norm);
-  const bool skip = !ok || OP == kOpNone || (OP == kOpAdamw && !clip.finite) ||
+  const bool skip = OP == kOpNone || (OP == kOpAdamw && !clip.finite) ||
                     (OP == kOpScale && prm.in_place && clip.factor == 1.f);
   if (!skip && opening.tensor >= 0) {
     if constexpr (OP != kOpNone) {
@@ -1332,7 +1325,7 @@ __global__ void __launch_bounds__(kListWarps * 32, 1)
       }
     }
   }
-  if (ok && span.tensor >= 0)
+  if (span.tensor >= 0)
     join_spanning<NORM>(prm, span, [&](int b, int k) { return all[b].edge[k]; });
   if (blockIdx.x == 0) {
     if (threadIdx.x == 0) write_clip(prm, total, clip);

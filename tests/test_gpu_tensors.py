@@ -376,6 +376,36 @@ def test_adamw_rows_of_every_width(width, dtype, layout):
         assert torch.equal(h, x.to(BF16))
 
 
+@pytest.mark.parametrize("blocks", range(1, 17))
+def test_cluster_of_every_size(blocks):
+    """Lists that fill 1 to 16 blocks of a cluster (8192 bytes each), with tensors that lie in one block,
+    reach into the next one, and go through all of them: each norm, and what every block makes of the
+    sum."""
+    g = gen(100 + blocks)
+    n = 2048 * blocks
+    for sizes in ((n,), (5, n - 5), (n - 5, 5), (n // 3, n // 3, n - 2 * (n // 3)), (700,) * (n // 700),
+                  (3, n - 2003, 1000, 1000)):
+        grads = [make((k,), F32, "dense", g, 0.1 * (i + 1)) for i, k in enumerate(sizes)]
+        before = [x.clone() for x in grads]
+        st = state_like([(k,) for k in sizes], g)
+        ref = [[x.double() for x in t] for t in st]
+        ts = absnt.GradTensors(grads, params=st[0], m=st[1], v=st[2])
+        for order in ORDERS:
+            absnt.abs_grad_norm(ts, norm_type=order)
+            check_norms(ts, grads, order)
+        absnt.abs_grad_adamw(ts, HP, 3, 0.5)
+        total = check_norms(ts, grads, 2)
+        factor = 0.5 / (total + 1e-6)
+        for i, x in enumerate(before):
+            w, m1, v1, e_p, e_m, e_v = adamw_ref(*(t[i] for t in ref), x.double() * factor, HP, 3)
+            for got, want, tol in zip((t[i] for t in st), (w, m1, v1), (e_p, e_m, e_v)):
+                assert ((got.double() - want).abs() <= tol).all()
+        absnt.abs_grad_clip(ts, 0.5)
+        check_norms(ts, before, 2)
+        for x, b in zip(grads, before):
+            check_scaled(x, b, factor, F32)
+
+
 def test_adamw_is_the_flat_call():
     """On one dense fp32 tensor, without clipping: the update of abs_adamw_step, bit for bit."""
     g = gen(9)
