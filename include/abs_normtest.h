@@ -491,7 +491,7 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  * "Gradient clipping 1.0" in the hyper-parameter tables of Appendix C).
  *
  *   x_t,i        element i of tensor t, and s = grad_scale, a factor known before the call
- *                (1/micro-batches, 1/loss scale; a float, not 0)
+ *                (1/micro-batches, 1/loss scale; in the range of a float, not 0 as one)
  *   N_t          the norm of s*x_t:  (sum_i |s x_t,i|^p)^(1/p) for p = 1, 2, or max_i |s x_t,i|
  *   N            the same norm over all tensors, (sum_t N_t^p)^(1/p) or max_t N_t
  *   c            min(1, max_norm / (N + 1e-6)), the clipping coefficient
@@ -502,9 +502,9 @@ int abs_schedule_advance(abs_schedule* s, int64_t b_test);
  * work area serves one call at a time: calls on it have to be ordered (one stream, or events).
  * Make the first call on a device outside of any stream capture; later ones may be captured.
  *
- * Range and accuracy: sums are held in fp64 (fp32 within 16 bytes of input); the norm of finite
- * gradients is right also where their fp32 squares overflow or vanish.  Results do not depend on
- * the order in which blocks run.  s c is rounded to float once (below 2^-126, for norms above 1e38
+ * Range and accuracy: sums are held in fp64 (at most eight values are added in fp32 first); the norm
+ * of finite gradients is right also where their fp32 squares overflow or vanish.  Results do not depend
+ * on the order in which blocks run.  s c is rounded to float once (below 2^-126, for norms above 1e38
  * max_norm, with fewer bits).  A norm that is not finite (a NaN or infinite gradient) raises
  * ABS_FLAG_NONFINITE in the header; c is then 1 and a clipping AdamW leaves params, m and v as they are.
  */
@@ -569,8 +569,8 @@ int abs_grad_norm(const void* plan, void* work, int norm_type, double grad_scale
                   float* norms_out, abs_stream_t stream);
 
 /*
- * Clipping by the global norm: y = (s c) x, rounded once to the type of y.  y is the gradient
- * itself, or the plan's `outs`.  max_norm finite, > 0.
+ * Clipping by the global norm: y = (s c) x, a product in fp32 that is then rounded to the type of y.
+ * y is the gradient itself, or the plan's `outs`.  max_norm finite, > 0.
  *   sum_in   NULL: the call computes the norm first (norms_out as above).  Else a double in device
  *            memory, the SUM over this and other ranks' tensors: no norm is computed, norms_out[0]
  *            and [1] and the header follow from it, norms_out[2..] are left.

@@ -659,7 +659,8 @@ class GradTensors:
 
       grads        CUDA tensors of any shapes, float32 / bfloat16 / float16 mixed: dense in any
                    order of dimensions, or with the strides of a matrix once neighbouring dimensions
-                   are merged (columns of a wider matrix, a transposed one).  Empty ones are fine.
+                   are merged (columns of a wider matrix, a transposed one).  Dimensions are merged in
+                   the parameter's order where there are params.  Empty ones are fine.
       out          same shapes, any of the types: abs_grad_clip writes there; None: in place
       params, m, v float32, same shapes, dense, all three in one order of dimensions: updated by
                    abs_grad_adamw, with the hyper-parameters of groups[i] (None: all group 0)
@@ -667,8 +668,10 @@ class GradTensors:
 
     The object keeps the plan of the list and its work area, and the results of the latest call:
     `norm` (global norm, one float32), `coef` (clipping coefficient), `norms` (one per tensor).
-    Built once for tensors that stay where they are (a training loop's buckets and state); build
-    another when a gradient moves.  Calls on one object have to be ordered: one stream, or events
+    Built once for tensors that stay where they are (a training loop's buckets and state; gradients
+    that zero_grad(set_to_none=False) zeroes in place); it costs many times a call.  A gradient that
+    moves (set_to_none=True) is not noticed: the object keeps the old tensor and goes on working on
+    it, so build another one then.  Calls on one object have to be ordered: one stream, or events
     between streams."""
 
     def __init__(self, grads, out=None, params=None, m=None, v=None, params_bf16=None, groups=None):

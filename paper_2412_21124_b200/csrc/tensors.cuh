@@ -221,8 +221,8 @@ __device__ __forceinline__ float max_abs(float acc, float x) {
   return r;
 }
 
-// Running sum of one thread: |x|, x^2 or max |x|.  The values of a 16-byte vector are added in
-// fp32 (their products of 8-bit significands are exact there), the vectors in fp64.
+// Running sum of one thread: |x|, x^2 or max |x|.  The values of a 16-byte vector, or eight of a view
+// with rows, are added in fp32 (products of 8-bit significands are exact there), the rest in fp64.
 template <int NORM>
 struct NormAcc {
   double s = 0.0;
@@ -271,7 +271,7 @@ __device__ __forceinline__ uint4 ld_grad_16(const void* p) {
 
 // One lane's share of a segment.  KEEP: its rows are also left in shared memory, at `keep` (this
 // lane's place in row 0), one after the other.  SMALL: fewer loads at once, for lists of a few rows a
-// warp, where fetching the instructions of a larger body is what shows (60k elements: 3.5 -> 3.4 us).
+// warp, where fetching the instructions of a larger body is what shows (60k elements: 0.1 us of 3.5).
 template <typename T, int NORM, bool KEEP, bool SMALL>
 __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, const Segment& s,
                                                      uint32_t lane, uint4* keep) {
@@ -324,7 +324,10 @@ __device__ __forceinline__ NormAcc<NORM> segment_acc(const TensorsParams& prm, c
       return acc;
     }
     // 24 at once: few bytes are under way with single elements (30M fp16 in column slices, from
-    // memory: 16, 24, 32 at once 32.4, 29.9, 30.3 us; dense 15.7)
+    // memory: 16, 24, 32 at once 32.4, 29.9, 30.3 us; dense 15.7).  The registers are those of the whole
+    // kernel, 128 instead of 96 for 16 at once.  What that does to dense lists (us, 16 / 24): norm of 1.5M
+    // bf16 5.7 / 5.8, 4M 5.8 / 5.8, 50M fp16 17.3 / 17.2, 300M bf16 89.1 / 89.2; with scaling 8.9 / 8.6,
+    // 9.8 / 9.8, 48.5 / 48.3, 279.6 / 279.7, and 16M fp16 15.8 / 16.1
     constexpr int kWalk = SMALL ? 8 : 24;
     Walk<int32_t> w = grad_walk<int32_t>(e, s.start + lane, 32);
     g += w.base;
@@ -862,13 +865,15 @@ __device__ __forceinline__ void unit_scale(const TensorEntry& e, const UnitRange
   }
 }
 
-// y = factor * x, rounded once to y's type.  Bound by reading x again and writing y: a list that is
+// y = factor * x in fp32, rounded to y's type.  Bound by reading x again and writing y: a list that is
 // larger than what stays on chip is read twice, since the factor needs the whole norm.  One CTA per
 // unit, the last unit of the list first.  After this call's norm kernel the first loads are made before
 // the factor is waited for: that kernel lets this one start only after its own wait, so whatever wrote
-// the tensors before is done.  Four CTAs of 64 registers to an SM, against three of 80, norm and scaling
-// (us): 4M bf16 9.7 / 10.6, 16M fp16 16 / 18, 50M fp16 48.1 / 49.0, 300M bf16 279.5 / 279.0, 1.24G fp32
-// into bf16 1832 / 1818.
+// the tensors before is done.  Four CTAs of 64 registers to an SM (a thread spills 56
+// bytes), against three of 80, norm and scaling (us): 4M bf16 9.7 / 10.6, 16M fp16 16 / 18, 50M fp16
+// 48.1 / 49.0, 300M bf16 279.5 / 279.0, 1.24G fp32 into bf16 1832 / 1818.  The norm kernel's blocks of sums
+// (128 registers x 512 threads, all of an SM) leave no room beside them, so what runs early are the CTAs on
+// SMs whose block has ended; beside its blocks of maxima (101 registers) one fits neither.
 // Norm and scaling of 124M bf16 into bf16: 121 us = 6.2 TB/s of the 747 MB that they move; 1.24G fp32
 // into bf16: 1.84 ms = 6.7 TB/s of 12.4 GB.  Measured and dropped: one cooperative kernel in which each
 // warp scales what it read itself, with its last rows kept in shared memory (167 us and 2.5 ms: the

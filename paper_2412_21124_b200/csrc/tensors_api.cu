@@ -75,7 +75,7 @@ struct WorkLayout {
 // How the rows of a list are dealt out, a function of the list's sizes alone (and with it the shape of
 // every sum).  Lists of up to 2 MiB and 384 tensors go to the warps of one cluster, others to the
 // warps of all SMs.  Measured (fp32, us, cluster against all SMs): 60k elements in 20 tensors, norm
-// 3.4 / 5.0, clip 5.0 / 7.6; 500k: 4.3 / 5.4 and 8.7 / 9.1; 400 tensors of 100 elements: 5.1 / 5.0 and
+// 3.5 / 5.0, clip 5.0 / 7.6; 500k: 4.3 / 5.4 and 8.7 / 9.1; 400 tensors of 100 elements: 5.1 / 5.0 and
 // 7.1 / 7.0; 1600 tensors: 10.5 / 5.6 and 18.1 / 11.7.
 constexpr int kClusterTensors = 384;
 constexpr int64_t kRowBytes = 512;
