@@ -51,7 +51,10 @@ typedef void* abs_stream_t; /* a cudaStream_t */
 typedef enum {
   ABS_F32 = 0,
   ABS_BF16 = 1,
-  ABS_F16 = 2 /* only in abs_tensor lists; the calls on flat vectors answer ABS_ERR_DTYPE */
+  ABS_F16 = 2,  /* only in abs_tensor lists and in rows; the calls on flat vectors answer ABS_ERR_DTYPE */
+  ABS_E4M3 = 3, /* 8 bits, results with scales only: up to 448                                        */
+  ABS_E5M2 = 4, /* the same, up to 57344                                                              */
+  ABS_E8M0 = 5  /* a scale that is a power of two: the byte e + 127, 255 for NaN                      */
 } abs_dtype;
 
 typedef enum {
@@ -590,6 +593,103 @@ int abs_grad_clip(const void* plan, void* work, int norm_type, double grad_scale
 int abs_grad_adamw(const void* plan, void* work, const abs_adamw_hparams* hparams, int n_groups,
                    int64_t step, int norm_type, double grad_scale, double max_norm,
                    const double* sum_in, float* norms_out, abs_stream_t stream);
+
+/*
+ * ---- Norms of a model's layers ----------------------------------------------------------
+ * The root-mean-square norm (the models of Table 4 have two a layer) and its backward pass, on rows of
+ * matrices as layers hold them.  The backward pass can keep the weight's gradient of every sample of a packed
+ * batch apart: those are rows of the matrix that abs_persample_norm_test reads.
+ *
+ * A tensor is n0 x n1 rows of h values, the values of a row side by side; n1 is 1 for a plain matrix, the number
+ * of heads for queries and keys.  n0 n1 < 2^31, h at most ABS_MAX_NORM_WIDTH (ABS_ERR_TOO_LARGE).
+ */
+typedef struct {
+  void* data;      /* device, aligned to its element size; NULL: not given                                  */
+  int64_t stride0; /* elements from row (i, j) to (i + 1, j) and to (i, j + 1), >= 0; inputs may be         */
+  int64_t stride1; /* broadcast (0); that of a dimension of one is not looked at                            */
+  int32_t dtype;   /* an abs_dtype                                                                          */
+  int32_t reserved; /* 0                                                                                    */
+} abs_rows;
+
+enum { ABS_MAX_NORM_WIDTH = 16384, ABS_MAX_SAMPLES = 1 << 20 };
+#define ABS_MIN_NORM_EPS 1e-30
+
+/*
+ *   s = x + residual          (without residual: s = x), in fp32, not rounded before it is normalised
+ *   y_c = s_c w_c / sqrt(sum_i s_i^2 / h + eps)
+ *
+ * sum gets s rounded once, out gets y: rounded once, or in 8 bits with a scale for every `group` columns (32, 64,
+ * 128; the last group of a row may be shorter) or one for the row (0).  With a = max |y| of the group and M = 448
+ * (ABS_E4M3) or 57344 (ABS_E5M2):
+ *   scales of ABS_F32    a / M (at least 2^-126)
+ *   scales of ABS_E8M0   the smallest power of two that is not below a / M (at least 2^-127)
+ * and the value is y / scale, rounded to nearest.  A group of zeros has the scale 1; one that holds an infinity or a
+ * NaN has the scale NaN and all its values are NaN.  The scale of group g of row (i, j) goes to element
+ * i stride0 + j stride1 + g scale_stride2 of `scales`.
+ *
+ *   x         ABS_F32, ABS_BF16 or ABS_F16
+ *   residual  x's type or ABS_F32, or not given
+ *   sum       residual's type, or not given
+ *   out       any of the three types, or ABS_E4M3 / ABS_E5M2
+ *   weight    h contiguous values of one of the three types; NULL: ones
+ *   eps       ABS_MIN_NORM_EPS .. 1e30
+ * sum and out may each be x or residual themselves (same address, strides and type); otherwise no output may
+ * share a byte with anything else (ABS_ERR_ALIAS): exactly for tensors of the same strides, columns of one matrix; by
+ * their address ranges for others.  Sums of squares beyond the range of a float are formed scaled: finite
+ * rows have finite results.  No rows: nothing is done.  One launch, bound by reading and writing everything once.
+ */
+typedef struct {
+  int64_t n0, n1, h;
+  abs_rows x, residual, sum, out, scales;
+  int64_t scale_stride2;
+  const void* weight;
+  int32_t weight_dtype;
+  int32_t group;
+  double eps;
+} abs_rms_norm_args;
+int abs_rms_norm(const abs_rms_norm_args* args, abs_stream_t stream);
+
+/*
+ * With u_c = s_c / sqrt(sum_i s_i^2 / h + eps), which is formed again from s (what the forward pass wrote to
+ * `sum`, or its x), and g_c = dy_c w_c:
+ *   dx_c = (g_c - u_c sum_i g_i u_i / h) / sqrt(..) + dresidual_c       the gradient of s, so of x and residual both
+ *   dweight_c = sum over all rows of dy_c u_c
+ *   row b of dweight_samples = sample_scale * the same sum over the rows of sample b
+ *
+ *   dy               ABS_F32, ABS_BF16 or ABS_F16
+ *   s                dy's type or ABS_F32
+ *   dresidual        s's type: the gradient that reaches s past the norm; or not given
+ *   dx               any of the three types; may be dy, s or dresidual themselves
+ *   offsets          device, n_samples + 1 non-decreasing numbers: sample b is the rows (i, j) with
+ *                    offsets[b] <= i < offsets[b+1].  Rows before the first and behind the last sample are neither
+ *                    read nor written.  NULL with n_samples 0: all rows.  Offsets outside of 0..n0 are
+ *                    taken as the nearest of the two
+ *   dweight          device, h floats, or NULL
+ *   dweight_samples  device, n_samples rows of h floats, samples_ld floats apart, or NULL (needs offsets).  With a
+ *                    loss that is a mean over n_samples samples and sample_scale = n_samples its rows are the
+ *                    gradients of the samples' own losses, whose mean is dweight
+ *   work             device, abs_rms_norm_grad_bytes(...) bytes, 32-byte aligned, where one of the two sums is asked
+ *                    for (ABS_ERR_TOO_LARGE if work_bytes is less).  Nothing in it outlives the call; calls that
+ *                    may overlap need one each
+ * Sums over rows are formed in fp32 in an order that depends on the shapes and offsets alone.  Where a sample
+ * has no rows, and where there are no rows at all, sums are 0.  One launch, two with a sum.
+ */
+typedef struct {
+  int64_t n0, n1, h;
+  abs_rows dy, s, dresidual, dx;
+  const void* weight;
+  const int32_t* offsets;
+  float* dweight;
+  float* dweight_samples;
+  void* work;
+  int64_t n_samples, samples_ld, work_bytes;
+  double eps, sample_scale;
+  int32_t weight_dtype;
+  int32_t reserved;
+} abs_rms_norm_grad_args;
+/* 0 on invalid arguments.  Host, pure. */
+size_t abs_rms_norm_grad_bytes(int64_t n0, int64_t n1, int64_t h, int64_t n_samples);
+int abs_rms_norm_grad(const abs_rms_norm_grad_args* args, abs_stream_t stream);
 
 /*
  * Self-test of the bounded waits (no counterpart in the paper).  The staged kernels wait for

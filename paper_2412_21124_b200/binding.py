@@ -8,13 +8,14 @@ There is no CPU fallback: if the library has not been built, the first call rais
 import ctypes
 import math
 import os
+import struct
 
 import numpy as np
 import torch
 
 from . import build as _build
 
-ABS_F32, ABS_BF16, ABS_F16 = 0, 1, 2
+ABS_F32, ABS_BF16, ABS_F16, ABS_E4M3, ABS_E5M2, ABS_E8M0 = range(6)
 ABS_OK = 0
 ABS_ERR_NULL, ABS_ERR_RANGE, ABS_ERR_SHARDS, ABS_ERR_ALIGN, ABS_ERR_DTYPE, ABS_ERR_CUDA = (
     -1, -2, -3, -4, -5, -6)
@@ -28,6 +29,7 @@ ABS_STATS_HEADER, ABS_SHARD_STRIDE = 8, 4
 ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE, ABS_FLAG_VIOLATED = 1, 2, 4
 ABS_MAX_GROUPS, ABS_MAX_TENSORS = 16, 1 << 20
 ABS_NORM_MAX, ABS_NORM_1, ABS_NORM_2 = 0, 1, 2
+ABS_MAX_NORM_WIDTH, ABS_MAX_SAMPLES = 16384, 1 << 20
 ABS_GRAD_SUM, ABS_GRAD_NORM, ABS_GRAD_COEF, ABS_GRAD_FLAGS = 0, 1, 2, 4
 
 
@@ -135,6 +137,12 @@ def lib():
     L.abs_grad_clip.argtypes = [ptr, ptr, cint, dbl, dbl, ptr, ptr, ptr]
     L.abs_grad_adamw.restype = cint
     L.abs_grad_adamw.argtypes = [ptr, ptr, ptr, cint, i64, cint, dbl, dbl, ptr, ptr, ptr]
+    L.abs_rms_norm.restype = cint
+    L.abs_rms_norm.argtypes = [ptr, ptr]
+    L.abs_rms_norm_grad.restype = cint
+    L.abs_rms_norm_grad.argtypes = [ptr, ptr]
+    L.abs_rms_norm_grad_bytes.restype = sz
+    L.abs_rms_norm_grad_bytes.argtypes = [i64, i64, i64, i64]
     L.abs_selftest_bounded_wait.restype = cint
     L.abs_selftest_bounded_wait.argtypes = [cint, ptr, ptr]
     L.abs_status_string.restype = ctypes.c_char_p
@@ -841,6 +849,175 @@ def abs_grad_adamw(tensors, hparams, step, max_norm=0.0, norm_type=2, grad_scale
     if rc != ABS_OK:
         raise AbsError(rc, "abs_grad_adamw")
     return tensors.norm if max_norm else None
+
+
+# ------------------------------------------------------------------------ rows of matrices
+_ROW_DTYPES = {torch.float32: ABS_F32, torch.bfloat16: ABS_BF16, torch.float16: ABS_F16,
+               torch.float8_e4m3fn: ABS_E4M3, torch.float8_e5m2: ABS_E5M2,
+               torch.float8_e8m0fnu: ABS_E8M0}
+# abs_rows, abs_rms_norm_args and abs_rms_norm_grad_args as struct packs them: native alignment, as in C
+_ROWS = "Pqqii"
+_NO_ROWS = (0, 0, 0, 0, 0)
+_NORM_ARGS = struct.Struct("@3q" + 5 * _ROWS + "qPiid")
+_NORM_GRAD_ARGS = struct.Struct("@3q" + 4 * _ROWS + "5P3q2dii")
+
+
+def _row_shape(t, name):
+    """(n0, n1, h) of a tensor of one to three dimensions whose rows lie along the last."""
+    shape = t.shape
+    if len(shape) == 2:
+        return shape[0], 1, shape[1]
+    if len(shape) == 3:
+        return tuple(shape)
+    if len(shape) == 1:
+        return 1, 1, shape[0]
+    raise TypeError("%s: 1 to 3 dimensions, rows along the last, got shape %s" % (name, tuple(shape)))
+
+
+def _row_fields(t, shape, device, name):
+    """The abs_rows of a tensor that has to have this shape and live on this device."""
+    if t is None:
+        return _NO_ROWS
+    if t.shape != shape:
+        raise ValueError("%s: shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.get_device() != device:
+        _check_one_device(t)
+        raise ValueError("%s must be a CUDA tensor" % name)
+    code = _ROW_DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError("%s must not be %s" % (name, t.dtype))
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
+        raise TypeError("%s: the values of a row must lie side by side" % name)
+    return (t.data_ptr(), stride[0] if len(stride) > 1 else 0, stride[1] if len(stride) > 2 else 0, code, 0)
+
+
+def _flat_pointer(t, dtype, numel, device, name):
+    """The address of a contiguous tensor of one type and (unless numel is None) length; 0 for None."""
+    if t is None:
+        return 0
+    if t.get_device() != device:
+        _check_one_device(t)
+        raise ValueError("%s must be a CUDA tensor" % name)
+    if t.dtype != dtype or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise TypeError("%s must be a contiguous %s tensor%s"
+                        % (name, dtype, "" if numel is None else " of %d values" % numel))
+    return t.data_ptr()
+
+
+def _weight_fields(weight, h, device):
+    if weight is None:
+        return 0, ABS_F32
+    code = _ROW_DTYPES.get(weight.dtype, ABS_E8M0)
+    if code > ABS_F16:
+        raise TypeError("weight must not be %s" % weight.dtype)
+    return _flat_pointer(weight, weight.dtype, h, device, "weight"), code
+
+
+def _raw_stream(stream, device):
+    """The stream of a call as a number; without torch's stream object, which would cost more than the call."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream).value or 0
+
+
+def abs_rms_norm(x, weight, out, eps=1e-6, residual=None, sum_out=None, scales_out=None, group=0,
+                 stream=None):
+    """out = root-mean-square norm of the rows (last dimension) of x + residual, times weight (None: ones).
+
+      x, residual, sum_out, out   the same shape, one to three dimensions, any strides but a row's own: columns
+                                  of a fused projection, heads [tokens, heads, width], a sliced batch
+      residual    x's type or float32; sum_out (its type) gets x + residual, for the next layer and for
+                  abs_rms_norm_grad.  sum_out and out may be x or residual themselves
+      out         float32 / bfloat16 / float16; or float8_e4m3fn / float8_e5m2 with scales_out, of the shape
+                  x.shape[:-1] + (ceil(width / group),), or (1,) with group 0: float32, or float8_e8m0fnu for powers
+                  of two.  out * its scale is the value.  group: 32, 64, 128, or 0 for a scale a row
+
+    Returns out."""
+    device = torch._C._cuda_getDevice()
+    shape = x.shape
+    n0, n1, h = _row_shape(x, "x")
+    scales, scale_stride = _NO_ROWS, 0
+    if scales_out is not None:
+        groups = -(-h // group) if group > 0 else 1
+        scales = _row_fields(scales_out, shape[:-1] + (groups,), device, "scales_out") if groups == 1 or \
+            scales_out.stride(-1) == 1 else _apart(scales_out, shape[:-1] + (groups,), device)
+        scale_stride = scales_out.stride(-1)
+    w, w_code = _weight_fields(weight, h, device)
+    args = _NORM_ARGS.pack(
+        n0, n1, h, *_row_fields(x, shape, device, "x"), *_row_fields(residual, shape, device, "residual"),
+        *_row_fields(sum_out, shape, device, "sum_out"), *_row_fields(out, shape, device, "out"), *scales,
+        scale_stride, w, w_code, group, eps)
+    rc = lib().abs_rms_norm(args, _raw_stream(stream, device))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_rms_norm")
+    return out
+
+
+def _apart(scales, shape, device):
+    """Scales whose groups do not lie side by side (a transposed matrix of them): described by their first group."""
+    if scales.shape != shape:
+        raise ValueError("scales_out: shape %s, expected %s" % (tuple(scales.shape), tuple(shape)))
+    return _row_fields(scales[..., :1], shape[:-1] + (1,), device, "scales_out")
+
+
+def abs_rms_norm_grad_bytes(n0, n1, h, n_samples=0):
+    return int(lib().abs_rms_norm_grad_bytes(int(n0), int(n1), int(h), int(n_samples)))
+
+
+def alloc_rms_norm_work(s, n_samples=0):
+    """A work area for abs_rms_norm_grad on tensors of s's shape and at most n_samples samples."""
+    nbytes = abs_rms_norm_grad_bytes(*_row_shape(s, "s"), n_samples)
+    if nbytes == 0:
+        raise ValueError("invalid shape or number of samples")
+    return torch.empty(nbytes, dtype=torch.uint8, device=s.device)
+
+
+def abs_rms_norm_grad(dy, s, weight, dx, dweight, eps=1e-6, dresidual=None, offsets=None,
+                      dweight_samples=None, sample_scale=1.0, work=None, stream=None):
+    """Backward pass of abs_rms_norm: dx (the gradient of s, so of x and of residual) and dweight.
+
+      dy, s, dresidual, dx  one shape; s is what the forward pass wrote to sum_out (or its x), dresidual the gradient
+                            that reaches s past the norm.  dx may be dy, s or dresidual themselves
+      dweight          [h] float32, or None
+      offsets          int32 [samples + 1] on the GPU: sample b is dy[offsets[b]:offsets[b + 1]].  Rows of no
+                       sample are left as they are
+      dweight_samples  [samples, h] float32, rows any distance apart (columns of the matrix of a whole model), for
+                       abs_persample_norm_test: sample_scale times each sample's part of dweight.  Pass the number
+                       of samples for a loss that is their mean
+      work             alloc_rms_norm_work(s, samples), for dweight and dweight_samples
+
+    Returns dx."""
+    device = torch._C._cuda_getDevice()
+    shape = s.shape
+    n0, n1, h = _row_shape(s, "s")
+    w, w_code = _weight_fields(weight, h, device)
+    samples, table = 0, 0
+    if offsets is not None:
+        if offsets.dim() != 1 or offsets.numel() < 2:
+            raise TypeError("offsets must hold samples + 1 numbers")
+        samples = offsets.numel() - 1
+        table = _flat_pointer(offsets, torch.int32, None, device, "offsets")
+    apart, ld = 0, h
+    if dweight_samples is not None:
+        if offsets is None:
+            raise ValueError("dweight_samples needs offsets")
+        _, ld, _, code, _ = fields = _row_fields(dweight_samples, (samples, h), device, "dweight_samples")
+        if code != ABS_F32:
+            raise TypeError("dweight_samples must be float32")
+        apart, ld = fields[0], ld if samples > 1 else h
+    area, nbytes = 0, 0
+    if work is not None:
+        area, nbytes = _flat_pointer(work, work.dtype, None, device, "work"), work.numel() * work.element_size()
+    args = _NORM_GRAD_ARGS.pack(
+        n0, n1, h, *_row_fields(dy, shape, device, "dy"), *_row_fields(s, shape, device, "s"),
+        *_row_fields(dresidual, shape, device, "dresidual"), *_row_fields(dx, shape, device, "dx"), w, table,
+        _flat_pointer(dweight, torch.float32, h, device, "dweight"), apart, area, samples, ld, nbytes, eps,
+        sample_scale, w_code, 0)
+    rc = lib().abs_rms_norm_grad(args, _raw_stream(stream, device))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_rms_norm_grad")
+    return dx
 
 
 def abs_decide(S, n2, norm, eta, b_cur):

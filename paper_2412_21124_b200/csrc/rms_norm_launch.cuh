@@ -1,0 +1,120 @@
+// Which kernel a call of abs_rms_norm or abs_rms_norm_grad runs.  The functions are instantiated once for
+// each type of x (dy) in a translation unit of its own, rms_norm_inst.cu.
+#pragma once
+#include "launch.cuh"
+#include "rms_norm_grad.cuh"
+
+namespace absnt {
+
+constexpr int kSMs = 148;
+// the widest row: 32 warps of 16 values a lane
+constexpr int kMaxNormWidth = 32 * 32 * 16;
+
+// ---- forward
+template <int XT, int RT, int VEC, int L, int NI, int NR>
+cudaError_t norm_by_lanes(const NormParams& p, cudaStream_t st) {
+  const uint32_t per_block = 8 * (32 / L) * NR;
+  return launch_pdl(rms_norm_kernel<XT, RT, VEC, L, NI, NR, false>, dim3((p.rows + per_block - 1) / per_block),
+                    dim3(32, 8), st, p);
+}
+template <int XT, int RT, int VEC, int NI>
+cudaError_t norm_by_block(const NormParams& p, cudaStream_t st) {
+  constexpr int cols = 32 * lane_values<VEC>() * NI;  // of a warp
+  return launch_pdl(rms_norm_kernel<XT, RT, VEC, 32, NI, 1, true>, dim3(p.rows), dim3(32 * ((p.h + cols - 1) / cols), 1), st, p);
+}
+template <int XT, int RT>
+cudaError_t norm_vec(const NormParams& p, int vec, cudaStream_t st) {
+  const int h = p.h;
+  // A call of fewer rows than SMs is bound by the latency of one row: as many threads a row as there are
+  // pieces.  Otherwise a thread holds up to 32 values, so that few threads wait for one another.
+  const bool few = p.rows <= kSMs;
+  if (vec == 8) {
+    if (h <= 64) return norm_by_lanes<XT, RT, 8, 8, 1, 4>(p, st);
+    if (h <= 128) return norm_by_lanes<XT, RT, 8, 16, 1, 4>(p, st);
+    if (h <= 256) return norm_by_lanes<XT, RT, 8, 32, 1, 2>(p, st);
+    if (few && h <= 8192) return norm_by_block<XT, RT, 8, 1>(p, st);
+    if (h <= 512) return norm_by_lanes<XT, RT, 8, 32, 2, 1>(p, st);
+    if (h <= 1024) return norm_by_lanes<XT, RT, 8, 32, 4, 1>(p, st);
+    return norm_by_block<XT, RT, 8, 4>(p, st);
+  }
+  if (vec == 4) {
+    if (h <= 128) return norm_by_lanes<XT, RT, 4, 32, 1, 4>(p, st);
+    if (few && h <= 4096) return norm_by_block<XT, RT, 4, 1>(p, st);
+    if (h <= 512) return norm_by_lanes<XT, RT, 4, 32, 4, 1>(p, st);
+    return norm_by_block<XT, RT, 4, 4>(p, st);
+  }
+  if (h <= 128) return norm_by_lanes<XT, RT, 1, 32, 1, 4>(p, st);
+  if (few && h <= 4096) return norm_by_block<XT, RT, 1, 1>(p, st);
+  if (h <= 512) return norm_by_lanes<XT, RT, 1, 32, 4, 1>(p, st);
+  return norm_by_block<XT, RT, 1, 4>(p, st);
+}
+// r_dtype < 0: no residual
+template <int XT>
+cudaError_t launch_norm(const NormParams& p, int r_dtype, int vec, cudaStream_t st) {
+  if (r_dtype < 0) return norm_vec<XT, -1>(p, vec, st);
+  if (r_dtype == XT) return norm_vec<XT, XT>(p, vec, st);
+  return norm_vec<XT, ABS_F32>(p, vec, st);
+}
+
+// ---- backward
+// Blocks of the kernel that sums over rows: three of 256 threads on an SM (four where a row takes few
+// registers), or one of more.
+inline int64_t grad_blocks(int64_t rows, int64_t h) {
+  const int64_t most = kSMs * (h <= 512 ? 4 : h <= 4096 ? 3 : 1);
+  return rows < most ? rows : most;
+}
+inline int64_t record_pitch(int64_t h) { return (h + 7) / 8 * 8; }  // VEC 8 writes 32 bytes at once
+
+template <int GT, int ST, int VEC, int L, int NI>
+cudaError_t grad_by_lanes(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
+  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, L, NI, false, 256>, dim3(static_cast<unsigned>(blocks)),
+                    dim3(32, 8), st, p);
+}
+template <int GT, int ST, int VEC>
+cudaError_t grad_by_block(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
+  constexpr int NI = grad_pieces<VEC>();
+  constexpr int cols = 32 * lane_values<VEC>() * NI;
+  static_assert(cols == 512, "grad_blocks counts on it");
+  const int warps = (p.h + cols - 1) / cols;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  if (warps <= 8)
+    return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 256>, grid, dim3(32 * warps, 8 / warps), st, p);
+  if (warps <= 16)
+    return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 512>, grid, dim3(32 * warps, 1), st, p);
+  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 1024>, grid, dim3(32 * warps, 1), st, p);
+}
+template <int GT, int ST>
+cudaError_t grad_vec(const NormGradParams& p, int64_t blocks, int vec, cudaStream_t st) {
+  const int h = p.h;
+  if (vec == 8) {
+    if (h <= 64) return grad_by_lanes<GT, ST, 8, 8, 1>(p, blocks, st);
+    if (h <= 128) return grad_by_lanes<GT, ST, 8, 16, 1>(p, blocks, st);
+    if (h <= 256) return grad_by_lanes<GT, ST, 8, 32, 1>(p, blocks, st);
+    if (h <= 512) return grad_by_lanes<GT, ST, 8, 32, 2>(p, blocks, st);
+    return grad_by_block<GT, ST, 8>(p, blocks, st);
+  }
+  if (vec == 4) {
+    if (h <= 128) return grad_by_lanes<GT, ST, 4, 32, 1>(p, blocks, st);
+    if (h <= 512) return grad_by_lanes<GT, ST, 4, 32, 4>(p, blocks, st);
+    return grad_by_block<GT, ST, 4>(p, blocks, st);
+  }
+  if (h <= 128) return grad_by_lanes<GT, ST, 1, 32, 1>(p, blocks, st);
+  if (h <= 512) return grad_by_lanes<GT, ST, 1, 32, 4>(p, blocks, st);
+  return grad_by_block<GT, ST, 1>(p, blocks, st);
+}
+template <int GT>
+cudaError_t launch_norm_grad(const NormGradParams& p, int s_dtype, int64_t blocks, int vec, cudaStream_t st) {
+  if (s_dtype == GT) return grad_vec<GT, GT>(p, blocks, vec, st);
+  return grad_vec<GT, ABS_F32>(p, blocks, vec, st);
+}
+
+#ifndef ABS_INST_XT
+extern template cudaError_t launch_norm<ABS_F32>(const NormParams&, int, int, cudaStream_t);
+extern template cudaError_t launch_norm<ABS_BF16>(const NormParams&, int, int, cudaStream_t);
+extern template cudaError_t launch_norm<ABS_F16>(const NormParams&, int, int, cudaStream_t);
+extern template cudaError_t launch_norm_grad<ABS_F32>(const NormGradParams&, int, int64_t, int, cudaStream_t);
+extern template cudaError_t launch_norm_grad<ABS_BF16>(const NormGradParams&, int, int64_t, int, cudaStream_t);
+extern template cudaError_t launch_norm_grad<ABS_F16>(const NormGradParams&, int, int64_t, int, cudaStream_t);
+#endif
+
+}  // namespace absnt

@@ -1,0 +1,169 @@
+"""CPU-side checks of the calls on rows of matrices: every refusal comes before the first CUDA call.  As in
+test_abi_cpu.py, no device is visible while fabricated addresses are handed over: a call that its checks
+let through answers ABS_ERR_CUDA."""
+import itertools
+import os
+import random
+
+import pytest
+
+import __graft_entry__ as entry
+from paper_2412_21124_b200 import binding as B
+
+FAKE = 0x1000000
+LET_THROUGH = B.ABS_ERR_CUDA
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _no_visible_device():
+    old = os.environ.get("CUDA_VISIBLE_DEVICES")
+    os.environ["CUDA_VISIBLE_DEVICES"] = ""
+    yield
+    if old is None:
+        os.environ.pop("CUDA_VISIBLE_DEVICES", None)
+    else:
+        os.environ["CUDA_VISIBLE_DEVICES"] = old
+
+
+@pytest.fixture(scope="module")
+def L():
+    entry.build()
+    return B.lib()
+
+
+def far(i):
+    return FAKE + i * 0x10000000
+
+
+def rows(data=FAKE, s0=64, s1=0, dtype=B.ABS_F32, reserved=0):
+    return (data, s0, s1, dtype, reserved)
+
+
+NONE = (0, 0, 0, 0, 0)
+
+
+def norm(L, n0=10, n1=1, h=64, x=rows(far(1)), residual=NONE, sum=NONE, out=rows(far(2)), scales=NONE, stride2=0, weight=0,
+         w_dtype=0, group=0, eps=1e-6):
+    return L.abs_rms_norm(B._NORM_ARGS.pack(n0, n1, h, *x, *residual, *sum, *out, *scales, stride2, weight, w_dtype, group, eps),
+                          None)
+
+
+def grad(L, n0=10, n1=1, h=64, dy=rows(far(1)), s=rows(far(2)), add=NONE, dx=rows(far(3)), weight=0, offsets=0, dw=0, apart=0,
+         work=0, n_samples=0, ld=64, work_bytes=0, eps=1e-6, scale=1.0, w_dtype=0):
+    return L.abs_rms_norm_grad(B._NORM_GRAD_ARGS.pack(n0, n1, h, *dy, *s, *add, *dx, weight, offsets, dw, apart, work, n_samples,
+                                                      ld, work_bytes, eps, scale, w_dtype, 0), None)
+
+
+def test_argument_blocks_are_those_of_the_header():
+    assert (B._NORM_ARGS.size, B._NORM_GRAD_ARGS.size) == (216, 240)
+
+
+E4 = rows(far(2), dtype=B.ABS_E4M3)
+SC = rows(far(5), s0=1)
+MX = rows(far(5), s0=2, dtype=B.ABS_E8M0)
+
+
+@pytest.mark.parametrize("change,status", [
+    ({}, LET_THROUGH),
+    (dict(n0=0), B.ABS_OK), (dict(n1=0, x=NONE, out=NONE), B.ABS_OK),
+    (dict(n0=-1), B.ABS_ERR_RANGE), (dict(h=0), B.ABS_ERR_RANGE), (dict(n0=1 << 31), B.ABS_ERR_RANGE),
+    (dict(n0=1 << 20, n1=1 << 20), B.ABS_ERR_RANGE),
+    (dict(h=16385, x=rows(far(1), s0=16385), out=rows(far(2), s0=16385)), B.ABS_ERR_TOO_LARGE),
+    (dict(x=NONE), B.ABS_ERR_NULL), (dict(out=NONE), B.ABS_ERR_NULL), (dict(sum=rows(far(3))), B.ABS_ERR_NULL),
+    (dict(x=rows(far(1), dtype=6)), B.ABS_ERR_DTYPE), (dict(x=rows(far(1), dtype=B.ABS_E4M3)), B.ABS_ERR_DTYPE),
+    (dict(out=rows(far(2), dtype=B.ABS_E8M0)), B.ABS_ERR_DTYPE),
+    (dict(residual=rows(far(3), dtype=B.ABS_BF16)), B.ABS_ERR_DTYPE),
+    (dict(x=rows(far(1), dtype=B.ABS_BF16), residual=rows(far(3))), LET_THROUGH),
+    (dict(residual=rows(far(3)), sum=rows(far(4), dtype=B.ABS_BF16)), B.ABS_ERR_DTYPE),
+    (dict(x=rows(far(1) + 2)), B.ABS_ERR_ALIGN), (dict(x=rows(far(1) + 2, dtype=B.ABS_BF16)), LET_THROUGH),
+    (dict(x=rows(far(1), s0=-64)), B.ABS_ERR_RANGE), (dict(x=rows(far(1), reserved=1)), B.ABS_ERR_RANGE),
+    (dict(x=rows(far(1), s0=1 << 45)), B.ABS_ERR_RANGE), (dict(x=rows(far(1), s0=0)), LET_THROUGH),
+    (dict(out=rows(far(2), s0=0)), B.ABS_ERR_ALIAS), (dict(out=rows(far(2), s0=63)), B.ABS_ERR_ALIAS),
+    (dict(n0=1, out=rows(far(2), s0=0)), LET_THROUGH),
+    (dict(eps=0.0), B.ABS_ERR_RANGE), (dict(eps=float("nan")), B.ABS_ERR_RANGE), (dict(eps=float("inf")), B.ABS_ERR_RANGE),
+    (dict(weight=far(6)), LET_THROUGH), (dict(weight=far(6), w_dtype=B.ABS_E4M3), B.ABS_ERR_DTYPE),
+    (dict(weight=far(6) + 2), B.ABS_ERR_ALIGN), (dict(weight=far(2) + 640), B.ABS_ERR_ALIAS),
+    # in place, and not quite
+    (dict(out=rows(far(1))), LET_THROUGH), (dict(out=rows(far(1) + 4)), B.ABS_ERR_ALIAS),
+    (dict(out=rows(far(1), s0=65)), B.ABS_ERR_ALIAS), (dict(out=rows(far(1), dtype=B.ABS_BF16)), B.ABS_ERR_ALIAS),
+    (dict(x=rows(far(1), s0=128), out=rows(far(1) + 256, s0=128)), LET_THROUGH),  # other columns
+    (dict(x=rows(far(1), s0=128), out=rows(far(1) + 252, s0=128)), B.ABS_ERR_ALIAS),
+    (dict(residual=rows(far(3)), sum=rows(far(3)), out=rows(far(1))), LET_THROUGH),
+    (dict(residual=rows(far(3)), sum=rows(far(2))), B.ABS_ERR_ALIAS),
+    # 8 bits
+    (dict(out=E4), B.ABS_ERR_NULL), (dict(out=E4, scales=SC), LET_THROUGH), (dict(scales=SC), B.ABS_ERR_RANGE),
+    (dict(group=32), B.ABS_ERR_RANGE), (dict(out=E4, scales=MX, group=32, stride2=1), LET_THROUGH),
+    (dict(out=E4, scales=MX, group=16, stride2=1), B.ABS_ERR_RANGE), (dict(out=E4, scales=MX, group=-1), B.ABS_ERR_RANGE),
+    (dict(out=E4, scales=rows(far(5), s0=1, dtype=B.ABS_BF16)), B.ABS_ERR_DTYPE),
+    (dict(out=E4, scales=MX, group=32, stride2=0), B.ABS_ERR_ALIAS),
+    (dict(out=E4, scales=rows(far(5), s0=1, dtype=B.ABS_E8M0), group=32, stride2=1), B.ABS_ERR_ALIAS),
+    (dict(out=E4, scales=rows(far(5), s0=1, dtype=B.ABS_E8M0), group=32, stride2=10), LET_THROUGH),
+    (dict(out=E4, scales=rows(far(5), s0=1, dtype=B.ABS_E8M0), group=32, stride2=9), B.ABS_ERR_ALIAS),
+    (dict(out=E4, scales=rows(far(2) + 64, s0=1)), B.ABS_ERR_ALIAS),
+])
+def test_norm_checks(L, change, status):
+    assert norm(L, **change) == status
+
+
+WORK = dict(work=far(7), work_bytes=1 << 20)
+
+
+@pytest.mark.parametrize("change,status", [
+    ({}, LET_THROUGH), (dict(n0=0, dy=NONE, s=NONE, dx=NONE), B.ABS_OK),
+    (dict(dy=NONE), B.ABS_ERR_NULL), (dict(s=NONE), B.ABS_ERR_NULL), (dict(dx=NONE), B.ABS_ERR_NULL),
+    (dict(dw=far(6)), B.ABS_ERR_NULL), (dict(dw=far(6), **WORK), LET_THROUGH),
+    (dict(dw=far(6), work=far(7), work_bytes=11 * 64 * 4 - 1), B.ABS_ERR_TOO_LARGE),
+    (dict(dw=far(6), work=far(7), work_bytes=11 * 64 * 4), LET_THROUGH),
+    (dict(dw=far(6), work=far(7) + 16, work_bytes=1 << 20), B.ABS_ERR_ALIGN),
+    (dict(dw=far(6) + 1, **WORK), B.ABS_ERR_ALIGN), (dict(dw=far(3), **WORK), B.ABS_ERR_ALIAS),
+    (dict(dw=far(1), **WORK), B.ABS_ERR_ALIAS), (dict(dw=far(7), **WORK), B.ABS_ERR_ALIAS),
+    (dict(dw=far(6), work=far(2), work_bytes=1 << 20), B.ABS_ERR_ALIAS),
+    (dict(offsets=far(8)), B.ABS_ERR_NULL), (dict(n_samples=3), B.ABS_ERR_NULL),
+    (dict(offsets=far(8), n_samples=3), LET_THROUGH), (dict(offsets=far(8) + 2, n_samples=3), B.ABS_ERR_ALIGN),
+    (dict(offsets=far(8), n_samples=(1 << 20) + 1), B.ABS_ERR_RANGE), (dict(n_samples=-1), B.ABS_ERR_RANGE),
+    (dict(apart=far(9), **WORK), B.ABS_ERR_NULL),
+    (dict(offsets=far(8), n_samples=3, apart=far(9), **WORK), LET_THROUGH),
+    (dict(offsets=far(8), n_samples=3, apart=far(9), ld=63, **WORK), B.ABS_ERR_RANGE),
+    (dict(offsets=far(8), n_samples=3, apart=far(9), ld=1 << 46, **WORK), B.ABS_ERR_RANGE),
+    (dict(offsets=far(8), n_samples=1, apart=far(9), ld=0, **WORK), LET_THROUGH),
+    (dict(offsets=far(8), n_samples=3, apart=far(9), dw=far(9) + 256, **WORK), B.ABS_ERR_ALIAS),
+    (dict(offsets=far(9), n_samples=3, apart=far(9), **WORK), B.ABS_ERR_ALIAS),
+    (dict(weight=far(3)), B.ABS_ERR_ALIAS), (dict(weight=far(6), w_dtype=9), B.ABS_ERR_DTYPE),
+    (dict(dx=rows(far(1))), LET_THROUGH), (dict(dx=rows(far(2))), LET_THROUGH), (dict(dx=rows(far(1) + 4)), B.ABS_ERR_ALIAS),
+    (dict(dx=rows(far(3), s0=32)), B.ABS_ERR_ALIAS), (dict(dx=rows(far(3), dtype=B.ABS_E4M3)), B.ABS_ERR_DTYPE),
+    (dict(dy=rows(far(1), dtype=B.ABS_F16)), LET_THROUGH), (dict(s=rows(far(2), dtype=B.ABS_F16)), B.ABS_ERR_DTYPE),
+    (dict(add=rows(far(4), dtype=B.ABS_F16)), B.ABS_ERR_DTYPE),
+    (dict(eps=-1.0), B.ABS_ERR_RANGE), (dict(scale=float("nan")), B.ABS_ERR_RANGE), (dict(scale=float("inf")), B.ABS_ERR_RANGE),
+])
+def test_gradient_checks(L, change, status):
+    assert grad(L, **change) == status
+
+
+def test_work_bytes(L):
+    f = L.abs_rms_norm_grad_bytes
+    assert f(10, 1, 64, 0) == 11 * 64 * 4 and f(10, 1, 61, 0) == 11 * 64 * 4
+    assert f(10, 1, 64, 3) == (10 + 13 + 1) * 64 * 4
+    for bad in ((-1, 1, 64, 0), (1, 1, 0, 0), (1, 1, 16385, 0), (1 << 31, 1, 64, 0), (1, 1, 64, -1), (1, 1, 64, (1 << 20) + 1)):
+        assert f(*bad) == 0
+
+
+def test_overlaps_of_views_against_a_search(L):
+    """Tensors of the same strides: the answer is exact.  Compared with the sets of bytes that the rows cover."""
+    rng = random.Random(1)
+    seen = {True: 0, False: 0}
+    for _ in range(1500):
+        n0, n1, h = rng.randint(1, 4), rng.randint(1, 4), rng.randint(1, 5)
+        s1 = h + rng.randint(0, 4)
+        s0 = n1 * s1 + rng.randint(0, 6)
+        if rng.random() < 0.3:  # the outer dimension lies inside
+            s0, s1 = h + rng.randint(0, 4), 0
+            s1 = n0 * s0 + rng.randint(0, 6)
+        d = rng.randint(-3 * (s0 + s1), 3 * (s0 + s1))
+
+        def cover(at):
+            return {at + i * s0 + j * s1 + c for i, j, c in itertools.product(range(n0), range(n1), range(h))}
+        touch = bool(cover(0) & cover(d)) and d != 0
+        rc = norm(L, n0, n1, h, x=rows(far(3), s0, s1), out=rows(far(3) + 4 * d, s0, s1))
+        assert rc == (B.ABS_ERR_ALIAS if touch else LET_THROUGH), (n0, n1, h, s0, s1, d)
+        seen[touch] += 1
+    assert min(seen.values()) > 100
