@@ -692,6 +692,58 @@ size_t abs_rms_norm_grad_bytes(int64_t n0, int64_t n1, int64_t h, int64_t n_samp
 int abs_rms_norm_grad(const abs_rms_norm_grad_args* args, abs_stream_t stream);
 
 /*
+ * ---- Distillation -----------------------------------------------------------------------
+ * A student's loss against the top logits of a teacher, token by token, and in the same call its gradient on the
+ * student's logits: the loss of the per-sample test is a mean over samples, so tokens carry weights and samples
+ * have losses of their own.  With tau the temperature, q the softmax of the row's logits / tau:
+ *
+ *   without teacher_lse   p = softmax over the row's top of t / tau,  loss = tau^2 sum_j p_j ln(p_j / q_j)
+ *   with teacher_lse      p_j = exp(t_j / tau - lse),  p_r = max(0, 1 - sum_j p_j),  q_r the sum of q outside the top;
+ *                         loss = tau^2 (sum_j p_j ln(p_j / q_j) + p_r ln(p_r / q_r)).  Where nothing is outside
+ *                         of the top (it is the whole vocabulary, or the rest is -inf) p_r counts as 0
+ *   dlogits_i             weight * grad_scale * tau * (q_i - p_i) in the top,
+ *                         weight * grad_scale * tau * q_i (1 - p_r / q_r) elsewhere: the derivative of
+ *                         weight * grad_scale * loss
+ *
+ *   logits         rows x vocab, ABS_F32, ABS_BF16 or ABS_F16 (stride0 from row to row); vocab at most
+ *                  ABS_MAX_VOCAB (ABS_ERR_TOO_LARGE).  -inf masks an index, and so does the type's lowest value, but
+ *                  not as the whole rest of a row whose p_r is positive: the loss then says how far away it is
+ *   top_ids        device, rows x top indices of id_bytes 4 or 8 (signed), ids_stride from row to row; top is
+ *                  1..ABS_MAX_TOP.  An entry whose index is not one of 0..vocab-1 (-1, say) is left out; an index
+ *                  that a row names twice has both probabilities
+ *   top_logits     rows x top, one of the three types.  -inf: no probability.  A row none of whose entries has
+ *                  one has, without teacher_lse, the loss and the gradient 0
+ *   teacher_lse    device, rows floats: ln sum exp(t / tau) over the teacher's whole vocabulary, or NULL
+ *   weights        device, rows floats, or NULL: ones.  Rows of weight 0 are not read: loss 0, gradient 0
+ *   offsets        device, n_samples + 1 non-decreasing row numbers, as in abs_rms_norm_grad; NULL with n_samples 0: one
+ *                  sample of all rows.  Rows before the first and behind the last sample are neither read nor
+ *                  written
+ *   losses         device, rows floats: the loss of each row, without its weight
+ *   sample_losses  device, n_samples floats (one without offsets), or NULL: sum of weight * loss over the sample's rows
+ *   dlogits        the logits' type, or not given; may be the logits themselves
+ *   temperature    1e-3 .. 1e3
+ * Sums are formed in fp32 (over samples in fp64) in an order that depends on the shapes alone.  A NaN or
+ * infinity (+inf among the logits) makes its row's loss and gradient NaN.  One launch, two with sample_losses.
+ * Bound by reading the logits once and writing the gradient once.
+ */
+enum { ABS_MAX_TOP = 512, ABS_MAX_VOCAB = 1 << 20 };
+typedef struct {
+  int64_t rows, vocab, top;
+  abs_rows logits, dlogits, top_logits;
+  const void* top_ids;
+  const float* teacher_lse;
+  const float* weights;
+  const int32_t* offsets;
+  float* losses;
+  float* sample_losses;
+  int64_t ids_stride, n_samples;
+  double temperature, grad_scale;
+  int32_t id_bytes;
+  int32_t reserved;
+} abs_distill_args;
+int abs_distill_loss(const abs_distill_args* args, abs_stream_t stream);
+
+/*
  * Self-test of the bounded waits (no counterpart in the paper).  The staged kernels wait for
  * their asynchronous copies on shared-memory barriers, and every such wait gives up after a
  * fixed number of polls (2^18, about one second on a B200) instead of spinning for ever; a kernel whose wait gave up

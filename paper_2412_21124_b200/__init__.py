@@ -8,7 +8,7 @@ from .binding import (ABS_BF16, ABS_F16, ABS_F32, ABS_GRAD_COEF, ABS_GRAD_FLAGS,
                       abs_grad_norm, ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE,  # noqa: F401
                       ABS_FLAG_VIOLATED, AbsError, FusedStep, abs_adamw_hparams, abs_adamw_step, abs_adamw_step_clipped,
                       abs_adamw_step_mixed, abs_normtest_adamw_mixed,
-                      abs_decide, abs_combine_sums, abs_noalloc_fits,
+                      abs_decide, abs_combine_sums, abs_distill_loss, abs_noalloc_fits,
                       abs_norm_test, abs_normtest_adamw, abs_normtest_adamw_noalloc,
                       abs_norm_test_coordwise, abs_normtest_adamw_coordwise, abs_norm_test_q,
                       abs_norm_test_accumulate, abs_norm_test_accumulate_adamw,

@@ -30,6 +30,7 @@ ABS_FLAG_DEGENERATE, ABS_FLAG_NONFINITE, ABS_FLAG_VIOLATED = 1, 2, 4
 ABS_MAX_GROUPS, ABS_MAX_TENSORS = 16, 1 << 20
 ABS_NORM_MAX, ABS_NORM_1, ABS_NORM_2 = 0, 1, 2
 ABS_MAX_NORM_WIDTH, ABS_MAX_SAMPLES = 16384, 1 << 20
+ABS_MAX_TOP, ABS_MAX_VOCAB = 512, 1 << 20
 ABS_GRAD_SUM, ABS_GRAD_NORM, ABS_GRAD_COEF, ABS_GRAD_FLAGS = 0, 1, 2, 4
 
 
@@ -143,6 +144,8 @@ def lib():
     L.abs_rms_norm_grad.argtypes = [ptr, ptr]
     L.abs_rms_norm_grad_bytes.restype = sz
     L.abs_rms_norm_grad_bytes.argtypes = [i64, i64, i64, i64]
+    L.abs_distill_loss.restype = cint
+    L.abs_distill_loss.argtypes = [ptr, ptr]
     L.abs_selftest_bounded_wait.restype = cint
     L.abs_selftest_bounded_wait.argtypes = [cint, ptr, ptr]
     L.abs_status_string.restype = ctypes.c_char_p
@@ -855,11 +858,12 @@ def abs_grad_adamw(tensors, hparams, step, max_norm=0.0, norm_type=2, grad_scale
 _ROW_DTYPES = {torch.float32: ABS_F32, torch.bfloat16: ABS_BF16, torch.float16: ABS_F16,
                torch.float8_e4m3fn: ABS_E4M3, torch.float8_e5m2: ABS_E5M2,
                torch.float8_e8m0fnu: ABS_E8M0}
-# abs_rows, abs_rms_norm_args and abs_rms_norm_grad_args as struct packs them: native alignment, as in C
+# abs_rows and the argument blocks of the calls as struct packs them: native alignment, as in C
 _ROWS = "Pqqii"
 _NO_ROWS = (0, 0, 0, 0, 0)
 _NORM_ARGS = struct.Struct("@3q" + 5 * _ROWS + "qPiid")
 _NORM_GRAD_ARGS = struct.Struct("@3q" + 4 * _ROWS + "5P3q2dii")
+_DISTILL_ARGS = struct.Struct("@3q" + 3 * _ROWS + "6P2q2dii")
 
 
 def _row_shape(t, name):
@@ -919,6 +923,15 @@ def _raw_stream(stream, device):
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(device)
     return _stream(stream).value or 0
+
+
+def _sample_table(offsets, device):
+    """(number of samples, address of their offsets)"""
+    if offsets is None:
+        return 0, 0
+    if offsets.dim() != 1 or offsets.numel() < 2:
+        raise TypeError("offsets must hold samples + 1 numbers")
+    return offsets.numel() - 1, _flat_pointer(offsets, torch.int32, None, device, "offsets")
 
 
 def abs_rms_norm(x, weight, out, eps=1e-6, residual=None, sum_out=None, scales_out=None, group=0,
@@ -992,12 +1005,7 @@ def abs_rms_norm_grad(dy, s, weight, dx, dweight, eps=1e-6, dresidual=None, offs
     shape = s.shape
     n0, n1, h = _row_shape(s, "s")
     w, w_code = _weight_fields(weight, h, device)
-    samples, table = 0, 0
-    if offsets is not None:
-        if offsets.dim() != 1 or offsets.numel() < 2:
-            raise TypeError("offsets must hold samples + 1 numbers")
-        samples = offsets.numel() - 1
-        table = _flat_pointer(offsets, torch.int32, None, device, "offsets")
+    samples, table = _sample_table(offsets, device)
     apart, ld = 0, h
     if dweight_samples is not None:
         if offsets is None:
@@ -1018,6 +1026,60 @@ def abs_rms_norm_grad(dy, s, weight, dx, dweight, eps=1e-6, dresidual=None, offs
     if rc != ABS_OK:
         raise AbsError(rc, "abs_rms_norm_grad")
     return dx
+
+
+def abs_distill_loss(logits, top_ids, top_logits, losses_out, temperature=1.0, teacher_lse=None, weights=None,
+                     offsets=None, sample_losses_out=None, dlogits=None, grad_scale=1.0, stream=None):
+    """Distillation from a teacher's top logits: temperature^2 * KL(teacher || student) of every row, and with dlogits
+    its gradient in the same call.
+
+      logits       [rows, vocab] float32 / bfloat16 / float16, rows any distance apart
+      top_ids      [rows, top] int64 or int32: where the teacher has its top entries.  Indices outside of the
+                   vocabulary (-1) leave an entry out
+      top_logits   [rows, top]: the teacher's logits there
+      teacher_lse  [rows] float32: log-sum-exp of the teacher's logits / temperature over its whole vocabulary.  The mass
+                   that its top leaves then counts against the student's outside of the top; without it
+                   the teacher's softmax is taken over its top alone
+      weights      [rows] float32: the loss is sum of weights * losses.  Rows of weight 0 are not read
+      offsets      int32 [samples + 1]: as in abs_rms_norm_grad; rows of no sample are left as they are
+      losses_out   [rows] float32, without the weights
+      sample_losses_out  [samples] float32 (one value without offsets): sum of weights * losses of each
+      dlogits      like logits, or logits itself: gradient of grad_scale * sum of weights * losses
+
+    Returns losses_out."""
+    device = torch._C._cuda_getDevice()
+    shape = logits.shape
+    if len(shape) != 2 or top_ids.dim() != 2:
+        raise TypeError("logits and top_ids must be matrices")
+    rows, vocab = shape
+    top = top_ids.shape[1]
+    ids = _flat_rows(top_ids, (rows, top), device)
+    samples, table = _sample_table(offsets, device)
+    args = _DISTILL_ARGS.pack(
+        rows, vocab, top, *_row_fields(logits, shape, device, "logits"), *_row_fields(dlogits, shape, device, "dlogits"),
+        *_row_fields(top_logits, (rows, top), device, "top_logits"), ids,
+        _flat_pointer(teacher_lse, torch.float32, rows, device, "teacher_lse"),
+        _flat_pointer(weights, torch.float32, rows, device, "weights"), table,
+        _flat_pointer(losses_out, torch.float32, rows, device, "losses_out"),
+        _flat_pointer(sample_losses_out, torch.float32, samples or 1, device, "sample_losses_out"),
+        top_ids.stride(0), samples, temperature, grad_scale, 8 if top_ids.dtype == torch.int64 else 4, 0)
+    rc = lib().abs_distill_loss(args, _raw_stream(stream, device))
+    if rc != ABS_OK:
+        raise AbsError(rc, "abs_distill_loss")
+    return losses_out
+
+
+def _flat_rows(ids, shape, device):
+    if ids.get_device() != device:
+        _check_one_device(ids)
+        raise ValueError("top_ids must be a CUDA tensor")
+    if ids.dtype not in (torch.int64, torch.int32):
+        raise TypeError("top_ids must be int64 or int32")
+    if ids.shape != shape:
+        raise ValueError("top_ids: shape %s, expected %s" % (tuple(ids.shape), shape))
+    if ids.stride(1) != 1 and shape[1] > 1:
+        raise TypeError("top_ids: the entries of a row must lie side by side")
+    return ids.data_ptr()
 
 
 def abs_decide(S, n2, norm, eta, b_cur):

@@ -26,7 +26,7 @@ STREAM_COMBINATIONS = [("BF16", 1, 0), ("F32", 1, 0), ("BF16", 0, 1), ("F32", 0,
                        ("BF16", 0, 0), ("F32", 0, 0), ("BF16", 1, 2), ("F32", 1, 2),
                        ("BF16", 0, 2), ("F32", 0, 2)]
 
-# types of a row's values: the norms' kernels are compiled once for each
+# types of a row's values: the kernels on rows are compiled once for each
 ROW_TYPES = ["ABS_F32", "ABS_BF16", "ABS_F16"]
 
 
@@ -56,9 +56,10 @@ def _jobs():
                 jobs.append((os.path.join(_OBJ, "stream_%s_%d_%d.o" % (gt.lower(), adam, stat)), src,
                              ["-DABS_INST_GT=%s" % gt, "-DABS_INST_ADAM=%d" % adam,
                               "-DABS_INST_STAT=%d" % stat]))
-        elif name == "rms_norm_inst":
+        elif name in ("rms_norm_inst", "distill_inst"):
             for xt in ROW_TYPES:
-                jobs.append((os.path.join(_OBJ, "rms_norm_%s.o" % xt.lower()), src, ["-DABS_INST_XT=%s" % xt]))
+                obj = "%s_%s.o" % (name[:-len("_inst")], xt.lower())
+                jobs.append((os.path.join(_OBJ, obj), src, ["-DABS_INST_XT=%s" % xt]))
         else:
             jobs.append((os.path.join(_OBJ, name + ".o"), src, []))
     return jobs

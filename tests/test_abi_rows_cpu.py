@@ -167,3 +167,45 @@ def test_overlaps_of_views_against_a_search(L):
         assert rc == (B.ABS_ERR_ALIAS if touch else LET_THROUGH), (n0, n1, h, s0, s1, d)
         seen[touch] += 1
     assert min(seen.values()) > 100
+
+
+# ------------------------------------------------------------------------------------- distillation
+def distill(L, rows_=10, vocab=100, top=8, z=rows(far(1), s0=100), dz=NONE, t=rows(far(3), s0=8), ids=far(4), lse=0, weights=0,
+            offsets=0, losses=far(5), samples=0, ids_stride=8, n_samples=0, tau=1.0, scale=1.0, id_bytes=8):
+    return L.abs_distill_loss(B._DISTILL_ARGS.pack(rows_, vocab, top, *z, *dz, *t, ids, lse, weights, offsets, losses, samples,
+                                                   ids_stride, n_samples, tau, scale, id_bytes, 0), None)
+
+
+def test_distillation_argument_block():
+    assert B._DISTILL_ARGS.size == 24 + 3 * 32 + 6 * 8 + 2 * 8 + 2 * 8 + 8
+
+
+DZ = rows(far(2), s0=100)
+
+
+@pytest.mark.parametrize("change,status", [
+    ({}, LET_THROUGH), (dict(dz=DZ), LET_THROUGH), (dict(rows_=0, z=NONE, t=NONE, ids=0, losses=0), B.ABS_OK),
+    (dict(rows_=-1), B.ABS_ERR_RANGE), (dict(rows_=1 << 31), B.ABS_ERR_RANGE), (dict(vocab=0), B.ABS_ERR_RANGE),
+    (dict(vocab=(1 << 20) + 1), B.ABS_ERR_TOO_LARGE), (dict(vocab=1 << 20, z=rows(far(1), s0=1 << 20)), LET_THROUGH),
+    (dict(top=0), B.ABS_ERR_RANGE), (dict(top=513), B.ABS_ERR_RANGE),
+    (dict(tau=0.0), B.ABS_ERR_RANGE), (dict(tau=float("nan")), B.ABS_ERR_RANGE), (dict(tau=1e4), B.ABS_ERR_RANGE),
+    (dict(scale=float("nan")), B.ABS_ERR_RANGE), (dict(id_bytes=2), B.ABS_ERR_DTYPE), (dict(id_bytes=4), LET_THROUGH),
+    (dict(z=NONE), B.ABS_ERR_NULL), (dict(t=NONE), B.ABS_ERR_NULL), (dict(ids=0), B.ABS_ERR_NULL), (dict(losses=0), B.ABS_ERR_NULL),
+    (dict(z=rows(far(1), s0=100, dtype=B.ABS_E4M3)), B.ABS_ERR_DTYPE), (dict(dz=rows(far(2), s0=100, dtype=B.ABS_BF16)), B.ABS_ERR_DTYPE),
+    (dict(t=rows(far(3), s0=8, dtype=B.ABS_F16)), LET_THROUGH), (dict(t=rows(far(3), s0=8, dtype=7)), B.ABS_ERR_DTYPE),
+    (dict(ids=far(4) + 4), B.ABS_ERR_ALIGN), (dict(ids=far(4) + 4, id_bytes=4), LET_THROUGH), (dict(ids=far(4) + 2, id_bytes=4), B.ABS_ERR_ALIGN),
+    (dict(ids_stride=-1), B.ABS_ERR_RANGE), (dict(ids_stride=0, t=rows(far(3), s0=0)), LET_THROUGH),
+    (dict(losses=far(5) + 2), B.ABS_ERR_ALIGN), (dict(weights=far(6) + 1), B.ABS_ERR_ALIGN), (dict(lse=far(6) + 1), B.ABS_ERR_ALIGN),
+    (dict(offsets=far(7)), B.ABS_ERR_NULL), (dict(n_samples=2), B.ABS_ERR_NULL), (dict(offsets=far(7), n_samples=2), LET_THROUGH),
+    (dict(offsets=far(7), n_samples=(1 << 20) + 1), B.ABS_ERR_RANGE),
+    (dict(dz=rows(far(1), s0=100)), LET_THROUGH), (dict(dz=rows(far(1) + 4, s0=100)), B.ABS_ERR_ALIAS),
+    (dict(z=rows(far(1), s0=200), dz=rows(far(1) + 400, s0=200)), LET_THROUGH),
+    (dict(dz=rows(far(2), s0=99)), B.ABS_ERR_ALIAS), (dict(dz=rows(far(3), s0=100)), B.ABS_ERR_ALIAS),
+    (dict(dz=rows(far(4) + 64, s0=100)), B.ABS_ERR_ALIAS), (dict(dz=DZ, weights=far(2)), B.ABS_ERR_ALIAS),
+    (dict(losses=far(1)), B.ABS_ERR_ALIAS), (dict(losses=far(3)), B.ABS_ERR_ALIAS), (dict(losses=far(4) + 320), B.ABS_ERR_ALIAS),
+    (dict(losses=far(4) + 640), LET_THROUGH), (dict(losses=far(4) + 320, id_bytes=4), LET_THROUGH),
+    (dict(weights=far(5)), B.ABS_ERR_ALIAS), (dict(samples=far(5) + 36), B.ABS_ERR_ALIAS), (dict(samples=far(5) + 40), LET_THROUGH),
+    (dict(lse=far(8), samples=far(8)), B.ABS_ERR_ALIAS), (dict(dz=DZ, samples=far(2)), B.ABS_ERR_ALIAS),
+])
+def test_distillation_checks(L, change, status):
+    assert distill(L, **change) == status
