@@ -26,6 +26,7 @@ struct DistillParams {
   uint32_t rows;
   int n_samples;
   int vocab, top, t_dtype, id_bytes;
+  double inv_tau;
   float c;                 // log2(e) / tau
   float tau;
   float loss_scale;        // tau^2 ln 2: of logarithms to base 2
@@ -75,6 +76,11 @@ __device__ __forceinline__ void store_one(unsigned char* row, int i, float v) {
   if constexpr (DT == ABS_F32) reinterpret_cast<float*>(row)[i] = v;
   else if constexpr (DT == ABS_BF16) reinterpret_cast<__nv_bfloat16*>(row)[i] = __float2bfloat16_rn(v);
   else reinterpret_cast<__half*>(row)[i] = __float2half_rn(v);
+}
+
+// log2 of exp(t / tau - lse): the two are often large and close, so their difference is taken in 64 bits
+__device__ __forceinline__ float log_of_share(const DistillParams& p, float t, float lse) {
+  return static_cast<float>(static_cast<double>(t) * p.inv_tau - static_cast<double>(lse)) * 1.44269504f;
 }
 
 // joins of a block of 16 warps, in a fixed order; `room` is not used again before the next barrier
@@ -140,7 +146,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
   bool again = false;
   if (id >= 0) again = atomicOr(&in_top[id >> 5], 1u << (id & 31)) & (1u << (id & 31));
   // in units of log2; an entry that has no probability takes no part
-  const float log_p = p.lse ? t * p.c - p.lse[row] * 1.44269504f : (t - st.m) * p.c - log2f(st.s);
+  const float log_p = p.lse ? log_of_share(p, t, p.lse[row]) : (t - st.m) * p.c - log2f(st.s);
   const bool some = id >= 0 && t != -INFINITY;
   const float pj = some ? exp2_fast(log_p) : 0.f;
   sh_p[tid] = pj;

@@ -1,0 +1,610 @@
+// The distillation kernel of vocabularies whose rows fit the shared memory of a cluster: logits are read from
+// HBM once, gradient and loss come from what is on the chip.
+//
+// A row is cut into 16-byte units from the boundary before its first value, and the units go in equal runs to the
+// blocks of a cluster of 1 to 8.  The warps of a block have four parts:
+//   feeder   runs ahead: brings the block's run of the next rows into a ring of stages by bulk copies; meanwhile
+//            finds out where the top's entries lie in it and works out the teacher's probabilities
+//   workers  pass 1 of a row: take the top's logits out of the stage (-inf stays in their place), sum 2^((z - m) c)
+//            over the rest.  Pass 2, of the row before: the same exponentials once more times one factor are the
+//            gradient, written 16 bytes at a time; the top's places follow behind the next barrier
+//   topper   sums over the top's entries while the workers are at pass 1
+//   joiner   joins the warps' sums, exchanges them with the other blocks by asynchronous stores into their shared
+//            memory, and gives the workers the factor
+// so that neither the loads nor the joins keep a worker waiting.  A special warp gets an eighth of its
+// scheduler's slots beside the workers: what it does in a row decides the rate, hence three of them.  Earlier
+// forms, rows of 128256: workers that joined among themselves and kept the exponentials in registers meanwhile spent
+// 13,000 cycles on a row of which 4,600 were passes; one warp for teacher, top and joins 9,400.
+// Rows need not begin on 16-byte boundaries: gradient and logits must only lie at the same distance from one.
+//
+// Bounds: HBM, 2 bytes a value read and 2 written (16 bits); the exponentials, 16 a clock and SM, take 0.73 of the
+// time of these accesses, with and without the gradient.  Every wait is bounded (see normtest_bulk.cuh); one that
+// runs out makes its row NaN.
+#pragma once
+#include "distill.cuh"
+#include "normtest_bulk.cuh"
+
+namespace absnt {
+
+constexpr int kRingMaxCluster = 8;
+constexpr int kRingMaxStages = 4;
+
+struct RingParams {
+  DistillParams d;
+  int blocks;        // of a cluster
+  int units;         // of a block
+  int stages;        // at least 2: pass 2 of a row comes after pass 1 of the next
+  int stage_bytes;   // units and 16 bytes an entry of the top, a multiple of 16
+  const unsigned char *z_begin, *z_end;  // the logits' first byte and the one behind their last
+};
+
+enum { kRowAlone = 0, kRowNoWeight = 1, kRowWork = 2 };
+
+// what a block knows of a row after pass 1: the rest's sum, the top's, and of the block's entries of the top the sum
+// of p (tau^2 ln p - tau (z - m)) with m the top's reference, and the sum of p
+struct RingSums {
+  ExpSum rest, top;
+  float cross, p;
+  float unused[2];
+};
+// what the workers need of a row for pass 2
+struct RingAnswer {
+  float factor, m;        // of the rest: factor * 2^((z - m) c)
+  float g, m_all, over_s; // of the top: g (2^((z - m_all) c) over_s - p)
+};
+// the top's entries of a row in its stage: place in the block's run (-1: elsewhere), logit, log2 p, p.  When the
+// topper is done log_p holds p summed over the entries of the same index
+struct RingTop {
+  int* place;
+  float *z, *log_p, *p;
+};
+
+// the largest of a warp's values, by their bits: as signed integers they are ordered like the floats once those of
+// negative ones are turned round.  No value is a NaN.
+__device__ __forceinline__ float warp_max(float x) {
+  int b = __float_as_int(x);
+  b ^= (b >> 31) & 0x7fffffff;
+  b = __reduce_max_sync(0xffffffffu, b);
+  return __int_as_float(b ^ ((b >> 31) & 0x7fffffff));
+}
+// joins over the warp's lanes
+__device__ __forceinline__ ExpSum warp_join(ExpSum x, float c) {
+  const float m = warp_max(x.m);
+  return {m, lanes_sum<32>(x.s * exp2_fast((x.m - m) * c))};
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// 32 bytes into the same place of another block's shared memory, counted on the barrier there
+__device__ __forceinline__ void send_sums(const RingSums& x, RingSums* to, uint64_t* bar, uint32_t rank) {
+  uint32_t a, b;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(to)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_addr(bar)), "r"(rank));
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];" ::"r"(a),
+               "f"(x.rest.m), "f"(x.rest.s), "f"(x.top.m), "f"(x.top.s), "r"(b)
+               : "memory");
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];" ::"r"(a + 16),
+               "f"(x.cross), "f"(x.p), "f"(0.f), "f"(0.f), "r"(b)
+               : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void workers_barrier() {  // all warps but the feeder
+  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+}
+
+template <int DT>
+__host__ __device__ constexpr int unit_values() {
+  return 16 / elem_bytes<DT>();
+}
+template <int DT>
+__device__ __forceinline__ float value_of(const uint32_t (&w)[4], int j) {
+  if constexpr (DT == ABS_F32) return __uint_as_float(w[j]);
+  if constexpr (DT == ABS_BF16) return __uint_as_float((j & 1) ? (w[j >> 1] & 0xffff0000u) : (w[j >> 1] << 16));
+  return from_half_word<DT>((j & 1) ? (w[j >> 1] >> 16) : (w[j >> 1] & 0xffffu));
+}
+
+
+// two floats at once: one instruction slot
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 pair_as(uint64_t x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^((z - m) c) of two values, as a pair
+template <int DT>
+__device__ __forceinline__ float2 exp_pair(const uint32_t (&w)[4], int j, uint64_t minus_m, uint64_t c) {
+  const float2 a = pair_as(pair_mul(pair_add(pair_of(value_of<DT>(w, j), value_of<DT>(w, j + 1)), minus_m), c));
+  return make_float2(exp2_fast(a.x), exp2_fast(a.y));
+}
+// the larger of two words of values, place by place
+template <int DT>
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (DT == ABS_F32) r = __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  else if constexpr (DT == ABS_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ float max_of_word(uint32_t w) {
+  if constexpr (DT == ABS_F32) return __uint_as_float(w);
+  return fmaxf(from_half_word<DT>(w & 0xffffu), from_half_word<DT>(w >> 16));
+}
+
+// A unit of a row's gradient; i0: the index of its first value.  The first and last of a row may reach out of it.
+template <int DT>
+__device__ __forceinline__ void write_unit(unsigned char* to, int i0, int vocab, const uint32_t (&out)[4]) {
+  constexpr int U = unit_values<DT>();
+  if (i0 >= 0 && i0 + U <= vocab) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j)
+    if (i0 + j >= 0 && i0 + j < vocab) {
+      if constexpr (DT == ABS_F32) reinterpret_cast<uint32_t*>(to)[j] = out[j];
+      else reinterpret_cast<unsigned short*>(to)[j] = static_cast<unsigned short>(out[j >> 1] >> (16 * (j & 1)));
+    }
+}
+
+constexpr int ring_blocks_per_sm(int threads) { return threads == 128 ? 5 : 1024 / threads; }  // 928: 1
+
+// THREADS (at most 928) workers and three special warps; a worker takes up to NU units of a row
+template <int DT, int THREADS, int NU, bool GRAD>
+__global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
+    distill_ring_kernel(const __grid_constant__ RingParams r) {
+  constexpr int U = unit_values<DT>();
+  constexpr int ESZ = elem_bytes<DT>();
+  constexpr int kWarps = THREADS / 32;
+  const DistillParams& p = r.d;
+  extern __shared__ __align__(16) unsigned char ring[];  // the stages, then a bit for each place of the block's run
+  __shared__ __align__(8) uint64_t full[kRingMaxStages], empty[kRingMaxStages];
+  __shared__ __align__(8) uint64_t taken[2], summed[2], answered[2], sums_here[2];
+  __shared__ int repeated_in[kRingMaxStages];  // an index of this block's run is named twice
+  __shared__ int any_in[kRingMaxStages];       // the teacher names something
+  __shared__ __align__(16) ExpSum from_warps[2][kWarps];
+  __shared__ __align__(16) RingSums from_top[2], from_blocks[2][kRingMaxCluster];
+  __shared__ RingAnswer answers[2];
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rank = r.blocks > 1 ? static_cast<int>(cluster_rank()) : 0;
+  const uint32_t cluster = blockIdx.x / r.blocks, clusters = gridDim.x / r.blocks;
+  uint32_t* const marks = reinterpret_cast<uint32_t*>(ring + r.stages * r.stage_bytes);
+  const int first_unit = rank * r.units;
+  bool dead = false;  // a wait of this thread ran out: it waits no more, and what it computes is NaN
+  const float nan = __uint_as_float(0x7fffffffu);
+
+  if (tid == 0) {
+    for (int s = 0; s < r.stages; ++s) {
+      mbar_init(&full[s], 2);        // the copy has been asked for; the top's entries are there
+      mbar_init(&empty[s], kWarps);
+    }
+    for (int k = 0; k < 2; ++k) {
+      mbar_init(&taken[k], 1);           // the top's logits
+      mbar_init(&summed[k], kWarps + 1); // by workers and topper
+      mbar_init(&answered[k], 1);
+      mbar_init(&sums_here[k], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = tid; i < (r.units * U + 31) / 32; i += THREADS + 96) marks[i] = 0u;
+  __syncthreads();
+  if (r.blocks > 1) cluster_barrier();
+  grid_dependency_wait();
+
+  int64_t low = 0, high = p.rows;
+  if (p.offsets) {
+    low = p.offsets[0];
+    high = p.offsets[p.n_samples];
+  }
+  // Rows of this cluster: cluster, cluster + clusters, ...  Only rows that are worked on take a stage; n counts them.
+  // Every warp finds out for itself, from the call's arguments alone, which those are, and so which barriers it
+  // passes; a lane a row, the weights of 32 rows at a time.
+  float weights_ahead = 0.f;
+  uint32_t seen = 0;
+  auto kind_of = [&](uint32_t row, float& weight) {
+    if ((seen & 31) == 0) {
+      const int64_t mine = static_cast<int64_t>(row) + static_cast<int64_t>(lane) * clusters;
+      weights_ahead = p.weights && mine < p.rows ? p.weights[mine] : 1.f;
+    }
+    weight = __shfl_sync(0xffffffffu, weights_ahead, seen & 31);
+    ++seen;
+    return row < low || row >= high ? kRowAlone : weight == 0.f ? kRowNoWeight : kRowWork;
+  };
+  auto stage_of = [&](uint32_t n) { return ring + (n % r.stages) * r.stage_bytes; };
+  auto top_of = [&](unsigned char* stage) {
+    int* const place = reinterpret_cast<int*>(stage + r.units * 16);
+    float* const z = reinterpret_cast<float*>(place + p.top);
+    return RingTop{place, z, z + p.top, z + 2 * p.top};
+  };
+  float weight;
+
+  if (warp == kWarps + 2) {
+    // ---- the feeder; the first 64 entries of a row are asked for while the row before is prepared
+    constexpr int kAhead = 2;
+    struct Ahead {
+      int64_t row;
+      int id[kAhead];
+      float t[kAhead], lse;
+    };
+    uint32_t next_row = cluster;
+    auto look_ahead = [&]() {
+      Ahead x;
+      x.row = -1;
+      for (; next_row < p.rows && x.row < 0; next_row += clusters)
+        if (kind_of(next_row, weight) == kRowWork) x.row = next_row;
+      if (x.row >= 0) {
+        const uint32_t row = static_cast<uint32_t>(x.row);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int j = lane + 32 * k;
+          x.id[k] = j < p.top ? load_id(p, row, j) : -1;
+          x.t[k] = j < p.top ? load_teacher(p, row, j) : 0.f;
+        }
+        x.lse = p.lse ? p.lse[row] : 0.f;
+      }
+      return x;
+    };
+    uint32_t n = 0;
+    Ahead now = look_ahead();
+    while (now.row >= 0) {
+      const Ahead next = look_ahead();
+      const uint32_t row = static_cast<uint32_t>(now.row);
+      const uint32_t s = n % r.stages, turn = n / r.stages;
+      if (turn > 0 && !dead) dead = !mbar_wait_bounded(&empty[s], (turn - 1) & 1);
+      __syncwarp();
+      unsigned char* const stage = stage_of(n);
+      // the units of this block; the first and last of the row may reach out of the tensor at its ends
+      const unsigned char* z = row_of(p.z, row, 0);
+      const int before = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15);
+      const unsigned char* from = z - before;
+      const int n_units = (before + p.vocab * ESZ + 15) / 16;
+      int a = first_unit, e = min(first_unit + r.units, n_units);
+      if (a == 0 && from < r.z_begin) a = 1;
+      if (e == n_units && from + static_cast<int64_t>(e) * 16 > r.z_end) --e;
+      if (lane == 0) {
+        if (e > a && !dead) {
+          const uint32_t bytes = static_cast<uint32_t>(e - a) * 16u;
+          mbar_expect_tx(&full[s], bytes);
+          bulk_load(stage + (a - first_unit) * 16, from + static_cast<int64_t>(a) * 16, bytes, &full[s]);
+        } else {
+          mbar_arrive(&full[s]);
+        }
+      }
+      const RingTop top = top_of(stage);
+      const int shift = before / ESZ - first_unit * U;
+      float m = kLowest, sum = 0.f;
+      bool twice = false;
+      auto take = [&](int j, int id, float t) {
+        if (id < 0) t = -INFINITY;
+        const int at = id >= 0 && id + shift >= 0 && id + shift < r.units * U ? id + shift : -1;
+        top.place[j] = at;
+        top.log_p[j] = t;
+        m = fmaxf(m, t);
+        if (at >= 0) twice |= (atomicOr(&marks[at >> 5], 1u << (at & 31)) >> (at & 31)) & 1u;
+      };
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (lane + 32 * k < p.top) take(lane + 32 * k, now.id[k], now.t[k]);
+      for (int j = lane + 32 * kAhead; j < p.top; j += 32) {
+        const float t = load_teacher(p, row, j);
+        take(j, load_id(p, row, j), t);
+      }
+      if (!p.lse) {
+        m = warp_max(m);
+        for (int j = lane; j < p.top; j += 32) sum += exp2_fast((top.log_p[j] - m) * p.c);
+        sum = lanes_sum<32>(sum);
+      }
+      const float log_sum = log2f(sum);
+      twice = __any_sync(0xffffffffu, twice);
+      __syncwarp();  // all marks are set
+      for (int j = lane; j < p.top; j += 32) {
+        const float t = top.log_p[j];
+        const float l = t == -INFINITY ? t : p.lse ? log_of_share(p, t, now.lse) : (t - m) * p.c - log_sum;
+        top.log_p[j] = l;
+        top.p[j] = exp2_fast(l);
+        const int at = top.place[j];
+        if (at >= 0) marks[at >> 5] = 0u;
+      }
+      if (lane == 0) {
+        repeated_in[s] = twice;
+        any_in[s] = p.lse || sum != 0.f;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[s]);
+      now = next;
+      ++n;
+    }
+    // no copy is under way when the block ends, even where a worker gave up on one
+    for (uint32_t k = 0; k < static_cast<uint32_t>(r.stages) && k < n; ++k)
+      mbar_wait_bounded(&full[k], (n - 1 - k) / r.stages & 1);
+  } else if (warp == kWarps + 1) {
+    // ---- the topper
+    uint32_t n = 0;
+    for (uint32_t row = cluster; row < p.rows; row += clusters) {
+      if (kind_of(row, weight) != kRowWork) continue;
+      const uint32_t half = n & 1;
+      if (!dead) dead = !mbar_wait_bounded(&taken[half], (n >> 1) & 1);
+      __syncwarp();
+      const RingTop top = top_of(stage_of(n));
+      const bool repeated = repeated_in[n % r.stages];
+      float m = kLowest, sum = 0.f, sum_p = 0.f, cross = 0.f;
+      for (int j = lane; j < p.top; j += 32)
+        if (top.place[j] >= 0) m = fmaxf(m, top.z[j]);
+      m = warp_max(m);
+      for (int j = lane; j < p.top; j += 32)
+        if (top.place[j] >= 0) {
+          // Of the workers of one index named twice one at least has read its logit, others perhaps the -inf
+          // already.  The first entry stands for all of them.
+          float z = top.z[j];
+          const float pj = top.p[j];
+          float p_all = pj;
+          bool first = true;
+          if (repeated)
+            for (int k = 0; k < p.top; ++k)
+              if (k != j && top.place[k] == top.place[j]) {
+                if (k < j) first = false;
+                p_all += top.p[k];
+                if (top.z[k] != -INFINITY) z = top.z[k];
+              }
+          if (first) sum += exp2_fast((z - m) * p.c);
+          sum_p += pj;
+          if (pj != 0.f) cross += pj * (p.loss_scale * top.log_p[j] - p.tau * (z - m));
+          top.z[j] = z;
+          top.log_p[j] = p_all;
+        }
+      sum = lanes_sum<32>(sum);
+      sum_p = lanes_sum<32>(sum_p);
+      cross = lanes_sum<32>(cross);
+      if (lane == 0) {
+        from_top[half] = {{kLowest, 0.f}, {m, dead ? nan : sum}, cross, sum_p, {}};
+        mbar_arrive(&summed[half]);
+      }
+      ++n;
+    }
+  } else if (warp == kWarps) {
+    // ---- the joiner
+    uint32_t n = 0;
+    for (uint32_t row = cluster; row < p.rows; row += clusters) {
+      const int kind = kind_of(row, weight);
+      if (kind == kRowNoWeight && rank == 0 && lane == 0) p.losses[row] = 0.f;
+      if (kind != kRowWork) continue;
+      const uint32_t half = n & 1;
+      if (!dead) dead = !mbar_wait_bounded(&summed[half], (n >> 1) & 1);
+      __syncwarp();
+      const float g = any_in[n % r.stages] ? weight * p.grad_scale : 0.f;  // a teacher that names nothing asks for nothing
+      RingSums x = from_top[half];
+      x.rest = warp_join(lane < kWarps ? from_warps[half][lane] : ExpSum{kLowest, 0.f}, p.c);
+      if (dead) x.rest.s = nan;
+      if (r.blocks > 1) {
+        if (lane == 0) mbar_expect_tx(&sums_here[half], r.blocks * 32u);
+        __syncwarp();
+        if (lane < r.blocks) send_sums(x, &from_blocks[half][rank], &sums_here[half], lane);
+        if (!dead) dead = !mbar_wait_bounded(&sums_here[half], (n >> 1) & 1);
+        __syncwarp();
+        x = lane < r.blocks ? from_blocks[half][lane] : RingSums{{kLowest, 0.f}, {kLowest, 0.f}, 0.f, 0.f, {}};
+        const float m_rest = warp_max(x.rest.m), m_top = warp_max(x.top.m);
+        x.rest.s *= exp2_fast((x.rest.m - m_rest) * p.c);
+        if (x.p != 0.f) x.cross += p.tau * (m_top - x.top.m) * x.p;
+        x.top.s *= exp2_fast((x.top.m - m_top) * p.c);
+        static_assert(kRingMaxCluster == 8, "sums over the first eight lanes");
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) {
+          x.rest.s += __shfl_xor_sync(0xffffffffu, x.rest.s, d);
+          x.top.s += __shfl_xor_sync(0xffffffffu, x.top.s, d);
+          x.p += __shfl_xor_sync(0xffffffffu, x.p, d);
+          x.cross += __shfl_xor_sync(0xffffffffu, x.cross, d);
+        }
+        x.rest.m = m_rest;
+        x.top.m = m_top;
+        if (dead) x.rest.s = nan;
+      }
+      // lanes 0 to 7 know the row
+      const ExpSum all = join(x.rest, x.top, p.c);
+      float p_rest = p.lse ? fmaxf(1.f - x.p, 0.f) : 0.f;
+      if (p.lse && x.p != x.p) p_rest = x.p;
+      if (x.rest.s == 0.f) p_rest = 0.f;
+      if (lane == 0) {
+        if constexpr (GRAD) {
+          const float over_s = 1.f / all.s;
+          answers[half] = {g * (exp2_fast((x.rest.m - all.m) * p.c) * over_s - (p_rest != 0.f ? p_rest / x.rest.s : 0.f)),
+                           x.rest.m, g, all.m, over_s};
+        }
+        mbar_arrive(&answered[half]);
+        if (rank == 0) {
+          const float log_s = log2f(all.s);
+          float loss = x.cross + p.loss_scale * log_s * x.p;
+          if (x.p != 0.f) loss += p.tau * (all.m - x.top.m) * x.p;
+          if (p_rest != 0.f)
+            loss += p_rest * (p.loss_scale * (log2f(p_rest) - log2f(x.rest.s) + log_s) + p.tau * (all.m - x.rest.m));
+          p.losses[row] = loss;
+        }
+      }
+      __syncwarp();
+      ++n;
+    }
+  } else {
+    // ---- the workers
+    uint32_t n = 0, row_before = 0;
+    unsigned char* late_at = nullptr;  // a gradient of the top that waits for the next barrier
+    float late = 0.f;
+    auto write_late = [&]() {
+      if (late_at) store_one<DT>(late_at, 0, late);
+      late_at = nullptr;
+    };
+    // pass 2 of the row that pass 1 was done of before the latest
+    auto finish = [&](uint32_t k, uint32_t row) {
+      if (!dead) dead = !mbar_wait_bounded(&answered[k & 1], (k >> 1) & 1);
+      unsigned char* const stage = stage_of(k);
+      if constexpr (GRAD) {
+        const int before = static_cast<int>(reinterpret_cast<uintptr_t>(row_of(p.z, row, 0)) & 15);
+        const int n_units = (before + p.vocab * ESZ + 15) / 16;
+        const int mine = min(r.units, n_units - first_unit);
+        const int ahead = before / ESZ;
+        unsigned char* const dz = row_of(p.dz, row, 0) - before + static_cast<int64_t>(first_unit) * 16;
+        const RingAnswer answer = answers[k & 1];
+        const float factor = dead ? nan : answer.factor;
+        if (tid < p.top) {
+          const RingTop top = top_of(stage);
+          const int at = top.place[tid];
+          if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U) &&
+              static_cast<unsigned>(at + first_unit * U - ahead) < static_cast<unsigned>(p.vocab)) {
+            late_at = dz + at * ESZ;
+            late = answer.g * (exp2_fast((top.z[tid] - answer.m_all) * p.c) * answer.over_s - top.log_p[tid]);
+          }
+        }
+        const uint64_t minus_m = pair_of(-answer.m, -answer.m), c = pair_of(p.c, p.c), f = pair_of(factor, factor);
+#pragma unroll
+        for (int q = 0; q < NU; ++q) {
+          const int u = tid + q * THREADS;
+          if (u >= mine) continue;
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          uint32_t out[4];
+#pragma unroll
+          for (int j = 0; j < U; j += 2) {
+            const float2 e = exp_pair<DT>(w, j, minus_m, c);
+            const float2 d = pair_as(pair_mul(pair_of(e.x, e.y), f));
+            if constexpr (DT == ABS_F32) {
+              out[j] = __float_as_uint(d.x);
+              out[j + 1] = __float_as_uint(d.y);
+            } else {
+              out[j / 2] = pack_16x2<DT>(d.x, d.y);
+            }
+          }
+          write_unit<DT>(dz + u * 16, (first_unit + u) * U - ahead, p.vocab, out);
+        }
+      }
+      // the stage has been read: the copy of a later row may overwrite it
+      fence_generic_to_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[k % r.stages]);
+    };
+
+    for (uint32_t row = cluster; row < p.rows; row += clusters) {
+      const int kind = kind_of(row, weight);
+      if (kind == kRowAlone) continue;
+      const unsigned char* const z = row_of(p.z, row, 0);
+      const int before = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15);
+      const int n_units = (before + p.vocab * ESZ + 15) / 16;
+      const int mine = min(r.units, n_units - first_unit);  // units of this block; may be negative
+      const int ahead = before / ESZ;                       // values before the row in unit 0
+      if (kind == kRowNoWeight) {
+        if constexpr (GRAD) {
+          const uint32_t none[4] = {};
+          unsigned char* const dz = row_of(p.dz, row, 0) - before + static_cast<int64_t>(first_unit) * 16;
+          for (int u = tid; u < mine; u += THREADS) write_unit<DT>(dz + u * 16, (first_unit + u) * U - ahead, p.vocab, none);
+        }
+        continue;
+      }
+      if (!dead) dead = !mbar_wait_bounded(&full[n % r.stages], (n / r.stages) & 1);
+      unsigned char* const stage = stage_of(n);
+
+      // values of the row's first and last unit: outside of the row, or not brought by the copy
+      if (tid < 2 * U) {
+        const int unit = tid < U ? 0 : n_units - 1;
+        const int j = tid % U;
+        if (unit >= first_unit && unit < first_unit + mine && (tid < U || n_units > 1)) {
+          const int i = unit * U + j - ahead;  // index in the row
+          const unsigned char* from = z - before + static_cast<int64_t>(unit) * 16;
+          unsigned char* to = stage + (unit - first_unit) * 16;
+          if (i < 0 || i >= p.vocab) {
+            store_one<DT>(to, j, -INFINITY);
+          } else if (from < r.z_begin || from + 16 > r.z_end) {
+            if constexpr (DT == ABS_F32) reinterpret_cast<uint32_t*>(to)[j] = reinterpret_cast<const uint32_t*>(from)[j];
+            else reinterpret_cast<unsigned short*>(to)[j] = reinterpret_cast<const unsigned short*>(from)[j];
+          }
+        }
+      }
+      const bool edges = (first_unit == 0 && z - before < r.z_begin) ||
+                         (first_unit + mine == n_units && z - before + static_cast<int64_t>(n_units) * 16 > r.z_end);
+      if (edges) workers_barrier<THREADS>();  // the top may lie among what has just been put there
+      if (tid < p.top) {
+        const RingTop top = top_of(stage);
+        const int at = top.place[tid];
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U)) {
+          top.z[tid] = load_one<DT>(stage, at);
+          store_one<DT>(stage, at, -INFINITY);
+        }
+      }
+      workers_barrier<THREADS>();
+      if (tid == 0) mbar_arrive(&taken[n & 1]);
+      if constexpr (GRAD) write_late();
+
+      // pass 1
+      uint32_t w[NU][4];
+      const uint32_t none = DT == ABS_F32 ? 0xff800000u : DT == ABS_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+      uint32_t top = none;
+#pragma unroll
+      for (int q = 0; q < NU; ++q) {
+        const int u = tid + q * THREADS;
+        uint4 v = make_uint4(none, none, none, none);
+        if (u < mine) v = *reinterpret_cast<const uint4*>(stage + u * 16);
+        w[q][0] = v.x;
+        w[q][1] = v.y;
+        w[q][2] = v.z;
+        w[q][3] = v.w;
+        top = max_words<DT>(top, max_words<DT>(max_words<DT>(v.x, v.y), max_words<DT>(v.z, v.w)));
+      }
+      const float m = warp_max(fmaxf(max_of_word<DT>(top), kLowest));
+      const uint64_t minus_m = pair_of(-m, -m), c = pair_of(p.c, p.c);
+      uint64_t sums = pair_of(0.f, 0.f);
+#pragma unroll
+      for (int q = 0; q < NU; ++q)
+#pragma unroll
+        for (int j = 0; j < U; j += 2) {
+          const float2 e = exp_pair<DT>(w[q], j, minus_m, c);
+          sums = pair_add(sums, pair_of(e.x, e.y));
+        }
+      const float2 both = pair_as(sums);
+      const float sum = lanes_sum<32>(dead ? nan : both.x + both.y);
+      if (lane == 0) {
+        from_warps[n & 1][warp] = {m, sum};
+        mbar_arrive(&summed[n & 1]);
+      }
+      if (n > 0) finish(n - 1, row_before);
+      row_before = row;
+      ++n;
+    }
+    if (n > 0) {
+      if constexpr (GRAD) {
+        workers_barrier<THREADS>();
+        write_late();
+      }
+      finish(n - 1, row_before);
+      if constexpr (GRAD) {
+        workers_barrier<THREADS>();
+        write_late();
+      }
+    }
+  }
+  // no block leaves while another may still send sums to it
+  __syncthreads();
+  if (r.blocks > 1) cluster_barrier();
+}
+
+}  // namespace absnt

@@ -15,6 +15,8 @@
 
 namespace absnt {
 
+constexpr int kSMs = 148;
+
 // Launch with the programmatic-stream-serialization attribute (see grid_dependency_wait).
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t st,

@@ -6,7 +6,6 @@
 
 namespace absnt {
 
-constexpr int kSMs = 148;
 // the widest row: 32 warps of 16 values a lane
 constexpr int kMaxNormWidth = 32 * 32 * 16;
 
