@@ -33,23 +33,22 @@ struct RingShape {
   int blocks, threads, units, stages, stage_bytes;
   size_t smem;
 };
-constexpr int kRingUnits = 4;  // of a worker: 32 values of 16 bits, 16 floats
+constexpr int kRingUnits = 8;  // of a worker, at most: 64 values of 16 bits, 32 floats
 constexpr int kRingSmemPerSM = 228 * 1024, kRingStatic = 3 * 1024;  // the latter with what a block takes anyway
 constexpr int kRingSmemMost = 224 * 1024;                            // dynamic, of a block that has an SM to itself
 
 inline RingShape ring_shape(const DistillParams& p, int esz) {
   RingShape s = {};
   const int64_t total = (16 - esz + static_cast<int64_t>(p.vocab) * esz + 15) / 16;  // with the worst alignment
-  // as few blocks as hold a row with two blocks on an SM; with 928 workers and one block if that is too many
-  int64_t blocks = (total + 512 * kRingUnits - 1) / (512 * kRingUnits);
-  if (blocks > kRingMaxCluster) blocks = (total + 928 * kRingUnits - 1) / (928 * kRingUnits);
+  // as few blocks as hold a row with two blocks on an SM; with 512 workers and one block if that is too many
+  int64_t blocks = (total + 256 * kRingUnits - 1) / (256 * kRingUnits);
+  if (blocks > kRingMaxCluster) blocks = (total + 512 * kRingUnits - 1) / (512 * kRingUnits);
   if (blocks > kRingMaxCluster) return s;
   // few rows: every SM gets a part of one, down to 4 KB
   while (blocks * 2 <= kRingMaxCluster && p.rows * blocks * 2 <= kSMs && total / (blocks * 2) >= 256) blocks *= 2;
   s.units = static_cast<int>((total + blocks - 1) / blocks);
   s.threads = 128;
-  while (s.threads <= 512 && (s.threads * kRingUnits < s.units || s.threads < p.top)) s.threads *= 2;
-  if (s.threads > 512) s.threads = 928;
+  while (s.threads * kRingUnits < s.units || s.threads < p.top) s.threads *= 2;
   s.stage_bytes = s.units * 16 + p.top * 16;
   const int marks = (s.units * (16 / esz) + 31) / 32 * 4;
   for (int per_sm = ring_blocks_per_sm(s.threads);; per_sm = (per_sm + 1) / 2) {
@@ -66,7 +65,7 @@ inline RingShape ring_shape(const DistillParams& p, int esz) {
 
 template <int DT, int THREADS, bool GRAD>
 cudaError_t distill_by_ring(const DistillParams& p, const RingShape& s, cudaStream_t st) {
-  const auto kernel = distill_ring_kernel<DT, THREADS, kRingUnits, GRAD>;
+  const auto kernel = distill_ring_kernel<DT, THREADS, GRAD>;
   cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kRingSmemMost);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -102,8 +101,7 @@ template <int DT, bool GRAD>
 cudaError_t distill_by_ring_of(const DistillParams& p, const RingShape& s, cudaStream_t st) {
   if (s.threads == 128) return distill_by_ring<DT, 128, GRAD>(p, s, st);
   if (s.threads == 256) return distill_by_ring<DT, 256, GRAD>(p, s, st);
-  if (s.threads == 512) return distill_by_ring<DT, 512, GRAD>(p, s, st);
-  return distill_by_ring<DT, 928, GRAD>(p, s, st);
+  return distill_by_ring<DT, 512, GRAD>(p, s, st);
 }
 
 // vec: 8 where all rows of logits and gradient begin on boundaries of eight values, else 1

@@ -24,6 +24,8 @@
 #include "distill.cuh"
 #include "normtest_bulk.cuh"
 
+#include <type_traits>
+
 namespace absnt {
 
 constexpr int kRingMaxCluster = 8;
@@ -96,9 +98,21 @@ __device__ __forceinline__ void send_sums(const RingSums& x, RingSums* to, uint6
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
+// Barriers between the parts of a block.  A warp that waits at one takes no issue slots, one that polls an mbarrier
+// does (a failed look comes back after some thirty cycles); and as every warp comes to each of them
+// whatever has become of the mbarriers, none of them waits for good.
 template <int N>
-__device__ __forceinline__ void workers_barrier() {  // all warps but the feeder
+__device__ __forceinline__ void workers_barrier() {
   asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+}
+enum { kTopTaken = 2, kSummed = 4, kAnswered = 6 };  // and one more each: of rows by turns
+template <int N>
+__device__ __forceinline__ void part_sync(int id) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void part_arrive(int id) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(N) : "memory");
 }
 
 template <int DT>
@@ -113,7 +127,7 @@ __device__ __forceinline__ float value_of(const uint32_t (&w)[4], int j) {
 }
 
 
-// two floats at once: one instruction slot
+// two floats in one instruction slot
 __device__ __forceinline__ uint64_t pair_of(float a, float b) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
@@ -134,12 +148,31 @@ __device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-// 2^((z - m) c) of two values, as a pair
-template <int DT>
-__device__ __forceinline__ float2 exp_pair(const uint32_t (&w)[4], int j, uint64_t minus_m, uint64_t c) {
-  const float2 a = pair_as(pair_mul(pair_add(pair_of(value_of<DT>(w, j), value_of<DT>(w, j + 1)), minus_m), c));
-  return make_float2(exp2_fast(a.x), exp2_fast(a.y));
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
 }
+// 2^((z - m) c) as 2^(z c - r) with r the rounded m c: one fma and one exponential.  What the rounding of r costs is
+// the same factor for all values, 2^(m c - r), and is taken back once, in `correction`.  Where m c may not be a float
+// (m a masking value, or as large) values differ by so much that only those that equal m count; an infinite m and a NaN
+// among the values give NaN.
+struct Exponentials {
+  float m, c, minus_r, correction;
+  bool far;
+  __device__ __forceinline__ Exponentials(float m_, float c_) : m(m_), c(c_) {
+    far = !(fabsf(m) < 1e36f);
+    minus_r = -(m * c);
+    correction = far ? 1.f : exp2_fast(-fmaf(m, c, minus_r));
+  }
+  __device__ __forceinline__ uint64_t operator()(float a, float b) const {
+    const float2 x = pair_as(pair_fma(pair_of(a, b), pair_of(c, c), pair_of(minus_r, minus_r)));
+    return pair_of(exp2_fast(x.x), exp2_fast(x.y));
+  }
+  __device__ __forceinline__ float of_far(float z) const {
+    return z == m ? 1.f + (m - m) : z < m ? 0.f : __uint_as_float(0x7fffffffu);
+  }
+};
 // the larger of two words of values, place by place
 template <int DT>
 __device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b) {
@@ -171,10 +204,10 @@ __device__ __forceinline__ void write_unit(unsigned char* to, int i0, int vocab,
     }
 }
 
-constexpr int ring_blocks_per_sm(int threads) { return threads == 128 ? 5 : 1024 / threads; }  // 928: 1
+constexpr int ring_blocks_per_sm(int threads) { return 512 / threads; }
 
-// THREADS (at most 928) workers and three special warps; a worker takes up to NU units of a row
-template <int DT, int THREADS, int NU, bool GRAD>
+// THREADS workers and three special warps
+template <int DT, int THREADS, bool GRAD>
 __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
     distill_ring_kernel(const __grid_constant__ RingParams r) {
   constexpr int U = unit_values<DT>();
@@ -183,7 +216,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
   const DistillParams& p = r.d;
   extern __shared__ __align__(16) unsigned char ring[];  // the stages, then a bit for each place of the block's run
   __shared__ __align__(8) uint64_t full[kRingMaxStages], empty[kRingMaxStages];
-  __shared__ __align__(8) uint64_t taken[2], summed[2], answered[2], sums_here[2];
+  __shared__ __align__(8) uint64_t sums_here[2];
   __shared__ int repeated_in[kRingMaxStages];  // an index of this block's run is named twice
   __shared__ int any_in[kRingMaxStages];       // the teacher names something
   __shared__ __align__(16) ExpSum from_warps[2][kWarps];
@@ -203,12 +236,8 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       mbar_init(&full[s], 2);        // the copy has been asked for; the top's entries are there
       mbar_init(&empty[s], kWarps);
     }
-    for (int k = 0; k < 2; ++k) {
-      mbar_init(&taken[k], 1);           // the top's logits
-      mbar_init(&summed[k], kWarps + 1); // by workers and topper
-      mbar_init(&answered[k], 1);
-      mbar_init(&sums_here[k], 1);
-    }
+    mbar_init(&sums_here[0], 1);
+    mbar_init(&sums_here[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   for (int i = tid; i < (r.units * U + 31) / 32; i += THREADS + 96) marks[i] = 0u;
@@ -233,9 +262,19 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
     }
     weight = __shfl_sync(0xffffffffu, weights_ahead, seen & 31);
     ++seen;
-    return row < low || row >= high ? kRowAlone : weight == 0.f ? kRowNoWeight : kRowWork;
+    return row < low || row >= high ? kRowAlone : __any_sync(0xffffffffu, weight != 0.f) ? kRowWork : kRowNoWeight;
   };
-  auto stage_of = [&](uint32_t n) { return ring + (n % r.stages) * r.stage_bytes; };
+  struct Place {  // of row n in the ring: n = turn * stages + s
+    int s, turn, stages;
+    __device__ __forceinline__ void next() {
+      if (++s == stages) {
+        s = 0;
+        ++turn;
+      }
+    }
+  };
+  Place ring_n{0, 0, r.stages};
+  auto stage_of = [&](const Place& x) { return ring + x.s * r.stage_bytes; };
   auto top_of = [&](unsigned char* stage) {
     int* const place = reinterpret_cast<int*>(stage + r.units * 16);
     float* const z = reinterpret_cast<float*>(place + p.top);
@@ -244,12 +283,13 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
   float weight;
 
   if (warp == kWarps + 2) {
-    // ---- the feeder; the first 64 entries of a row are asked for while the row before is prepared
+    // ---- the feeder; the first 64 entries of a row are asked for while the row before is prepared (as words that
+    // nothing is done with until then: a conversion would wait for them)
     constexpr int kAhead = 2;
     struct Ahead {
       int64_t row;
-      int id[kAhead];
-      float t[kAhead], lse;
+      uint32_t id[kAhead], id_high[kAhead], t[kAhead];
+      float lse;
     };
     uint32_t next_row = cluster;
     auto look_ahead = [&]() {
@@ -262,8 +302,18 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
           const int j = lane + 32 * k;
-          x.id[k] = j < p.top ? load_id(p, row, j) : -1;
-          x.t[k] = j < p.top ? load_teacher(p, row, j) : 0.f;
+          x.id[k] = x.id_high[k] = x.t[k] = 0u;
+          if (j < p.top) {
+            const uint32_t* const id = reinterpret_cast<const uint32_t*>(p.ids + static_cast<int64_t>(row) * p.ids_stride);
+            if (p.id_bytes == 8) {
+              x.id[k] = id[2 * j];
+              x.id_high[k] = id[2 * j + 1];
+            } else {
+              x.id[k] = id[j];
+            }
+            const unsigned char* const t = row_of(p.t, row, 0);
+            x.t[k] = p.t_dtype == ABS_F32 ? reinterpret_cast<const uint32_t*>(t)[j] : reinterpret_cast<const unsigned short*>(t)[j];
+          }
         }
         x.lse = p.lse ? p.lse[row] : 0.f;
       }
@@ -274,10 +324,10 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
     while (now.row >= 0) {
       const Ahead next = look_ahead();
       const uint32_t row = static_cast<uint32_t>(now.row);
-      const uint32_t s = n % r.stages, turn = n / r.stages;
-      if (turn > 0 && !dead) dead = !mbar_wait_bounded(&empty[s], (turn - 1) & 1);
+      const int s = ring_n.s;
+      if (ring_n.turn > 0 && !dead) dead = !mbar_wait_bounded(&empty[s], (ring_n.turn - 1) & 1);
       __syncwarp();
-      unsigned char* const stage = stage_of(n);
+      unsigned char* const stage = stage_of(ring_n);
       // the units of this block; the first and last of the row may reach out of the tensor at its ends
       const unsigned char* z = row_of(p.z, row, 0);
       const int before = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15);
@@ -309,7 +359,14 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       };
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
-        if (lane + 32 * k < p.top) take(lane + 32 * k, now.id[k], now.t[k]);
+        if (lane + 32 * k < p.top) {
+          // an index of 8 bytes is one of the vocabulary's if its high word is 0 and its low word is
+          const bool known = now.id_high[k] == 0u && now.id[k] < static_cast<uint32_t>(p.vocab);
+          const float t = p.t_dtype == ABS_F32    ? __uint_as_float(now.t[k])
+                          : p.t_dtype == ABS_BF16 ? from_half_word<ABS_BF16>(now.t[k])
+                                                  : from_half_word<ABS_F16>(now.t[k]);
+          take(lane + 32 * k, known ? static_cast<int>(now.id[k]) : -1, t);
+        }
       for (int j = lane + 32 * kAhead; j < p.top; j += 32) {
         const float t = load_teacher(p, row, j);
         take(j, load_id(p, row, j), t);
@@ -337,6 +394,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       __syncwarp();
       if (lane == 0) mbar_arrive(&full[s]);
       now = next;
+      ring_n.next();
       ++n;
     }
     // no copy is under way when the block ends, even where a worker gave up on one
@@ -348,10 +406,10 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
     for (uint32_t row = cluster; row < p.rows; row += clusters) {
       if (kind_of(row, weight) != kRowWork) continue;
       const uint32_t half = n & 1;
-      if (!dead) dead = !mbar_wait_bounded(&taken[half], (n >> 1) & 1);
-      __syncwarp();
-      const RingTop top = top_of(stage_of(n));
-      const bool repeated = repeated_in[n % r.stages];
+      part_sync<64>(kTopTaken + half);
+      const RingTop top = top_of(stage_of(ring_n));
+      const bool repeated = repeated_in[ring_n.s];
+      ring_n.next();
       float m = kLowest, sum = 0.f, sum_p = 0.f, cross = 0.f;
       for (int j = lane; j < p.top; j += 32)
         if (top.place[j] >= 0) m = fmaxf(m, top.z[j]);
@@ -380,10 +438,9 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       sum = lanes_sum<32>(sum);
       sum_p = lanes_sum<32>(sum_p);
       cross = lanes_sum<32>(cross);
-      if (lane == 0) {
-        from_top[half] = {{kLowest, 0.f}, {m, dead ? nan : sum}, cross, sum_p, {}};
-        mbar_arrive(&summed[half]);
-      }
+      if (lane == 0)
+        from_top[half] = {{kLowest, 0.f}, {m, sum}, cross, sum_p, {}};
+      part_arrive<THREADS + 64>(kSummed + half);
       ++n;
     }
   } else if (warp == kWarps) {
@@ -394,9 +451,9 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       if (kind == kRowNoWeight && rank == 0 && lane == 0) p.losses[row] = 0.f;
       if (kind != kRowWork) continue;
       const uint32_t half = n & 1;
-      if (!dead) dead = !mbar_wait_bounded(&summed[half], (n >> 1) & 1);
-      __syncwarp();
-      const float g = any_in[n % r.stages] ? weight * p.grad_scale : 0.f;  // a teacher that names nothing asks for nothing
+      part_sync<THREADS + 64>(kSummed + half);
+      const float g = any_in[ring_n.s] ? weight * p.grad_scale : 0.f;  // a teacher that names nothing asks for nothing
+      ring_n.next();
       RingSums x = from_top[half];
       x.rest = warp_join(lane < kWarps ? from_warps[half][lane] : ExpSum{kLowest, 0.f}, p.c);
       if (dead) x.rest.s = nan;
@@ -428,179 +485,199 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       float p_rest = p.lse ? fmaxf(1.f - x.p, 0.f) : 0.f;
       if (p.lse && x.p != x.p) p_rest = x.p;
       if (x.rest.s == 0.f) p_rest = 0.f;
-      if (lane == 0) {
-        if constexpr (GRAD) {
-          const float over_s = 1.f / all.s;
-          answers[half] = {g * (exp2_fast((x.rest.m - all.m) * p.c) * over_s - (p_rest != 0.f ? p_rest / x.rest.s : 0.f)),
-                           x.rest.m, g, all.m, over_s};
-        }
-        mbar_arrive(&answered[half]);
-        if (rank == 0) {
-          const float log_s = log2f(all.s);
-          float loss = x.cross + p.loss_scale * log_s * x.p;
-          if (x.p != 0.f) loss += p.tau * (all.m - x.top.m) * x.p;
-          if (p_rest != 0.f)
-            loss += p_rest * (p.loss_scale * (log2f(p_rest) - log2f(x.rest.s) + log_s) + p.tau * (all.m - x.rest.m));
-          p.losses[row] = loss;
-        }
+      if (GRAD && lane == 0) {
+        const float over_s = 1.f / all.s;
+        answers[half] = {g * (exp2_fast((x.rest.m - all.m) * p.c) * over_s - (p_rest != 0.f ? p_rest / x.rest.s : 0.f)),
+                         x.rest.m, g, all.m, over_s};
+      }
+      part_arrive<THREADS + 32>(kAnswered + half);
+      if (rank == 0 && lane == 0) {
+        const float log_s = log2f(all.s);
+        float loss = x.cross + p.loss_scale * log_s * x.p;
+        if (x.p != 0.f) loss += p.tau * (all.m - x.top.m) * x.p;
+        if (p_rest != 0.f)
+          loss += p_rest * (p.loss_scale * (log2f(p_rest) - log2f(x.rest.s) + log_s) + p.tau * (all.m - x.rest.m));
+        p.losses[row] = loss;
       }
       __syncwarp();
       ++n;
     }
   } else {
     // ---- the workers
-    uint32_t n = 0, row_before = 0;
+    uint32_t row = cluster;
     unsigned char* late_at = nullptr;  // a gradient of the top that waits for the next barrier
     float late = 0.f;
     auto write_late = [&]() {
       if (late_at) store_one<DT>(late_at, 0, late);
       late_at = nullptr;
     };
-    // pass 2 of the row that pass 1 was done of before the latest
-    auto finish = [&](uint32_t k, uint32_t row) {
-      if (!dead) dead = !mbar_wait_bounded(&answered[k & 1], (k >> 1) & 1);
-      unsigned char* const stage = stage_of(k);
-      if constexpr (GRAD) {
-        const int before = static_cast<int>(reinterpret_cast<uintptr_t>(row_of(p.z, row, 0)) & 15);
-        const int n_units = (before + p.vocab * ESZ + 15) / 16;
-        const int mine = min(r.units, n_units - first_unit);
-        const int ahead = before / ESZ;
-        unsigned char* const dz = row_of(p.dz, row, 0) - before + static_cast<int64_t>(first_unit) * 16;
-        const RingAnswer answer = answers[k & 1];
-        const float factor = dead ? nan : answer.factor;
+    // the row whose pass 2 is still to come
+    uint32_t n = 0;
+    Place ring_before = ring_n;
+    unsigned char* dz_before = nullptr;  // of this block's first unit
+    int mine_before = 0, i_before = 0;
+    for (;;) {
+      // the next row to work on; those that do not count on the way
+      const unsigned char* z = nullptr;
+      unsigned char* dz = nullptr;
+      int before = 0, n_units = 0, mine = 0, i_first = 0;
+      bool have = false;
+      for (; row < p.rows && !have; row += clusters) {
+        const int kind = kind_of(row, weight);
+        if (kind == kRowAlone) continue;
+        z = row_of(p.z, row, 0);
+        before = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15);
+        n_units = (before + p.vocab * ESZ + 15) / 16;
+        mine = min(r.units, n_units - first_unit);   // units of this block; may be negative
+        i_first = first_unit * U - before / ESZ;     // index of its first value in the row; may be negative
+        if constexpr (GRAD) dz = row_of(p.dz, row, 0) - before + static_cast<int64_t>(first_unit) * 16;
+        have = kind == kRowWork;
+        if (GRAD && !have) {
+          const uint32_t none[4] = {};
+          for (int u = tid; u < mine; u += THREADS) write_unit<DT>(dz + u * 16, i_first + u * U, p.vocab, none);
+        }
+      }
+      unsigned char* const stage = stage_of(ring_n);
+      // Every piece of a copy that lands wakes whoever waits for the whole: only the warps that have something to do
+      // before the barrier wait for it there (with all of them at it, polling took four of ten instructions); the
+      // others look once behind the barrier, when it has landed.
+      const bool early = warp * 32 < max(p.top, 2 * U);
+      if (have) {
+        if (early && !dead) dead = !mbar_wait_bounded(&full[ring_n.s], ring_n.turn & 1);
+        // values of the row's first and last unit: outside of the row, or not brought by the copy
+        if (tid < 2 * U) {
+          const int unit = tid < U ? 0 : n_units - 1;
+          const int j = tid % U;
+          if (unit >= first_unit && unit < first_unit + mine && (tid < U || n_units > 1)) {
+            const int i = i_first + (unit - first_unit) * U + j;  // index in the row
+            const unsigned char* from = z - before + static_cast<int64_t>(unit) * 16;
+            unsigned char* to = stage + (unit - first_unit) * 16;
+            if (i < 0 || i >= p.vocab) {
+              store_one<DT>(to, j, -INFINITY);
+            } else if (from < r.z_begin || from + 16 > r.z_end) {
+              if constexpr (DT == ABS_F32) reinterpret_cast<uint32_t*>(to)[j] = reinterpret_cast<const uint32_t*>(from)[j];
+              else reinterpret_cast<unsigned short*>(to)[j] = reinterpret_cast<const unsigned short*>(from)[j];
+            }
+          }
+        }
+        const bool edges = (first_unit == 0 && z - before < r.z_begin) ||
+                           (first_unit + mine == n_units && z - before + static_cast<int64_t>(n_units) * 16 > r.z_end);
+        if (edges) workers_barrier<THREADS>();  // the top may lie among what has just been put there
         if (tid < p.top) {
           const RingTop top = top_of(stage);
           const int at = top.place[tid];
-          if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U) &&
-              static_cast<unsigned>(at + first_unit * U - ahead) < static_cast<unsigned>(p.vocab)) {
-            late_at = dz + at * ESZ;
-            late = answer.g * (exp2_fast((top.z[tid] - answer.m_all) * p.c) * answer.over_s - top.log_p[tid]);
+          if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U)) {
+            top.z[tid] = load_one<DT>(stage, at);
+            store_one<DT>(stage, at, -INFINITY);
           }
-        }
-        const uint64_t minus_m = pair_of(-answer.m, -answer.m), c = pair_of(p.c, p.c), f = pair_of(factor, factor);
-#pragma unroll
-        for (int q = 0; q < NU; ++q) {
-          const int u = tid + q * THREADS;
-          if (u >= mine) continue;
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          uint32_t out[4];
-#pragma unroll
-          for (int j = 0; j < U; j += 2) {
-            const float2 e = exp_pair<DT>(w, j, minus_m, c);
-            const float2 d = pair_as(pair_mul(pair_of(e.x, e.y), f));
-            if constexpr (DT == ABS_F32) {
-              out[j] = __float_as_uint(d.x);
-              out[j + 1] = __float_as_uint(d.y);
-            } else {
-              out[j / 2] = pack_16x2<DT>(d.x, d.y);
-            }
-          }
-          write_unit<DT>(dz + u * 16, (first_unit + u) * U - ahead, p.vocab, out);
-        }
-      }
-      // the stage has been read: the copy of a later row may overwrite it
-      fence_generic_to_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&empty[k % r.stages]);
-    };
-
-    for (uint32_t row = cluster; row < p.rows; row += clusters) {
-      const int kind = kind_of(row, weight);
-      if (kind == kRowAlone) continue;
-      const unsigned char* const z = row_of(p.z, row, 0);
-      const int before = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15);
-      const int n_units = (before + p.vocab * ESZ + 15) / 16;
-      const int mine = min(r.units, n_units - first_unit);  // units of this block; may be negative
-      const int ahead = before / ESZ;                       // values before the row in unit 0
-      if (kind == kRowNoWeight) {
-        if constexpr (GRAD) {
-          const uint32_t none[4] = {};
-          unsigned char* const dz = row_of(p.dz, row, 0) - before + static_cast<int64_t>(first_unit) * 16;
-          for (int u = tid; u < mine; u += THREADS) write_unit<DT>(dz + u * 16, (first_unit + u) * U - ahead, p.vocab, none);
-        }
-        continue;
-      }
-      if (!dead) dead = !mbar_wait_bounded(&full[n % r.stages], (n / r.stages) & 1);
-      unsigned char* const stage = stage_of(n);
-
-      // values of the row's first and last unit: outside of the row, or not brought by the copy
-      if (tid < 2 * U) {
-        const int unit = tid < U ? 0 : n_units - 1;
-        const int j = tid % U;
-        if (unit >= first_unit && unit < first_unit + mine && (tid < U || n_units > 1)) {
-          const int i = unit * U + j - ahead;  // index in the row
-          const unsigned char* from = z - before + static_cast<int64_t>(unit) * 16;
-          unsigned char* to = stage + (unit - first_unit) * 16;
-          if (i < 0 || i >= p.vocab) {
-            store_one<DT>(to, j, -INFINITY);
-          } else if (from < r.z_begin || from + 16 > r.z_end) {
-            if constexpr (DT == ABS_F32) reinterpret_cast<uint32_t*>(to)[j] = reinterpret_cast<const uint32_t*>(from)[j];
-            else reinterpret_cast<unsigned short*>(to)[j] = reinterpret_cast<const unsigned short*>(from)[j];
-          }
-        }
-      }
-      const bool edges = (first_unit == 0 && z - before < r.z_begin) ||
-                         (first_unit + mine == n_units && z - before + static_cast<int64_t>(n_units) * 16 > r.z_end);
-      if (edges) workers_barrier<THREADS>();  // the top may lie among what has just been put there
-      if (tid < p.top) {
-        const RingTop top = top_of(stage);
-        const int at = top.place[tid];
-        if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U)) {
-          top.z[tid] = load_one<DT>(stage, at);
-          store_one<DT>(stage, at, -INFINITY);
         }
       }
       workers_barrier<THREADS>();
-      if (tid == 0) mbar_arrive(&taken[n & 1]);
       if constexpr (GRAD) write_late();
 
-      // pass 1
-      uint32_t w[NU][4];
-      const uint32_t none = DT == ABS_F32 ? 0xff800000u : DT == ABS_BF16 ? 0xff80ff80u : 0xfc00fc00u;
-      uint32_t top = none;
-#pragma unroll
-      for (int q = 0; q < NU; ++q) {
-        const int u = tid + q * THREADS;
-        uint4 v = make_uint4(none, none, none, none);
-        if (u < mine) v = *reinterpret_cast<const uint4*>(stage + u * 16);
-        w[q][0] = v.x;
-        w[q][1] = v.y;
-        w[q][2] = v.z;
-        w[q][3] = v.w;
-        top = max_words<DT>(top, max_words<DT>(max_words<DT>(v.x, v.y), max_words<DT>(v.z, v.w)));
-      }
-      const float m = warp_max(fmaxf(max_of_word<DT>(top), kLowest));
-      const uint64_t minus_m = pair_of(-m, -m), c = pair_of(p.c, p.c);
-      uint64_t sums = pair_of(0.f, 0.f);
-#pragma unroll
-      for (int q = 0; q < NU; ++q)
-#pragma unroll
-        for (int j = 0; j < U; j += 2) {
-          const float2 e = exp_pair<DT>(w[q], j, minus_m, c);
-          sums = pair_add(sums, pair_of(e.x, e.y));
+      if (have) {  // pass 1
+        if (!early && !dead) dead = !mbar_wait_bounded(&full[ring_n.s], ring_n.turn & 1);
+        if (warp == 0) part_arrive<64>(kTopTaken + (n & 1));
+        uint32_t top = DT == ABS_F32 ? 0xff800000u : DT == ABS_BF16 ? 0xff80ff80u : 0xfc00fc00u;
+        for (int u = tid; u < mine; u += THREADS) {
+          const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
+          top = max_words<DT>(top, max_words<DT>(max_words<DT>(v.x, v.y), max_words<DT>(v.z, v.w)));
         }
-      const float2 both = pair_as(sums);
-      const float sum = lanes_sum<32>(dead ? nan : both.x + both.y);
-      if (lane == 0) {
-        from_warps[n & 1][warp] = {m, sum};
-        mbar_arrive(&summed[n & 1]);
+        const float m = warp_max(fmaxf(max_of_word<DT>(top), kLowest));
+        const Exponentials ex(m, p.c);
+        uint64_t pairs = pair_of(0.f, 0.f);
+        float sum = 0.f;
+        if (!ex.far) {
+#pragma unroll 2
+          for (int u = tid; u < mine; u += THREADS) {
+            const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < U; j += 2) pairs = pair_add(pairs, ex(value_of<DT>(w, j), value_of<DT>(w, j + 1)));
+          }
+          sum = (pair_as(pairs).x + pair_as(pairs).y) * ex.correction;
+        } else {
+#pragma unroll 1
+          for (int u = tid; u < mine; u += THREADS)
+#pragma unroll 1
+            for (int j = 0; j < U; ++j) sum += ex.of_far(load_one<DT>(stage, u * U + j));
+        }
+        sum = lanes_sum<32>(dead ? nan : sum);
+        if (lane == 0) from_warps[n & 1][warp] = {m, sum};
+        part_arrive<THREADS + 64>(kSummed + (n & 1));
       }
-      if (n > 0) finish(n - 1, row_before);
-      row_before = row;
+
+      if (n > 0) {  // pass 2 of the row before
+        const uint32_t half = (n - 1) & 1;
+        part_sync<THREADS + 32>(kAnswered + half);
+        if constexpr (GRAD) {
+          unsigned char* const stage_before = stage_of(ring_before);
+          const RingAnswer answer = answers[half];
+          if (tid < p.top) {
+            const RingTop top = top_of(stage_before);
+            const int at = top.place[tid];
+            if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U) &&
+                static_cast<unsigned>(i_before + at) < static_cast<unsigned>(p.vocab)) {
+              late_at = dz_before + at * ESZ;
+              late = answer.g * (exp2_fast((top.z[tid] - answer.m_all) * p.c) * answer.over_s - top.log_p[tid]);
+            }
+          }
+          const Exponentials ex(answer.m, p.c);
+          const float f = dead ? nan : answer.factor * ex.correction;
+          // the units that lie in the row whole, then its first and last by a thread each
+          const int from = i_before < 0 ? 1 : 0;
+          const int to = i_before + mine_before * U > p.vocab ? mine_before - 1 : mine_before;
+          if (!ex.far) {
+            const uint64_t ff = pair_of(f, f);
+            auto unit = [&](int u, uint32_t (&out)[4]) {
+              const uint4 v = *reinterpret_cast<const uint4*>(stage_before + u * 16);
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int j = 0; j < U; j += 2) {
+                const float2 d = pair_as(pair_mul(ex(value_of<DT>(w, j), value_of<DT>(w, j + 1)), ff));
+                if constexpr (DT == ABS_F32) {
+                  out[j] = __float_as_uint(d.x);
+                  out[j + 1] = __float_as_uint(d.y);
+                } else {
+                  out[j / 2] = pack_16x2<DT>(d.x, d.y);
+                }
+              }
+            };
+            uint32_t out[4];
+#pragma unroll 2
+            for (int u = from + tid; u < to; u += THREADS) {
+              unit(u, out);
+              *reinterpret_cast<uint4*>(dz_before + u * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+            }
+            const int u = tid == 0 && from > 0 ? 0 : to;
+            if ((tid == 0 && from > 0 && mine_before > 0) || (tid == (from > 0 ? 32 : 0) && to >= from && to < mine_before)) {
+              unit(u, out);
+              write_unit<DT>(dz_before + u * 16, i_before + u * U, p.vocab, out);
+            }
+          } else {
+#pragma unroll 1
+            for (int u = tid; u < mine_before; u += THREADS)
+#pragma unroll 1
+              for (int k = u * U; k < u * U + U; ++k)
+                if (i_before + k >= 0 && i_before + k < p.vocab)
+                  store_one<DT>(dz_before, k, f * ex.of_far(load_one<DT>(stage_before, k)));
+          }
+        }
+        // the stage has been read: the copy of a later row may overwrite it
+        fence_generic_to_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&empty[ring_before.s]);
+      }
+      if (!have) break;
+      ring_before = ring_n;
+      dz_before = dz;
+      mine_before = mine;
+      i_before = i_first;
+      ring_n.next();
       ++n;
     }
-    if (n > 0) {
-      if constexpr (GRAD) {
-        workers_barrier<THREADS>();
-        write_late();
-      }
-      finish(n - 1, row_before);
-      if constexpr (GRAD) {
-        workers_barrier<THREADS>();
-        write_late();
-      }
-    }
+    workers_barrier<THREADS>();
+    if constexpr (GRAD) write_late();
   }
   // no block leaves while another may still send sums to it
   __syncthreads();
