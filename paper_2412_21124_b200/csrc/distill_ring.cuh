@@ -204,6 +204,28 @@ __device__ __forceinline__ void write_unit(unsigned char* to, int i0, int vocab,
     }
 }
 
+// Units u, u + STEP, ... below `end` of a stage, two at a time (one, three or four: 1 to 9% slower).
+template <int STEP, typename F>
+__device__ __forceinline__ void for_units(int u, int end, const unsigned char* stage, F f) {
+  constexpr int kAtOnce = 2;
+  for (; u + (kAtOnce - 1) * STEP < end; u += kAtOnce * STEP) {
+    uint4 v[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) v[k] = *reinterpret_cast<const uint4*>(stage + (u + k * STEP) * 16);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+      f(u + k * STEP, w);
+    }
+  }
+#pragma unroll 1
+  for (; u < end; u += STEP) {
+    const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    f(u, w);
+  }
+}
+
 constexpr int ring_blocks_per_sm(int threads) { return 512 / threads; }
 
 // THREADS workers and three special warps
@@ -579,22 +601,24 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
         if (!early && !dead) dead = !mbar_wait_bounded(&full[ring_n.s], ring_n.turn & 1);
         if (warp == 0) part_arrive<64>(kTopTaken + (n & 1));
         uint32_t top = DT == ABS_F32 ? 0xff800000u : DT == ABS_BF16 ? 0xff80ff80u : 0xfc00fc00u;
-        for (int u = tid; u < mine; u += THREADS) {
-          const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
-          top = max_words<DT>(top, max_words<DT>(max_words<DT>(v.x, v.y), max_words<DT>(v.z, v.w)));
-        }
+        for_units<THREADS>(tid, mine, stage, [&](int, const uint32_t (&w)[4]) {
+          top = max_words<DT>(top, max_words<DT>(max_words<DT>(w[0], w[1]), max_words<DT>(w[2], w[3])));
+        });
         const float m = warp_max(fmaxf(max_of_word<DT>(top), kLowest));
         const Exponentials ex(m, p.c);
         uint64_t pairs = pair_of(0.f, 0.f);
         float sum = 0.f;
         if (!ex.far) {
-#pragma unroll 2
-          for (int u = tid; u < mine; u += THREADS) {
-            const uint4 v = *reinterpret_cast<const uint4*>(stage + u * 16);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          for_units<THREADS>(tid, mine, stage, [&](int, const uint32_t (&w)[4]) {
+            uint64_t e[U / 2];
 #pragma unroll
-            for (int j = 0; j < U; j += 2) pairs = pair_add(pairs, ex(value_of<DT>(w, j), value_of<DT>(w, j + 1)));
-          }
+            for (int j = 0; j < U; j += 2) e[j / 2] = ex(value_of<DT>(w, j), value_of<DT>(w, j + 1));
+#pragma unroll
+            for (int d = U / 4; d > 0; d /= 2)
+#pragma unroll
+              for (int j = 0; j < d; ++j) e[j] = pair_add(e[j], e[j + d]);
+            pairs = pair_add(pairs, e[0]);
+          });
           sum = (pair_as(pairs).x + pair_as(pairs).y) * ex.correction;
         } else {
 #pragma unroll 1
@@ -629,9 +653,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
           const int to = i_before + mine_before * U > p.vocab ? mine_before - 1 : mine_before;
           if (!ex.far) {
             const uint64_t ff = pair_of(f, f);
-            auto unit = [&](int u, uint32_t (&out)[4]) {
-              const uint4 v = *reinterpret_cast<const uint4*>(stage_before + u * 16);
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            auto unit = [&](const uint32_t (&w)[4], uint32_t (&out)[4]) {
 #pragma unroll
               for (int j = 0; j < U; j += 2) {
                 const float2 d = pair_as(pair_mul(ex(value_of<DT>(w, j), value_of<DT>(w, j + 1)), ff));
@@ -643,15 +665,17 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
                 }
               }
             };
-            uint32_t out[4];
-#pragma unroll 2
-            for (int u = from + tid; u < to; u += THREADS) {
-              unit(u, out);
+            for_units<THREADS>(from + tid, to, stage_before, [&](int u, const uint32_t (&w)[4]) {
+              uint32_t out[4];
+              unit(w, out);
               *reinterpret_cast<uint4*>(dz_before + u * 16) = make_uint4(out[0], out[1], out[2], out[3]);
-            }
+            });
             const int u = tid == 0 && from > 0 ? 0 : to;
             if ((tid == 0 && from > 0 && mine_before > 0) || (tid == (from > 0 ? 32 : 0) && to >= from && to < mine_before)) {
-              unit(u, out);
+              const uint4 v = *reinterpret_cast<const uint4*>(stage_before + u * 16);
+              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+              uint32_t out[4];
+              unit(w, out);
               write_unit<DT>(dz_before + u * 16, i_before + u * U, p.vocab, out);
             }
           } else {
