@@ -134,7 +134,11 @@ int abs_rms_norm(const abs_rms_norm_args* a, abs_stream_t stream) {
 
 size_t abs_rms_norm_grad_bytes(int64_t n0, int64_t n1, int64_t h, int64_t n_samples) {
   if (check_shape(n0, n1, h) != ABS_OK || n_samples < 0 || n_samples > ABS_MAX_SAMPLES) return 0;
-  const int64_t blocks = grad_blocks(n0 * n1, h);
+  int64_t blocks = 0;  // the most that a call of this shape takes: its tensors' alignment decides
+  for (int vec : {8, 4, 1}) {
+    const int64_t n = grad_blocks(n0 * n1, h, vec);
+    if (n > blocks) blocks = n;
+  }
   // one record a block, and with a table one for each sample and one more for each block
   return static_cast<size_t>(blocks + (n_samples ? blocks + n_samples : 0) + 1) * record_pitch(h) * sizeof(float);
 }
@@ -202,9 +206,12 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
   p.offsets = a->offsets;
   p.n_samples = static_cast<int>(a->n_samples);
   p.pitch = record_pitch(a->h);
-  const int64_t blocks = grad_blocks(p.rows, a->h);
+  int64_t blocks = 0;
   float* const work = static_cast<float*>(a->work);
   if (!empty) {
+    const Rows* const all[] = {&dy, &s, &add, &dx};
+    const int vec = vector_width(a->h, a->weight, a->weight_dtype, all, 4);
+    blocks = grad_blocks(p.rows, a->h, vec);
     p.dy = dy.arg();
     p.s = s.arg();
     p.add = add.arg();
@@ -216,8 +223,6 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
     if (a->dweight_samples) p.pieces = work + blocks * p.pitch;
     p.inv_h = static_cast<float>(1.0 / static_cast<double>(a->h));
     p.eps = static_cast<float>(a->eps);
-    const Rows* const all[] = {&dy, &s, &add, &dx};
-    const int vec = vector_width(a->h, a->weight, a->weight_dtype, all, 4);
     cudaError_t e;
     if (dy.dtype == ABS_F32) e = launch_norm_grad<ABS_F32>(p, s.dtype, blocks, vec, st);
     else if (dy.dtype == ABS_BF16) e = launch_norm_grad<ABS_BF16>(p, s.dtype, blocks, vec, st);

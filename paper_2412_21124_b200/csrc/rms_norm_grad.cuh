@@ -56,20 +56,29 @@ __host__ __device__ constexpr int grad_pieces() {
   return VEC == 8 ? 2 : 4;
 }
 
-template <int GT, int ST, int VEC, int L, int NI, bool BLOCK, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) rms_norm_grad_kernel(const NormGradParams p) {
+// BLOCK: a row by blockDim.x / 32 warps, blockDim.y rows at once, the weight as floats in dynamic shared memory (its 16
+// registers are the difference between three blocks on an SM and spills).  Otherwise a row by L lanes, NR rows
+// of a group of lanes at once, the weight in registers.
+// Blocks of 256 threads on an SM.  Three of 80 registers; two of up to 128 where a thread has four rows under way, or
+// single values (a register each) instead of vectors.
+__host__ __device__ constexpr int grad_blocks_per_sm(bool block, int vec) { return block && vec > 1 ? 3 : 2; }
+
+template <int GT, int ST, int VEC, int L, int NI, int NR, bool BLOCK, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(BLOCK, VEC) : 1) rms_norm_grad_kernel(const NormGradParams p) {
   constexpr int E = lane_values<VEC>();
   constexpr int kGroups = 32 / L;
   constexpr bool JOIN = THREADS == 256;  // several groups of threads hold rows: their sums are added
   __shared__ float part[2][BLOCK ? 64 : 1];
   __shared__ float part_again[2][BLOCK ? 64 : 1];
   __shared__ float joined[JOIN ? 8 * 32 * NI * E : 1];
+  extern __shared__ __align__(16) float weight_smem[];
 
   const int lane = threadIdx.x & 31, l = lane % L;
   const int warps = BLOCK ? static_cast<int>(blockDim.x) >> 5 : 1;
   const int warp = BLOCK ? static_cast<int>(threadIdx.x) >> 5 : 0;
   const int mine = BLOCK ? static_cast<int>(threadIdx.y) * warps : 0;
-  const int together = static_cast<int>(blockDim.y) * (BLOCK ? 1 : kGroups);  // rows at once
+  const int apart = static_cast<int>(blockDim.y) * (BLOCK ? 1 : kGroups);  // rows between two of a thread's
+  const int together = apart * NR;                                         // rows at once
   const int place = BLOCK ? static_cast<int>(threadIdx.y) : static_cast<int>(threadIdx.y) * kGroups + lane / L;
   const int cols = warps * (NI * L * E);
   grid_dependency_wait();
@@ -90,13 +99,36 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) rms_norm_grad
     b = low;
   }
 
-  float w[NI][E], acc[NI][E];
+  float w[BLOCK ? 1 : NI][E], acc[NI][E];
+  // four values of a thread side by side, so that a warp reads 512 bytes in a row
+  auto weight_at = [&](int i, int q) { return weight_smem + ((i * (E / 4) + q) * static_cast<int>(blockDim.x) + static_cast<int>(threadIdx.x)) * 4; };
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    load_weight<VEC>(w[i], p.w, p.w_dtype, (i * warps + warp) * (L * E), l, p.h);
+    float* const wi = w[BLOCK ? 0 : i];
+    load_weight<VEC>(wi, p.w, p.w_dtype, (i * warps + warp) * (L * E), l, p.h);
+    if (BLOCK && threadIdx.y == 0)
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q)
+        *reinterpret_cast<float4*>(weight_at(i, q)) = make_float4(wi[4 * q], wi[4 * q + 1], wi[4 * q + 2], wi[4 * q + 3]);
 #pragma unroll
     for (int j = 0; j < E; ++j) acc[i][j] = 0.f;
   }
+  if (BLOCK) __syncthreads();
+  auto take_weight = [&](int i, float (&to)[E]) {
+    if constexpr (BLOCK) {
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q) {
+        const float4 x = *reinterpret_cast<const float4*>(weight_at(i, q));
+        to[4 * q] = x.x;
+        to[4 * q + 1] = x.y;
+        to[4 * q + 2] = x.z;
+        to[4 * q + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) to[j] = w[i][j];
+    }
+  };
 
   int parity = 0;
   bool first_of_run = true;
@@ -110,98 +142,129 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) rms_norm_grad
       }
     }
     for (int64_t at = row0; at < stop; at += together) {
-      const uint32_t row = static_cast<uint32_t>(at) + place;
-      const bool live = row < stop;
-      const int h = live ? p.h : 0;
-      const uint32_t ri = p.n1 == 1 ? row : row / p.n1;
-      const uint32_t rj = p.n1 == 1 ? 0 : row - ri * p.n1;
-      Piece<ST, VEC> s[NI], add[NI];
-      Piece<GT, VEC> dy[NI];
-      const unsigned char *ps = row_of(p.s, ri, rj), *pg = row_of(p.dy, ri, rj);
+      uint32_t ri[NR], rj[NR];
+      bool live[NR];
+      Piece<ST, VEC> s[NR][NI], add[NR][NI];
+      Piece<GT, VEC> dy[NR][NI];
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        s[i].load(ps, (i * warps + warp) * (L * E), l, h);
-        dy[i].load(pg, (i * warps + warp) * (L * E), l, h);
-      }
-      if (p.add.p) {
-        const unsigned char* pa = row_of(p.add, ri, rj);
+      for (int k = 0; k < NR; ++k) {
+        const uint32_t row = static_cast<uint32_t>(at) + place + k * apart;
+        live[k] = row < stop;
+        ri[k] = p.n1 == 1 ? row : row / p.n1;
+        rj[k] = p.n1 == 1 ? 0 : row - ri[k] * p.n1;
+        const int h = live[k] ? p.h : 0;
+        const unsigned char *ps = row_of(p.s, ri[k], rj[k]), *pg = row_of(p.dy, ri[k], rj[k]);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) add[i].load(pa, (i * warps + warp) * (L * E), l, h);
-      } else {
+        for (int i = 0; i < NI; ++i) {
+          s[k][i].load(ps, (i * warps + warp) * (L * E), l, h);
+          dy[k][i].load(pg, (i * warps + warp) * (L * E), l, h);
+        }
+        if (p.add.p) {
+          const unsigned char* pa = row_of(p.add, ri[k], rj[k]);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) add[i].zero();
+          for (int i = 0; i < NI; ++i) add[k][i].load(pa, (i * warps + warp) * (L * E), l, h);
+        } else {
+#pragma unroll
+          for (int i = 0; i < NI; ++i) add[k][i].zero();
+        }
       }
 
-      float ss = 0.f, sg = 0.f;
+      float ss[NR], sg[NR];
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
+      for (int k = 0; k < NR; ++k) {
+        ss[k] = sg[k] = 0.f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          const float x = s[i].get(j);
-          ss = fmaf(x, x, ss);
-          sg = fmaf(dy[i].get(j) * w[i][j], x, sg);
+        for (int i = 0; i < NI; ++i) {
+          float wi[E];
+          take_weight(i, wi);
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            const float x = s[k][i].get(j);
+            ss[k] = fmaf(x, x, ss[k]);
+            sg[k] = fmaf(dy[k][i].get(j) * wi[j], x, sg[k]);
+          }
         }
-      ss = lanes_sum<L>(ss);
-      sg = lanes_sum<L>(sg);
+        ss[k] = lanes_sum<L>(ss[k]);
+        sg[k] = lanes_sum<L>(sg[k]);
+      }
       bool again;
       if constexpr (BLOCK) {
+        static_assert(NR == 1, "one row of a block's group at a time");
         if (lane == 0) {
-          part[parity][mine + warp] = ss;
-          part[parity][32 + mine + warp] = sg;
+          part[parity][mine + warp] = ss[0];
+          part[parity][32 + mine + warp] = sg[0];
         }
         __syncthreads();
         const int all = warps * static_cast<int>(blockDim.y);
         again = __any_sync(0xffffffffu, lane < all && !(part[parity][lane < all ? lane : 0] <= kSquaresLimit));
-        ss = lanes_sum<32>(lane < warps ? part[parity][mine + lane] : 0.f);
-        sg = lanes_sum<32>(lane < warps ? part[parity][32 + mine + lane] : 0.f);
+        ss[0] = lanes_sum<32>(lane < warps ? part[parity][mine + lane] : 0.f);
+        sg[0] = lanes_sum<32>(lane < warps ? part[parity][32 + mine + lane] : 0.f);
       } else {
-        again = __any_sync(0xffffffffu, !(ss <= kSquaresLimit));
+        bool over = false;
+#pragma unroll
+        for (int k = 0; k < NR; ++k) over |= !(ss[k] <= kSquaresLimit);
+        again = __any_sync(0xffffffffu, over);
       }
-      float rstd = rsqrtf(fmaf(ss, p.inv_h, p.eps)), scale = 1.f;
+      float rstd[NR], scale[NR];
+#pragma unroll
+      for (int k = 0; k < NR; ++k) {
+        rstd[k] = rsqrtf(fmaf(ss[k], p.inv_h, p.eps));
+        scale[k] = 1.f;
+      }
       if (again) {  // see kSquaresLimit
-        if (!(ss <= kSquaresLimit)) scale = kDown;
-        float ts = 0.f, tg = 0.f;
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
+        for (int k = 0; k < NR; ++k) {
+          if (!(ss[k] <= kSquaresLimit)) scale[k] = kDown;
+          float ts = 0.f, tg = 0.f;
 #pragma unroll
-          for (int j = 0; j < E; ++j) {
-            const float x = s[i].get(j) * scale;
-            ts = fmaf(x, x, ts);
-            tg = fmaf(dy[i].get(j) * w[i][j], x, tg);
+          for (int i = 0; i < NI; ++i) {
+            float wi[E];
+            take_weight(i, wi);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+              const float x = s[k][i].get(j) * scale[k];
+              ts = fmaf(x, x, ts);
+              tg = fmaf(dy[k][i].get(j) * wi[j], x, tg);
+            }
           }
-        ts = lanes_sum<L>(ts);
-        tg = lanes_sum<L>(tg);
-        if constexpr (BLOCK) {
-          if (lane == 0) {
-            part_again[parity][mine + warp] = ts;
-            part_again[parity][32 + mine + warp] = tg;
+          ts = lanes_sum<L>(ts);
+          tg = lanes_sum<L>(tg);
+          if constexpr (BLOCK) {
+            if (lane == 0) {
+              part_again[parity][mine + warp] = ts;
+              part_again[parity][32 + mine + warp] = tg;
+            }
+            __syncthreads();
+            ts = lanes_sum<32>(lane < warps ? part_again[parity][mine + lane] : 0.f);
+            tg = lanes_sum<32>(lane < warps ? part_again[parity][32 + mine + lane] : 0.f);
           }
-          __syncthreads();
-          ts = lanes_sum<32>(lane < warps ? part_again[parity][mine + lane] : 0.f);
-          tg = lanes_sum<32>(lane < warps ? part_again[parity][32 + mine + lane] : 0.f);
-        }
-        if (scale != 1.f) {
-          rstd = rsqrtf(ts * p.inv_h);
-          sg = tg;
+          if (scale[k] != 1.f) {
+            rstd[k] = rsqrtf(ts * p.inv_h);
+            sg[k] = tg;
+          }
         }
       }
       parity ^= 1;
 
-      const float unit = scale * rstd;            // u = s scale rstd: one product where nothing was scaled
-      const float a = sg * rstd * p.inv_h;
-      if (live) {
-        unsigned char* px = row_of(p.dx, ri, rj);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          float v[E];
+      for (int k = 0; k < NR; ++k) {
+        const float unit = scale[k] * rstd[k];  // u = s scale rstd; scaled first, so that neither vanishes
+        const float a = sg[k] * rstd[k] * p.inv_h;
+        if (live[k]) {
+          unsigned char* px = row_of(p.dx, ri[k], rj[k]);
 #pragma unroll
-          for (int j = 0; j < E; ++j) {
-            const float g = dy[i].get(j);
-            const float u = scale == 1.f ? s[i].get(j) * rstd : s[i].get(j) * scale * rstd;
-            acc[i][j] = fmaf(g, u, acc[i][j]);
-            v[j] = fmaf(unit, fmaf(-u, a, g * w[i][j]), add[i].get(j));
+          for (int i = 0; i < NI; ++i) {
+            float v[E], wi[E];
+            take_weight(i, wi);
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+              const float g = dy[k][i].get(j);
+              const float u = s[k][i].get(j) * scale[k] * rstd[k];
+              acc[i][j] = fmaf(g, u, acc[i][j]);
+              v[j] = fmaf(unit, fmaf(-u, a, g * wi[j]), add[k][i].get(j));
+            }
+            store_piece_as<VEC>(p.dx_dtype, px, (i * warps + warp) * (L * E), l, p.h, v);
           }
-          store_piece_as<VEC>(p.dx_dtype, px, (i * warps + warp) * (L * E), l, p.h, v);
         }
       }
     }
@@ -269,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 3 : 1) rms_norm_grad
 
 // Adds the records: blocks of 32 columns x kMergeSlices.  Block row b < n_out: the pieces of sample b, behind
 // them the totals.
-constexpr int kMergeSlices = 16;
+constexpr int kMergeSlices = 32;
 struct NormMergeParams {
   const float *totals, *pieces;
   int64_t pitch;
@@ -303,7 +366,7 @@ __global__ void __launch_bounds__(32 * kMergeSlices) rms_norm_merge_kernel(const
   }
   float x = 0.f;
   if (col < p.h)
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t k = lo + threadIdx.y; k < hi; k += kMergeSlices) x += from[k * p.pitch + col];
   sums[threadIdx.y][threadIdx.x] = x;
   __syncthreads();

@@ -56,49 +56,62 @@ cudaError_t launch_norm(const NormParams& p, int r_dtype, int vec, cudaStream_t 
 }
 
 // ---- backward
-// Blocks of the kernel that sums over rows: three of 256 threads on an SM (four where a row takes few
-// registers), or one of more.
-inline int64_t grad_blocks(int64_t rows, int64_t h) {
-  const int64_t most = kSMs * (h <= 512 ? 4 : h <= 4096 ? 3 : 1);
+// A row of at most this many values goes to the lanes of a warp, four rows at once.
+constexpr int grad_lane_values(int vec) { return vec == 8 ? 256 : 128; }
+// Blocks of the kernel that sums over rows: as many as fit the SMs at once.
+inline int64_t grad_blocks(int64_t rows, int64_t h, int vec) {
+  const int64_t most = kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec) : 1);
   return rows < most ? rows : most;
 }
 inline int64_t record_pitch(int64_t h) { return (h + 7) / 8 * 8; }  // VEC 8 writes 32 bytes at once
 
-template <int GT, int ST, int VEC, int L, int NI>
+template <int GT, int ST, int VEC, int L, int NI, int NR>
 cudaError_t grad_by_lanes(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
-  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, L, NI, false, 256>, dim3(static_cast<unsigned>(blocks)),
+  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, L, NI, NR, false, 256>, dim3(static_cast<unsigned>(blocks)),
                     dim3(32, 8), st, p);
+}
+template <int GT, int ST, int VEC, int THREADS>
+cudaError_t grad_by_block_of(const NormGradParams& p, int64_t blocks, int warps, cudaStream_t st) {
+  constexpr int NI = grad_pieces<VEC>();
+  const auto kernel = rms_norm_grad_kernel<GT, ST, VEC, 32, NI, 1, true, THREADS>;
+  const int values = warps * 32 * lane_values<VEC>() * NI;  // of the weight, with what lies behind the row's end
+  const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), THREADS * NI * lane_values<VEC>() * sizeof(float));
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(32 * warps, THREADS == 256 ? 8 / warps : 1);
+  cfg.dynamicSmemBytes = values * sizeof(float);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 template <int GT, int ST, int VEC>
 cudaError_t grad_by_block(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
-  constexpr int NI = grad_pieces<VEC>();
-  constexpr int cols = 32 * lane_values<VEC>() * NI;
+  constexpr int cols = 32 * lane_values<VEC>() * grad_pieces<VEC>();
   static_assert(cols == 512, "grad_blocks counts on it");
   const int warps = (p.h + cols - 1) / cols;
-  const dim3 grid(static_cast<unsigned>(blocks));
-  if (warps <= 8)
-    return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 256>, grid, dim3(32 * warps, 8 / warps), st, p);
-  if (warps <= 16)
-    return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 512>, grid, dim3(32 * warps, 1), st, p);
-  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, 32, NI, true, 1024>, grid, dim3(32 * warps, 1), st, p);
+  if (warps <= 8) return grad_by_block_of<GT, ST, VEC, 256>(p, blocks, warps, st);
+  if (warps <= 16) return grad_by_block_of<GT, ST, VEC, 512>(p, blocks, warps, st);
+  return grad_by_block_of<GT, ST, VEC, 1024>(p, blocks, warps, st);
 }
 template <int GT, int ST>
 cudaError_t grad_vec(const NormGradParams& p, int64_t blocks, int vec, cudaStream_t st) {
   const int h = p.h;
   if (vec == 8) {
-    if (h <= 64) return grad_by_lanes<GT, ST, 8, 8, 1>(p, blocks, st);
-    if (h <= 128) return grad_by_lanes<GT, ST, 8, 16, 1>(p, blocks, st);
-    if (h <= 256) return grad_by_lanes<GT, ST, 8, 32, 1>(p, blocks, st);
-    if (h <= 512) return grad_by_lanes<GT, ST, 8, 32, 2>(p, blocks, st);
+    if (h <= 64) return grad_by_lanes<GT, ST, 8, 8, 1, 4>(p, blocks, st);
+    if (h <= 128) return grad_by_lanes<GT, ST, 8, 16, 1, 4>(p, blocks, st);
+    if (h <= grad_lane_values(8)) return grad_by_lanes<GT, ST, 8, 32, 1, 4>(p, blocks, st);
     return grad_by_block<GT, ST, 8>(p, blocks, st);
   }
   if (vec == 4) {
-    if (h <= 128) return grad_by_lanes<GT, ST, 4, 32, 1>(p, blocks, st);
-    if (h <= 512) return grad_by_lanes<GT, ST, 4, 32, 4>(p, blocks, st);
+    if (h <= grad_lane_values(4)) return grad_by_lanes<GT, ST, 4, 32, 1, 4>(p, blocks, st);
     return grad_by_block<GT, ST, 4>(p, blocks, st);
   }
-  if (h <= 128) return grad_by_lanes<GT, ST, 1, 32, 1>(p, blocks, st);
-  if (h <= 512) return grad_by_lanes<GT, ST, 1, 32, 4>(p, blocks, st);
+  if (h <= grad_lane_values(1)) return grad_by_lanes<GT, ST, 1, 32, 1, 4>(p, blocks, st);
   return grad_by_block<GT, ST, 1>(p, blocks, st);
 }
 template <int GT>
