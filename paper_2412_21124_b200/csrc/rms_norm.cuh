@@ -16,8 +16,9 @@ struct NormParams {
   unsigned char* scales;           // NULL unless the output has 8 bits
   int64_t scale_s0, scale_s1, scale_s2;  // in elements
   const unsigned char* w;          // may be NULL
-  uint32_t rows, n1;
-  int h, group;                    // columns of a scale; the row's width: one scale a row
+  uint32_t rows;
+  Divisor n1;
+  int h, group, group_shift;       // columns of a scale, their log2; the row's width: one scale a row
   int w_dtype, sum_dtype, out_dtype, scale_dtype;
   float inv_h, eps;
 };
@@ -27,32 +28,46 @@ struct NormParams {
 constexpr float kSquaresLimit = 1e36f;
 constexpr float kDown = 0x1p-80f;
 
-// The scale of a group whose largest |y| has the bits `a`, and its reciprocal.  Not finite: NaN, which
-// makes all values of the group NaN.
-__device__ __forceinline__ void scale_of(uint32_t a, int out_dtype, int scale_dtype, float& scale, float& inv) {
-  if (a >= 0x7f800000u) {
-    scale = inv = __uint_as_float(0x7fffffffu);
-  } else if (a == 0u) {
-    scale = inv = 1.f;
-  } else if (scale_dtype == ABS_F32) {
-    scale = fmaxf(__uint_as_float(a) / (out_dtype == ABS_E4M3 ? 448.f : 57344.f), 0x1p-126f);
-    inv = 1.f / scale;
-  } else {
-    // the smallest 2^e with a <= M 2^e, where M = 1.75 * 2^8 (e4m3) or 1.75 * 2^15 (e5m2); at least 2^-127
-    int e = static_cast<int>(a >> 23) - 127 - (out_dtype == ABS_E4M3 ? 8 : 15) + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
-    e = max(e, -127);
-    scale = __uint_as_float(static_cast<uint32_t>(e + 127));  // the byte; see store_scale
-    inv = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-  }
-}
-__device__ __forceinline__ void store_scale(unsigned char* scales, int64_t at, int scale_dtype, uint32_t a, float scale) {
+// The scale of a group whose largest |y| has the bits `a`, as it is stored (a float's bits, or the byte), and its
+// reciprocal.  Not finite: NaN, which makes all values of the group NaN.
+__device__ __forceinline__ uint32_t scale_of(uint32_t a, int out_dtype, int scale_dtype, float& inv) {
+  const bool wild = a >= 0x7f800000u, zero = a == 0u;
+  uint32_t stored;
   if (scale_dtype == ABS_F32) {
-    reinterpret_cast<float*>(scales)[at] = scale;
+    const float scale = fmaxf(__uint_as_float(a) / (out_dtype == ABS_E4M3 ? 448.f : 57344.f), 0x1p-126f);
+    inv = zero ? 1.f : 1.f / scale;
+    stored = zero ? 0x3f800000u : __float_as_uint(scale);
+    if (wild) stored = 0x7fffffffu;
   } else {
-    scales[at] = a >= 0x7f800000u ? 255 : a == 0u ? 127 : static_cast<unsigned char>(__float_as_uint(scale));
+    // the smallest 2^e with a <= M 2^e, where M = 1.75 * 2^8 (e4m3) or 1.75 * 2^15 (e5m2); at least 2^-127: a's exponent,
+    // one more if its fraction is above .75, less 8 or 15
+    const int byte = max(static_cast<int>((a + 0x1fffffu) >> 23) - (out_dtype == ABS_E4M3 ? 8 : 15), 0);
+    stored = wild ? 255u : zero ? 127u : static_cast<uint32_t>(byte);
+    inv = __uint_as_float((254u - stored) << 23);
   }
+  if (wild) inv = __uint_as_float(0x7fffffffu);
+  return stored;
+}
+__device__ __forceinline__ void store_scale(unsigned char* scales, int64_t at, int scale_dtype, uint32_t stored) {
+  if (scale_dtype == ABS_F32) reinterpret_cast<uint32_t*>(scales)[at] = stored;
+  else scales[at] = static_cast<unsigned char>(stored);
 }
 
+// max(a, |b|), NaN if one is: a's sign is clear
+__device__ __forceinline__ float larger(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+  return r;
+}
+template <int NI, int E>
+__device__ __forceinline__ float squares(const float (&s)[NI][E]) {
+  float t[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < NI; ++i)
+#pragma unroll
+    for (int j = 0; j < E; ++j) t[j & 1] = fmaf(s[i][j], s[i][j], t[j & 1]);
+  return t[0] + t[1];
+}
 // L lanes (a whole warp if BLOCK: blockDim.x / 32 of them) hold one row in NI pieces; without BLOCK a group
 // of lanes takes NR rows at once.  blockDim.y rows (warps) a block.
 template <int XT, int RT, int VEC, int L, int NI, int NR, bool BLOCK>
@@ -75,8 +90,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
   for (int k = 0; k < NR; ++k) {
     row[k] = slot + k * kGroups;
-    ri[k] = p.n1 == 1 ? row[k] : row[k] / p.n1;
-    rj[k] = p.n1 == 1 ? 0 : row[k] - ri[k] * p.n1;
+    split_row(row[k], p.n1, ri[k], rj[k]);
   }
   grid_dependency_wait();
 
@@ -87,8 +101,8 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
       const int h = row[k] < p.rows ? p.h : 0;  // nothing is loaded for rows behind the last
-      const unsigned char* px = row_of(p.x, ri[k], rj[k]);
-      const unsigned char* pr = HAS_R ? row_of(p.r, ri[k], rj[k]) : nullptr;
+      const unsigned char* px = row_of<VEC>(p.x, ri[k], rj[k]);
+      const unsigned char* pr = HAS_R ? row_of<VEC>(p.r, ri[k], rj[k]) : nullptr;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         x[k][i].load(px, (i * warps + warp) * (L * E), l, h);
@@ -109,12 +123,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
   float ss[NR];
 #pragma unroll
   for (int k = 0; k < NR; ++k) {
-    ss[k] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int j = 0; j < E; ++j) ss[k] = fmaf(s[k][i][j], s[k][i][j], ss[k]);
-    ss[k] = lanes_sum<L>(ss[k]);
+    ss[k] = lanes_sum<L>(squares(s[k]));
   }
 
   // the rounded sum goes out while the row's warps wait for one another
@@ -123,10 +132,9 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
       for (int k = 0; k < NR; ++k)
         if (row[k] < p.rows) {
-          unsigned char* ps = row_of(p.sum, ri[k], rj[k]);
+          unsigned char* ps = row_of<VEC>(p.sum, ri[k], rj[k]);
 #pragma unroll
-          for (int i = 0; i < NI; ++i)
-            store_piece<RT, VEC>(ps, (i * warps + warp) * (L * E), l, p.h, s[k][i]);
+          for (int i = 0; i < NI; ++i) store_piece<RT, VEC>(ps, (i * warps + warp) * (L * E), l, p.h, s[k][i]);
         }
     }
   }
@@ -151,15 +159,11 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
       const bool down = !(ss[k] <= kSquaresLimit);
-      float t = 0.f;
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-          if (down) s[k][i][j] *= kDown;
-          t = fmaf(s[k][i][j], s[k][i][j], t);
-        }
-      t = lanes_sum<L>(t);
+        for (int j = 0; j < E; ++j) s[k][i][j] *= down ? kDown : 1.f;
+      float t = lanes_sum<L>(squares(s[k]));
       if constexpr (BLOCK) {
         if (lane == 0) part_again[mine + warp] = t;
         __syncthreads();
@@ -169,91 +173,127 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     }
   }
 
+  if (!p.scales) {
+    // y, piece by piece; the branches on the types are taken once for all of a thread's pieces
+    with_type(p.w_dtype, [&](auto wt) {
 #pragma unroll
-  for (int i = 0; i < NI; ++i) {
-    const int first = (i * warps + warp) * (L * E);
-    float w[E];
-    load_weight<VEC>(w, p.w, p.w_dtype, first, l, p.h);
+      for (int i = 0; i < NI; ++i) {
+        const int first = (i * warps + warp) * (L * E);
+        float w[E];
+        load_weight_of<decltype(wt)::value, VEC>(w, p.w, first, l, p.h);
 #pragma unroll
-    for (int k = 0; k < NR; ++k)
+        for (int k = 0; k < NR; ++k)
 #pragma unroll
-      for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * w[j];
+          for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * w[j];
+      }
+    });
+    with_type(p.out_dtype, [&](auto ot) {
+#pragma unroll
+      for (int k = 0; k < NR; ++k)
+        if (row[k] < p.rows) {
+          unsigned char* const po = row_of<VEC>(p.out, ri[k], rj[k]);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) store_piece<decltype(ot)::value, VEC>(po, (i * warps + warp) * (L * E), l, p.h, s[k][i]);
+        }
+    });
+    return;
   }
 
-  if (p.scales) {
-    if (p.group >= p.h) {  // one scale a row
+  // 8 bits: the largest |s w| of a group times rstd is its largest |y|.  (rstd and the scale's reciprocal are not made one
+  // factor: it may overflow where their products with s w do not.)
+  uint32_t a_row[NR];
 #pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        uint32_t a = 0u;
+  for (int k = 0; k < NR; ++k) a_row[k] = 0u;
+  with_type(p.w_dtype, [&](auto wt) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j < E; ++j) a = max(a, __float_as_uint(s[k][i][j]) & 0x7fffffffu);
-        a = lanes_max(a, L);
-        if constexpr (BLOCK) {
-          if (lane == 0) part_max[mine + warp] = a;
-          __syncthreads();
-          a = lanes_max(lane < warps ? part_max[mine + lane] : 0u, 32);
-        }
-        float scale, inv;
-        scale_of(a, p.out_dtype, p.scale_dtype, scale, inv);
-        if (l == 0 && warp == 0 && row[k] < p.rows)
-          store_scale(p.scales, ri[k] * p.scale_s0 + rj[k] * p.scale_s1, p.scale_dtype, a, scale);
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j < E; ++j) s[k][i][j] *= inv;
-      }
-    } else {
+    for (int i = 0; i < NI; ++i) {
+      float w[E];
+      load_weight_of<decltype(wt)::value, VEC>(w, p.w, (i * warps + warp) * (L * E), l, p.h);
 #pragma unroll
       for (int k = 0; k < NR; ++k)
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const int first = (i * warps + warp) * (L * E);
-          const int64_t at = ri[k] * p.scale_s0 + rj[k] * p.scale_s1;
-          if constexpr (VEC == 1) {  // a group is 1, 2 or 4 of the four values of every lane
-            uint32_t a[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) a[j] = lanes_max(__float_as_uint(s[k][i][j]) & 0x7fffffffu, 32);
-            if (p.group >= 64) {
-              a[0] = a[1] = max(a[0], a[1]);
-              a[2] = a[3] = max(a[2], a[3]);
-            }
-            if (p.group >= 128) a[0] = a[1] = a[2] = a[3] = max(a[0], a[2]);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-              float scale, inv;
-              scale_of(a[j], p.out_dtype, p.scale_dtype, scale, inv);
-              const int c = first + 32 * j;
-              if (l == 0 && c < p.h && c % p.group == 0 && row[k] < p.rows)
-                store_scale(p.scales, at + c / p.group * p.scale_s2, p.scale_dtype, a[j], scale);
-              s[k][i][j] *= inv;
-            }
-          } else {
-            uint32_t a = 0u;
-#pragma unroll
-            for (int j = 0; j < E; ++j) a = max(a, __float_as_uint(s[k][i][j]) & 0x7fffffffu);
-            a = lanes_max(a, min(p.group / VEC, L));
-            float scale, inv;
-            scale_of(a, p.out_dtype, p.scale_dtype, scale, inv);
-            const int c = first + l * VEC;
-            if (c < p.h && c % p.group == 0 && row[k] < p.rows)
-              store_scale(p.scales, at + c / p.group * p.scale_s2, p.scale_dtype, a, scale);
-#pragma unroll
-            for (int j = 0; j < E; ++j) s[k][i][j] *= inv;
-          }
-        }
+        for (int j = 0; j < E; ++j) s[k][i][j] *= w[j];
     }
-  }
-
+  });
+  const bool of_row = p.group >= p.h;
+  if (of_row) {
 #pragma unroll
-  for (int k = 0; k < NR; ++k)
-    if (row[k] < p.rows) {
-      unsigned char* po = row_of(p.out, ri[k], rj[k]);
+    for (int k = 0; k < NR; ++k) {
+      float a = 0.f;
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        store_piece_as<VEC>(p.out_dtype, po, (i * warps + warp) * (L * E), l, p.h, s[k][i]);
+#pragma unroll
+        for (int j = 0; j < E; ++j) a = larger(a, s[k][i][j]);
+      a_row[k] = lanes_max(__float_as_uint(a), L);
+      if constexpr (BLOCK) {
+        if (lane == 0) part_max[mine + warp] = a_row[k];
+        __syncthreads();
+        a_row[k] = lanes_max(lane < warps ? part_max[mine + lane] : 0u, 32);
+      }
     }
+  }
+#pragma unroll
+  for (int k = 0; k < NR; ++k) {
+    const bool live = row[k] < p.rows;
+    unsigned char* const po = row_of<VEC>(p.out, ri[k], rj[k]);
+    auto scale_from = [&](uint32_t a, bool writer, int group) {
+      float inv;
+      const uint32_t stored = scale_of(__float_as_uint(__uint_as_float(a) * rstd[k]) & 0x7fffffffu, p.out_dtype, p.scale_dtype, inv);
+      if (writer && live)
+        store_scale(p.scales, ri[k] * p.scale_s0 + rj[k] * p.scale_s1 + group * p.scale_s2, p.scale_dtype, stored);
+      return inv;
+    };
+    if (of_row) {
+      const float inv = scale_from(a_row[k], l == 0 && warp == 0, 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int first = (i * warps + warp) * (L * E);
+        if constexpr (VEC == 1) {  // a group is 1, 2 or 4 of the four values of every lane
+          uint32_t a[E];
+#pragma unroll
+          for (int j = 0; j < E; ++j) a[j] = __reduce_max_sync(0xffffffffu, __float_as_uint(s[k][i][j]) & 0x7fffffffu);
+          if (p.group >= 64) {
+            a[0] = a[1] = max(a[0], a[1]);
+            a[2] = a[3] = max(a[2], a[3]);
+          }
+          if (p.group >= 128) a[0] = a[1] = a[2] = a[3] = max(a[0], a[2]);
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            const int c = first + 32 * j;
+            const float inv = scale_from(a[j], l == 0 && c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
+            s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+          }
+        } else {
+          float top = 0.f;
+#pragma unroll
+          for (int j = 0; j < E; ++j) top = larger(top, s[k][i][j]);
+          // the lanes of a group: 32 / VEC, twice or four times as many
+          uint32_t a = __float_as_uint(top);
+#pragma unroll
+          for (int d = 1; d < 32 / VEC; d <<= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, d));
+          if (p.group >= 64) a = max(a, __shfl_xor_sync(0xffffffffu, a, 32 / VEC));
+          if (p.group >= 128) a = max(a, __shfl_xor_sync(0xffffffffu, a, 64 / VEC));
+          const int c = first + l * VEC;
+          const float inv = scale_from(a, c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
+#pragma unroll
+          for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+        }
+      }
+    }
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int first = (i * warps + warp) * (L * E);
+        if (p.out_dtype == ABS_E4M3) store_piece<ABS_E4M3, VEC>(po, first, l, p.h, s[k][i]);
+        else store_piece<ABS_E5M2, VEC>(po, first, l, p.h, s[k][i]);
+      }
+    }
+  }
 }
 
 }  // namespace absnt

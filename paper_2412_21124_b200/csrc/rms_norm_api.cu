@@ -101,10 +101,12 @@ int abs_rms_norm(const abs_rms_norm_args* a, abs_stream_t stream) {
   }
 
   NormParams p = {};
-  p.x = x.arg();
-  p.r = r.arg();
-  p.sum = sum.arg();
-  p.out = out.arg();
+  const Rows* const all[] = {&x, &r, &sum, &out};
+  const int vec = vector_width(a->h, a->weight, a->weight_dtype, all, 4);
+  p.x = x.arg(vec);
+  p.r = r.arg(vec);
+  p.sum = sum.arg(vec);
+  p.out = out.arg(vec);
   if (eight) {
     p.scales = const_cast<unsigned char*>(scales.p);
     p.scale_s0 = scales.s0 / scales.esz;
@@ -113,7 +115,8 @@ int abs_rms_norm(const abs_rms_norm_args* a, abs_stream_t stream) {
   }
   p.w = static_cast<const unsigned char*>(a->weight);
   p.rows = static_cast<uint32_t>(a->n0 * a->n1);
-  p.n1 = static_cast<uint32_t>(a->n1);
+  p.n1 = divisor(static_cast<uint32_t>(a->n1));
+  for (int g = static_cast<int>(group); g > 1; g >>= 1) ++p.group_shift;
   p.h = static_cast<int>(a->h);
   p.group = static_cast<int>(group);
   p.w_dtype = a->weight_dtype;
@@ -121,8 +124,6 @@ int abs_rms_norm(const abs_rms_norm_args* a, abs_stream_t stream) {
   p.scale_dtype = scales.dtype;
   p.inv_h = static_cast<float>(1.0 / static_cast<double>(a->h));
   p.eps = static_cast<float>(a->eps);
-  const Rows* const all[] = {&x, &r, &sum, &out};
-  const int vec = vector_width(a->h, a->weight, a->weight_dtype, all, 4);
   const int r_dtype = r.given() ? r.dtype : -1;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
@@ -201,7 +202,7 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   NormGradParams p = {};
   p.rows = empty ? 0 : static_cast<uint32_t>(n0 * n1);
-  p.n1 = static_cast<uint32_t>(n1);
+  p.n1 = divisor(static_cast<uint32_t>(n1));
   p.h = static_cast<int>(a->h);
   p.offsets = a->offsets;
   p.n_samples = static_cast<int>(a->n_samples);
@@ -212,10 +213,10 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
     const Rows* const all[] = {&dy, &s, &add, &dx};
     const int vec = vector_width(a->h, a->weight, a->weight_dtype, all, 4);
     blocks = grad_blocks(p.rows, a->h, vec);
-    p.dy = dy.arg();
-    p.s = s.arg();
-    p.add = add.arg();
-    p.dx = dx.arg();
+    p.dy = dy.arg(vec);
+    p.s = s.arg(vec);
+    p.add = add.arg(vec);
+    p.dx = dx.arg(vec);
     p.w = static_cast<const unsigned char*>(a->weight);
     p.w_dtype = a->weight_dtype;
     p.dx_dtype = dx.dtype;
@@ -239,7 +240,7 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
   m.dw_samples = a->dweight_samples;
   m.ld = a->samples_ld;
   m.rows = p.rows;
-  m.n1 = p.n1;
+  m.n1 = p.n1.d;
   m.n_samples = p.n_samples;
   m.h = p.h;
   m.blocks = static_cast<int>(blocks);

@@ -23,7 +23,8 @@ struct NormGradParams {
   const int32_t* offsets;          // NULL: all rows, one sample
   float *totals, *pieces;          // may be NULL
   int64_t pitch;                   // floats between two records
-  uint32_t rows, n1;
+  uint32_t rows;
+  Divisor n1;
   int n_samples;
   int h, w_dtype, dx_dtype;
   float inv_h, eps;
@@ -61,9 +62,9 @@ __host__ __device__ constexpr int grad_pieces() {
 // of a group of lanes at once, the weight in registers.
 // Blocks of 256 threads on an SM.  Three of 80 registers; two of up to 128 where a thread has four rows under way, or
 // single values (a register each) instead of vectors.
-__host__ __device__ constexpr int grad_blocks_per_sm(bool block, int vec) { return block && vec > 1 ? 3 : 2; }
+__host__ __device__ constexpr int grad_blocks_per_sm(bool block, int vec) { return !block || vec > 1 ? 3 : 2; }
 
-template <int GT, int ST, int VEC, int L, int NI, int NR, bool BLOCK, int THREADS>
+template <int GT, int ST, bool ADD, int VEC, int L, int NI, int NR, bool BLOCK, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(BLOCK, VEC) : 1) rms_norm_grad_kernel(const NormGradParams p) {
   constexpr int E = lane_values<VEC>();
   constexpr int kGroups = 32 / L;
@@ -83,7 +84,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
   const int cols = warps * (NI * L * E);
   grid_dependency_wait();
 
-  const Span span = span_of(p.offsets, p.n_samples, p.n1, p.rows, gridDim.x);
+  const Span span = span_of(p.offsets, p.n_samples, p.n1.d, p.rows, gridDim.x);
   const int64_t c = blockIdx.x;
   if (c >= span.blocks) return;
   int64_t row0 = span.start(c);
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
     int low = 0, high = p.n_samples - 1;
     while (low < high) {
       const int mid = (low + high + 1) >> 1;
-      if (table_at(p.offsets, mid, p.n1, 0, p.rows) <= row0) low = mid;
+      if (table_at(p.offsets, mid, p.n1.d, 0, p.rows) <= row0) low = mid;
       else high = mid - 1;
     }
     b = low;
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     float* const wi = w[BLOCK ? 0 : i];
-    load_weight<VEC>(wi, p.w, p.w_dtype, (i * warps + warp) * (L * E), l, p.h);
+    with_type(p.w_dtype, [&](auto t) { load_weight_of<decltype(t)::value, VEC>(wi, p.w, (i * warps + warp) * (L * E), l, p.h); });
     if (BLOCK && threadIdx.y == 0)
 #pragma unroll
       for (int q = 0; q < E / 4; ++q)
@@ -135,57 +136,62 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
   while (row0 < end) {
     int64_t stop = end;
     if (p.offsets) {
-      while (b + 1 < p.n_samples && table_at(p.offsets, b + 1, p.n1, 0, p.rows) <= row0) ++b;
+      while (b + 1 < p.n_samples && table_at(p.offsets, b + 1, p.n1.d, 0, p.rows) <= row0) ++b;
       if (b + 1 < p.n_samples) {
-        const int64_t next = table_at(p.offsets, b + 1, p.n1, 0, p.rows);
+        const int64_t next = table_at(p.offsets, b + 1, p.n1.d, 0, p.rows);
         stop = next < end ? next : end;
       }
     }
     for (int64_t at = row0; at < stop; at += together) {
       uint32_t ri[NR], rj[NR];
       bool live[NR];
-      Piece<ST, VEC> s[NR][NI], add[NR][NI];
+      Piece<ST, VEC> s[NR][NI], add[ADD ? NR : 1][ADD ? NI : 1];
       Piece<GT, VEC> dy[NR][NI];
 #pragma unroll
       for (int k = 0; k < NR; ++k) {
         const uint32_t row = static_cast<uint32_t>(at) + place + k * apart;
         live[k] = row < stop;
-        ri[k] = p.n1 == 1 ? row : row / p.n1;
-        rj[k] = p.n1 == 1 ? 0 : row - ri[k] * p.n1;
+        split_row(row, p.n1, ri[k], rj[k]);
         const int h = live[k] ? p.h : 0;
-        const unsigned char *ps = row_of(p.s, ri[k], rj[k]), *pg = row_of(p.dy, ri[k], rj[k]);
+        const unsigned char *ps = row_of<VEC>(p.s, ri[k], rj[k]), *pg = row_of<VEC>(p.dy, ri[k], rj[k]);
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           s[k][i].load(ps, (i * warps + warp) * (L * E), l, h);
           dy[k][i].load(pg, (i * warps + warp) * (L * E), l, h);
         }
-        if (p.add.p) {
-          const unsigned char* pa = row_of(p.add, ri[k], rj[k]);
+        if constexpr (ADD) {
+          const unsigned char* pa = row_of<VEC>(p.add, ri[k], rj[k]);
 #pragma unroll
           for (int i = 0; i < NI; ++i) add[k][i].load(pa, (i * warps + warp) * (L * E), l, h);
-        } else {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) add[k][i].zero();
         }
       }
 
-      float ss[NR], sg[NR];
-#pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        ss[k] = sg[k] = 0.f;
+      // sum s^2 and sum g s over the row's lanes, of s times `by`
+      auto sums_of = [&](const Piece<ST, VEC> (&s)[NI], const Piece<GT, VEC> (&dy)[NI], float by, float& to_ss, float& to_sg) {
+        float a = 0.f, b = 0.f;
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
           float wi[E];
           take_weight(i, wi);
 #pragma unroll
           for (int j = 0; j < E; ++j) {
-            const float x = s[k][i].get(j);
-            ss[k] = fmaf(x, x, ss[k]);
-            sg[k] = fmaf(dy[k][i].get(j) * wi[j], x, sg[k]);
+            const float x = by == 1.f ? s[i].get(j) : s[i].get(j) * by;
+            a = fmaf(x, x, a);
+            b = fmaf(dy[i].get(j) * wi[j], x, b);
           }
         }
-        ss[k] = lanes_sum<L>(ss[k]);
-        sg[k] = lanes_sum<L>(sg[k]);
+        to_ss = lanes_sum<L>(a);
+        to_sg = lanes_sum<L>(b);
+      };
+      float ss[NR], sg[NR];
+#pragma unroll
+      for (int k = 0; k < NR; ++k) {
+        sums_of(s[k], dy[k], 1.f, ss[k], sg[k]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          s[k][i].keep_packed();
+          dy[k][i].keep_packed();
+        }
       }
       bool again;
       if constexpr (BLOCK) {
@@ -215,20 +221,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
 #pragma unroll
         for (int k = 0; k < NR; ++k) {
           if (!(ss[k] <= kSquaresLimit)) scale[k] = kDown;
-          float ts = 0.f, tg = 0.f;
-#pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            float wi[E];
-            take_weight(i, wi);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-              const float x = s[k][i].get(j) * scale[k];
-              ts = fmaf(x, x, ts);
-              tg = fmaf(dy[k][i].get(j) * wi[j], x, tg);
-            }
-          }
-          ts = lanes_sum<L>(ts);
-          tg = lanes_sum<L>(tg);
+          float ts, tg;
+          sums_of(s[k], dy[k], scale[k], ts, tg);
           if constexpr (BLOCK) {
             if (lane == 0) {
               part_again[parity][mine + warp] = ts;
@@ -248,23 +242,26 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
 
 #pragma unroll
       for (int k = 0; k < NR; ++k) {
-        const float unit = scale[k] * rstd[k];  // u = s scale rstd; scaled first, so that neither vanishes
+        const float unit = scale[k] * rstd[k];  // of the row as it is: down to 2^-128, where it still has 21 bits
         const float a = sg[k] * rstd[k] * p.inv_h;
         if (live[k]) {
-          unsigned char* px = row_of(p.dx, ri[k], rj[k]);
+          unsigned char* const px = row_of<VEC>(p.dx, ri[k], rj[k]);
+          with_type(p.dx_dtype, [&](auto xt) {
 #pragma unroll
-          for (int i = 0; i < NI; ++i) {
-            float v[E], wi[E];
-            take_weight(i, wi);
+            for (int i = 0; i < NI; ++i) {
+              float v[E], wi[E];
+              take_weight(i, wi);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-              const float g = dy[k][i].get(j);
-              const float u = s[k][i].get(j) * scale[k] * rstd[k];
-              acc[i][j] = fmaf(g, u, acc[i][j]);
-              v[j] = fmaf(unit, fmaf(-u, a, g * wi[j]), add[k][i].get(j));
+              for (int j = 0; j < E; ++j) {
+                const float g = dy[k][i].get(j), u = s[k][i].get(j) * unit;
+                acc[i][j] = fmaf(g, u, acc[i][j]);
+                const float x = fmaf(-u, a, g * wi[j]);
+                if constexpr (ADD) v[j] = fmaf(unit, x, add[k][i].get(j));
+                else v[j] = unit * x;
+              }
+              store_piece<decltype(xt)::value, VEC>(px, (i * warps + warp) * (L * E), l, p.h, v);
             }
-            store_piece_as<VEC>(p.dx_dtype, px, (i * warps + warp) * (L * E), l, p.h, v);
-          }
+          });
         }
       }
     }

@@ -21,30 +21,27 @@ cudaError_t norm_by_block(const NormParams& p, cudaStream_t st) {
   constexpr int cols = 32 * lane_values<VEC>() * NI;  // of a warp
   return launch_pdl(rms_norm_kernel<XT, RT, VEC, 32, NI, 1, true>, dim3(p.rows), dim3(32 * ((p.h + cols - 1) / cols), 1), st, p);
 }
+// As many threads a row as it has pieces, up to 1024: 32 registers a thread and so 2048 threads on an SM, whatever the width.
+// Two pieces a thread 65 us instead of 62 (16384 x 2048, bf16 and fp32) and 124 instead of 104 (8192 x 8192 into
+// 8 bits), four 68 and 133.  Narrow rows share a warp, four of a lane's at once: 26 us for 524288 rows of 64, one at a
+// time 36.
 template <int XT, int RT>
 cudaError_t norm_vec(const NormParams& p, int vec, cudaStream_t st) {
   const int h = p.h;
-  // A call of fewer rows than SMs is bound by the latency of one row: as many threads a row as there are
-  // pieces.  Otherwise a thread holds up to 32 values, so that few threads wait for one another.
-  const bool few = p.rows <= kSMs;
   if (vec == 8) {
     if (h <= 64) return norm_by_lanes<XT, RT, 8, 8, 1, 4>(p, st);
     if (h <= 128) return norm_by_lanes<XT, RT, 8, 16, 1, 4>(p, st);
     if (h <= 256) return norm_by_lanes<XT, RT, 8, 32, 1, 2>(p, st);
-    if (few && h <= 8192) return norm_by_block<XT, RT, 8, 1>(p, st);
-    if (h <= 512) return norm_by_lanes<XT, RT, 8, 32, 2, 1>(p, st);
-    if (h <= 1024) return norm_by_lanes<XT, RT, 8, 32, 4, 1>(p, st);
-    return norm_by_block<XT, RT, 8, 4>(p, st);
+    if (h <= 8192) return norm_by_block<XT, RT, 8, 1>(p, st);
+    return norm_by_block<XT, RT, 8, 2>(p, st);
   }
   if (vec == 4) {
     if (h <= 128) return norm_by_lanes<XT, RT, 4, 32, 1, 4>(p, st);
-    if (few && h <= 4096) return norm_by_block<XT, RT, 4, 1>(p, st);
-    if (h <= 512) return norm_by_lanes<XT, RT, 4, 32, 4, 1>(p, st);
+    if (h <= 4096) return norm_by_block<XT, RT, 4, 1>(p, st);
     return norm_by_block<XT, RT, 4, 4>(p, st);
   }
   if (h <= 128) return norm_by_lanes<XT, RT, 1, 32, 1, 4>(p, st);
-  if (few && h <= 4096) return norm_by_block<XT, RT, 1, 1>(p, st);
-  if (h <= 512) return norm_by_lanes<XT, RT, 1, 32, 4, 1>(p, st);
+  if (h <= 4096) return norm_by_block<XT, RT, 1, 1>(p, st);
   return norm_by_block<XT, RT, 1, 4>(p, st);
 }
 // r_dtype < 0: no residual
@@ -65,15 +62,15 @@ inline int64_t grad_blocks(int64_t rows, int64_t h, int vec) {
 }
 inline int64_t record_pitch(int64_t h) { return (h + 7) / 8 * 8; }  // VEC 8 writes 32 bytes at once
 
-template <int GT, int ST, int VEC, int L, int NI, int NR>
+template <int GT, int ST, bool ADD, int VEC, int L, int NI, int NR>
 cudaError_t grad_by_lanes(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
-  return launch_pdl(rms_norm_grad_kernel<GT, ST, VEC, L, NI, NR, false, 256>, dim3(static_cast<unsigned>(blocks)),
+  return launch_pdl(rms_norm_grad_kernel<GT, ST, ADD, VEC, L, NI, NR, false, 256>, dim3(static_cast<unsigned>(blocks)),
                     dim3(32, 8), st, p);
 }
-template <int GT, int ST, int VEC, int THREADS>
+template <int GT, int ST, bool ADD, int VEC, int THREADS>
 cudaError_t grad_by_block_of(const NormGradParams& p, int64_t blocks, int warps, cudaStream_t st) {
   constexpr int NI = grad_pieces<VEC>();
-  const auto kernel = rms_norm_grad_kernel<GT, ST, VEC, 32, NI, 1, true, THREADS>;
+  const auto kernel = rms_norm_grad_kernel<GT, ST, ADD, VEC, 32, NI, 1, true, THREADS>;
   const int values = warps * 32 * lane_values<VEC>() * NI;  // of the weight, with what lies behind the row's end
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), THREADS * NI * lane_values<VEC>() * sizeof(float));
   if (e != cudaSuccess) return e;
@@ -89,35 +86,36 @@ cudaError_t grad_by_block_of(const NormGradParams& p, int64_t blocks, int warps,
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
-template <int GT, int ST, int VEC>
+template <int GT, int ST, bool ADD, int VEC>
 cudaError_t grad_by_block(const NormGradParams& p, int64_t blocks, cudaStream_t st) {
   constexpr int cols = 32 * lane_values<VEC>() * grad_pieces<VEC>();
   static_assert(cols == 512, "grad_blocks counts on it");
   const int warps = (p.h + cols - 1) / cols;
-  if (warps <= 8) return grad_by_block_of<GT, ST, VEC, 256>(p, blocks, warps, st);
-  if (warps <= 16) return grad_by_block_of<GT, ST, VEC, 512>(p, blocks, warps, st);
-  return grad_by_block_of<GT, ST, VEC, 1024>(p, blocks, warps, st);
+  if (warps <= 8) return grad_by_block_of<GT, ST, ADD, VEC, 256>(p, blocks, warps, st);
+  if (warps <= 16) return grad_by_block_of<GT, ST, ADD, VEC, 512>(p, blocks, warps, st);
+  return grad_by_block_of<GT, ST, ADD, VEC, 1024>(p, blocks, warps, st);
 }
-template <int GT, int ST>
+template <int GT, int ST, bool ADD>
 cudaError_t grad_vec(const NormGradParams& p, int64_t blocks, int vec, cudaStream_t st) {
   const int h = p.h;
   if (vec == 8) {
-    if (h <= 64) return grad_by_lanes<GT, ST, 8, 8, 1, 4>(p, blocks, st);
-    if (h <= 128) return grad_by_lanes<GT, ST, 8, 16, 1, 4>(p, blocks, st);
-    if (h <= grad_lane_values(8)) return grad_by_lanes<GT, ST, 8, 32, 1, 4>(p, blocks, st);
-    return grad_by_block<GT, ST, 8>(p, blocks, st);
+    if (h <= 64) return grad_by_lanes<GT, ST, ADD, 8, 8, 1, 2>(p, blocks, st);
+    if (h <= 128) return grad_by_lanes<GT, ST, ADD, 8, 16, 1, 2>(p, blocks, st);
+    if (h <= grad_lane_values(8)) return grad_by_lanes<GT, ST, ADD, 8, 32, 1, 2>(p, blocks, st);
+    return grad_by_block<GT, ST, ADD, 8>(p, blocks, st);
   }
   if (vec == 4) {
-    if (h <= grad_lane_values(4)) return grad_by_lanes<GT, ST, 4, 32, 1, 4>(p, blocks, st);
-    return grad_by_block<GT, ST, 4>(p, blocks, st);
+    if (h <= grad_lane_values(4)) return grad_by_lanes<GT, ST, ADD, 4, 32, 1, 4>(p, blocks, st);
+    return grad_by_block<GT, ST, ADD, 4>(p, blocks, st);
   }
-  if (h <= grad_lane_values(1)) return grad_by_lanes<GT, ST, 1, 32, 1, 4>(p, blocks, st);
-  return grad_by_block<GT, ST, 1>(p, blocks, st);
+  if (h <= grad_lane_values(1)) return grad_by_lanes<GT, ST, ADD, 1, 32, 1, 4>(p, blocks, st);
+  return grad_by_block<GT, ST, ADD, 1>(p, blocks, st);
 }
 template <int GT>
 cudaError_t launch_norm_grad(const NormGradParams& p, int s_dtype, int64_t blocks, int vec, cudaStream_t st) {
-  if (s_dtype == GT) return grad_vec<GT, GT>(p, blocks, vec, st);
-  return grad_vec<GT, ABS_F32>(p, blocks, vec, st);
+  if (s_dtype == GT)
+    return p.add.p ? grad_vec<GT, GT, true>(p, blocks, vec, st) : grad_vec<GT, GT, false>(p, blocks, vec, st);
+  return p.add.p ? grad_vec<GT, ABS_F32, true>(p, blocks, vec, st) : grad_vec<GT, ABS_F32, false>(p, blocks, vec, st);
 }
 
 #ifndef ABS_INST_XT

@@ -12,17 +12,72 @@
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "abs_device.cuh"
 
 namespace absnt {
 
-// rows of a matrix as a kernel sees them; strides in bytes
+// Rows of a matrix as a kernel sees them; strides in bytes, and in units of `unit` bytes (the size of a thread's access)
+// where rows are read in vectors: one multiplication of 32 bits finds a row that lies up to 2^32 units away.
 struct RowsArg {
   unsigned char* p;
   int64_t s0, s1;
+  uint32_t u0, u1, unit;
 };
 __device__ __forceinline__ unsigned char* row_of(const RowsArg& a, uint32_t i, uint32_t j) {
   return a.p + static_cast<int64_t>(i) * a.s0 + static_cast<int64_t>(j) * a.s1;
+}
+template <int VEC>
+__device__ __forceinline__ unsigned char* row_of(const RowsArg& a, uint32_t i, uint32_t j) {
+  if constexpr (VEC == 1) return row_of(a, i, j);
+  return a.p + static_cast<uint64_t>(i * a.u0 + j * a.u1) * a.unit;
+}
+
+// n / d for n < 2^31 as a product with m = ceil(2^(31 + s) / d), s = ceil(log2 d): m d exceeds 2^(31 + s) by less than d <=
+// 2^s, so n m / 2^(31 + s) exceeds n / d by less than n / (2^31 d) < 1 / d, which never reaches the next whole number.
+struct Divisor {
+  uint32_t d, m, shift;  // shift: s - 1
+};
+inline Divisor divisor(uint32_t d) {
+  Divisor r = {d, 0, 0};
+  if (d < 2) return r;
+  uint32_t s = 1;
+  while ((uint64_t{1} << s) < d) ++s;
+  r.m = static_cast<uint32_t>(((uint64_t{1} << (31 + s)) + d - 1) / d);
+  r.shift = s - 1;
+  return r;
+}
+__device__ __forceinline__ void split_row(uint32_t row, const Divisor& by, uint32_t& i, uint32_t& j) {
+  i = by.d == 1 ? row : __umulhi(row, by.m) >> by.shift;
+  j = by.d == 1 ? 0u : row - i * by.d;
+}
+
+// ---- two floats in one instruction slot
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 pair_as(uint64_t x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
 }
 
 template <int DT>
@@ -59,25 +114,31 @@ struct Piece {
   }
   __device__ __forceinline__ void load(const unsigned char* row, int first, int l, int h) {
     if constexpr (VEC == 1) {
+      const unsigned char* const at = row + static_cast<int64_t>(first + l) * elem_bytes<DT>();
+      auto one = [&](int j) {
+        if constexpr (DT == ABS_F32) {
+          asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(w[j]) : "l"(at + 128 * j));
+        } else {
+          unsigned short x;
+          asm volatile("ld.global.L1::no_allocate.b16 %0, [%1];" : "=h"(x) : "l"(at + 64 * j));
+          w[j] = x;
+        }
+      };
+      if (first + 128 <= h) {  // all of the warp's pieces but the row's last
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const int c = first + l + 32 * j;
-        w[j] = 0u;
-        if (c < h) {
-          if constexpr (DT == ABS_F32) {
-            asm volatile("ld.global.L1::no_allocate.b32 %0, [%1];" : "=r"(w[j]) : "l"(row + 4 * static_cast<int64_t>(c)));
-          } else {
-            unsigned short x;
-            asm volatile("ld.global.L1::no_allocate.b16 %0, [%1];" : "=h"(x) : "l"(row + 2 * static_cast<int64_t>(c)));
-            w[j] = x;
-          }
+        for (int j = 0; j < E; ++j) one(j);
+      } else {
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          w[j] = 0u;
+          if (first + l + 32 * j < h) one(j);
         }
       }
     } else {
       const int c = first + l * VEC;
       zero();
       if (c < h) {
-        const unsigned char* p = row + static_cast<int64_t>(c) * elem_bytes<DT>();
+        const unsigned char* p = row + static_cast<uint32_t>(c) * elem_bytes<DT>();
         if constexpr (WORDS == 8) {
           asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                        : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]),
@@ -91,6 +152,13 @@ struct Piece {
           asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
         }
       }
+    }
+  }
+  // what follows unpacks the words again instead of keeping the values in twice the registers until then
+  __device__ __forceinline__ void keep_packed() {
+    if constexpr (DT != ABS_F32) {
+#pragma unroll
+      for (int k = 0; k < WORDS; ++k) asm volatile("" : "+r"(w[k]));
     }
   }
   __device__ __forceinline__ float get(int j) const {
@@ -118,19 +186,25 @@ template <int DT, int VEC>
 __device__ __forceinline__ void store_piece(unsigned char* row, int first, int l, int h, const float* v) {
   constexpr int E = lane_values<VEC>();
   if constexpr (VEC == 1) {
+    unsigned char* const at = row + static_cast<int64_t>(first + l) * elem_bytes<DT>();
+    auto one = [&](int j) {
+      if constexpr (DT == ABS_F32) reinterpret_cast<float*>(at)[32 * j] = v[j];
+      else if constexpr (DT == ABS_BF16) reinterpret_cast<__nv_bfloat16*>(at)[32 * j] = __float2bfloat16_rn(v[j]);
+      else if constexpr (DT == ABS_F16) reinterpret_cast<__half*>(at)[32 * j] = __float2half_rn(v[j]);
+      else at[32 * j] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, DT == ABS_E4M3 ? __NV_E4M3 : __NV_E5M2);
+    };
+    if (first + 128 <= h) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const int c = first + l + 32 * j;
-      if (c >= h) continue;
-      if constexpr (DT == ABS_F32) reinterpret_cast<float*>(row)[c] = v[j];
-      else if constexpr (DT == ABS_BF16) reinterpret_cast<__nv_bfloat16*>(row)[c] = __float2bfloat16_rn(v[j]);
-      else if constexpr (DT == ABS_F16) reinterpret_cast<__half*>(row)[c] = __float2half_rn(v[j]);
-      else row[c] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, DT == ABS_E4M3 ? __NV_E4M3 : __NV_E5M2);
+      for (int j = 0; j < E; ++j) one(j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (first + l + 32 * j < h) one(j);
     }
   } else {
     const int c = first + l * VEC;
     if (c >= h) return;
-    unsigned char* p = row + static_cast<int64_t>(c) * elem_bytes<DT>();
+    unsigned char* p = row + static_cast<uint32_t>(c) * elem_bytes<DT>();
     if constexpr (DT == ABS_F32) {
       if constexpr (VEC == 8)
         asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]),
@@ -159,33 +233,27 @@ __device__ __forceinline__ void store_piece(unsigned char* row, int first, int l
   }
 }
 
-// the same for a type known when the kernel runs (the same for all threads)
-template <int VEC>
-__device__ __forceinline__ void store_piece_as(int dt, unsigned char* row, int first, int l, int h, const float* v) {
-  if (dt == ABS_BF16) store_piece<ABS_BF16, VEC>(row, first, l, h, v);
-  else if (dt == ABS_F32) store_piece<ABS_F32, VEC>(row, first, l, h, v);
-  else if (dt == ABS_F16) store_piece<ABS_F16, VEC>(row, first, l, h, v);
-  else if (dt == ABS_E4M3) store_piece<ABS_E4M3, VEC>(row, first, l, h, v);
-  else store_piece<ABS_E5M2, VEC>(row, first, l, h, v);
+// f(the type) for one of the three types of 16 and 32 bits that is known when the kernel runs, the same for all threads
+template <typename F>
+__device__ __forceinline__ void with_type(int dt, F f) {
+  if (dt == ABS_BF16) f(std::integral_constant<int, ABS_BF16>());
+  else if (dt == ABS_F32) f(std::integral_constant<int, ABS_F32>());
+  else f(std::integral_constant<int, ABS_F16>());
 }
 
-// E values of a contiguous vector (a weight) of a type known when the kernel runs; ones if there is none
-template <int VEC>
-__device__ __forceinline__ void load_weight(float* v, const unsigned char* w, int dt, int first, int l, int h) {
+// E values of a contiguous vector (a weight); ones if there is none
+template <int DT, int VEC>
+__device__ __forceinline__ void load_weight_of(float* v, const unsigned char* w, int first, int l, int h) {
   constexpr int E = lane_values<VEC>();
-  if (!w) {
-#pragma unroll
-    for (int j = 0; j < E; ++j) v[j] = 1.f;
-    return;
-  }
-  auto take = [&](auto piece) {
+  if (w) {
+    Piece<DT, VEC> piece;
     piece.load(w, first, l, h);
 #pragma unroll
     for (int j = 0; j < E; ++j) v[j] = piece.get(j);
-  };
-  if (dt == ABS_BF16) take(Piece<ABS_BF16, VEC>());
-  else if (dt == ABS_F32) take(Piece<ABS_F32, VEC>());
-  else take(Piece<ABS_F16, VEC>());
+  } else {
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[j] = 1.f;
+  }
 }
 
 // sums and maxima over the aligned group of L lanes that a thread belongs to, in a fixed order

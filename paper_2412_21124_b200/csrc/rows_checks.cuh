@@ -24,7 +24,12 @@ struct Rows {
   bool given() const { return p != nullptr; }
   int64_t row_bytes() const { return h * esz; }
   int64_t bytes() const { return (n0 - 1) * s0 + (n1 - 1) * s1 + row_bytes(); }
-  RowsArg arg() const { return {const_cast<unsigned char*>(p), s0, s1}; }
+  // as a kernel that reads `vec` values at once sees it (see rows_aligned)
+  RowsArg arg(int vec = 1) const {
+    const int64_t unit = static_cast<int64_t>(vec) * (esz ? esz : 1);
+    return {const_cast<unsigned char*>(p), s0, s1, static_cast<uint32_t>(s0 / unit), static_cast<uint32_t>(s1 / unit),
+            static_cast<uint32_t>(unit)};
+  }
 };
 
 constexpr int64_t kMostElements = int64_t{1} << 46;  // between a tensor's first element and its last
@@ -86,10 +91,10 @@ inline bool rows_touch(const Rows& a, const Rows& b) {
   return false;
 }
 
-// all rows begin on multiples of `vec` values
+// all rows begin on multiples of `vec` values, and at most 2^32 such multiples behind the first
 inline bool rows_aligned(const Rows& r, int vec) {
   const int64_t a = static_cast<int64_t>(vec) * r.esz;
-  return !r.given() || (!misaligned(r.p, a) && r.s0 % a == 0 && r.s1 % a == 0);
+  return !r.given() || (!misaligned(r.p, a) && r.s0 % a == 0 && r.s1 % a == 0 && r.bytes() / a <= INT64_C(0xffffffff));
 }
 
 }  // namespace absnt
