@@ -65,7 +65,7 @@ __host__ __device__ constexpr int grad_pieces() {
 __host__ __device__ constexpr int grad_blocks_per_sm(bool block, int vec) { return !block || vec > 1 ? 3 : 2; }
 
 template <int GT, int ST, bool ADD, int VEC, int L, int NI, int NR, bool BLOCK, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(BLOCK, VEC) : 1) rms_norm_grad_kernel(const NormGradParams p) {
+__global__ void __launch_bounds__(THREADS, THREADS == 256 ? (BLOCK && NI < grad_pieces<VEC>() ? 4 : grad_blocks_per_sm(BLOCK, VEC)) : 1) rms_norm_grad_kernel(const NormGradParams p) {
   constexpr int E = lane_values<VEC>();
   constexpr int kGroups = 32 / L;
   constexpr bool JOIN = THREADS == 256;  // several groups of threads hold rows: their sums are added

@@ -57,7 +57,7 @@ cudaError_t launch_norm(const NormParams& p, int r_dtype, int vec, cudaStream_t 
 constexpr int grad_lane_values(int vec) { return vec == 8 ? 256 : 128; }
 // Blocks of the kernel that sums over rows: as many as fit the SMs at once.
 inline int64_t grad_blocks(int64_t rows, int64_t h, int vec) {
-  const int64_t most = kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec) : 1);
+  const int64_t most = kSMs * (h <= 2048 && h > grad_lane_values(vec) ? 4 : h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec) : 1);
   return rows < most ? rows : most;
 }
 inline int64_t record_pitch(int64_t h) { return (h + 7) / 8 * 8; }  // VEC 8 writes 32 bytes at once
@@ -67,9 +67,8 @@ cudaError_t grad_by_lanes(const NormGradParams& p, int64_t blocks, cudaStream_t 
   return launch_pdl(rms_norm_grad_kernel<GT, ST, ADD, VEC, L, NI, NR, false, 256>, dim3(static_cast<unsigned>(blocks)),
                     dim3(32, 8), st, p);
 }
-template <int GT, int ST, bool ADD, int VEC, int THREADS>
+template <int GT, int ST, bool ADD, int VEC, int THREADS, int NI = grad_pieces<VEC>()>
 cudaError_t grad_by_block_of(const NormGradParams& p, int64_t blocks, int warps, cudaStream_t st) {
-  constexpr int NI = grad_pieces<VEC>();
   const auto kernel = rms_norm_grad_kernel<GT, ST, ADD, VEC, 32, NI, 1, true, THREADS>;
   const int values = warps * 32 * lane_values<VEC>() * NI;  // of the weight, with what lies behind the row's end
   const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), THREADS * NI * lane_values<VEC>() * sizeof(float));
@@ -91,6 +90,10 @@ cudaError_t grad_by_block(const NormGradParams& p, int64_t blocks, cudaStream_t 
   constexpr int cols = 32 * lane_values<VEC>() * grad_pieces<VEC>();
   static_assert(cols == 512, "grad_blocks counts on it");
   const int warps = (p.h + cols - 1) / cols;
+  if (p.h <= 2048) {
+    constexpr int half = 32 * lane_values<VEC>() * (grad_pieces<VEC>() / 2);
+    return grad_by_block_of<GT, ST, ADD, VEC, 256, grad_pieces<VEC>() / 2>(p, blocks, (p.h + half - 1) / half, st);
+  }
   if (warps <= 8) return grad_by_block_of<GT, ST, ADD, VEC, 256>(p, blocks, warps, st);
   if (warps <= 16) return grad_by_block_of<GT, ST, ADD, VEC, 512>(p, blocks, warps, st);
   return grad_by_block_of<GT, ST, ADD, VEC, 1024>(p, blocks, warps, st);
