@@ -83,7 +83,7 @@ cudaError_t distill_by_ring(const DistillParams& p, const RingShape& s, cudaStre
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int64_t clusters = ring_clusters(reinterpret_cast<const void*>(kernel), cfg);
-  if (clusters < 1) return cudaErrorInvalidConfiguration;
+  if (clusters < 1) return distill_by_block<DT, 1>(p, st);  // a device that does not take the cluster
   if (clusters > p.rows) clusters = p.rows;
   cfg.gridDim = dim3(static_cast<unsigned>(clusters * s.blocks));
   cfg.numAttrs = 2;
