@@ -244,11 +244,12 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
   m.n_samples = p.n_samples;
   m.h = p.h;
   m.blocks = static_cast<int>(blocks);
-  m.col_blocks = (p.h + 31) / 32;
   m.n_out = a->dweight_samples ? p.n_samples : 0;
+  m.col_bits = m.n_out > 0 && blocks / m.n_out < 64 ? 7 : 5;
+  m.sample_blocks = ((p.h - 1) >> m.col_bits) + 1;
   m.scale = static_cast<float>(a->sample_scale);
-  const int64_t grid = (m.n_out + (a->dweight ? 1 : 0)) * static_cast<int64_t>(m.col_blocks);
-  const cudaError_t e = launch_pdl(rms_norm_merge_kernel, dim3(static_cast<unsigned>(grid)), dim3(32, kMergeSlices), st, m);
+  const int64_t grid = static_cast<int64_t>(m.n_out) * m.sample_blocks + (a->dweight ? (p.h + 31) / 32 : 0);
+  const cudaError_t e = launch_pdl(rms_norm_merge_kernel, dim3(static_cast<unsigned>(grid)), dim3(kMergeThreads), st, m);
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
 

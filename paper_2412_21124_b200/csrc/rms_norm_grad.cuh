@@ -327,9 +327,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? (BLOCK && NI < grad_
   }
 }
 
-// Adds the records: blocks of 32 columns x kMergeSlices.  Block row b < n_out: the pieces of sample b, behind
-// them the totals.
-constexpr int kMergeSlices = 32;
+// Adds the records, a block of 1024 threads for 32 columns by 32 slices of the records, or 128 by 8 where a sample has
+// few of them.  The first blocks take the pieces of the samples, those behind them the totals.
+constexpr int kMergeThreads = 1024;
 struct NormMergeParams {
   const float *totals, *pieces;
   int64_t pitch;
@@ -337,21 +337,27 @@ struct NormMergeParams {
   float *dw, *dw_samples;  // may be NULL
   int64_t ld;
   uint32_t rows, n1;
-  int n_samples, h, blocks, col_blocks;
+  int n_samples, h, blocks;
   int n_out;               // samples that are written: n_samples or 0
+  int col_bits;            // of the samples' blocks: 5 or 7
+  int sample_blocks;       // of a sample
   float scale;             // of dw_samples
 };
 
 #ifndef ABS_INST_XT  // no template: compiled where it is launched
-__global__ void __launch_bounds__(32 * kMergeSlices) rms_norm_merge_kernel(const NormMergeParams p) {
-  __shared__ float sums[kMergeSlices][32];
-  const int b = blockIdx.x / p.col_blocks;
-  const int col = (blockIdx.x - b * p.col_blocks) * 32 + threadIdx.x;
+__global__ void __launch_bounds__(kMergeThreads) rms_norm_merge_kernel(const NormMergeParams p) {
+  __shared__ float sums[kMergeThreads];
+  const int of_samples = p.n_out * p.sample_blocks;
+  const bool sample = static_cast<int>(blockIdx.x) < of_samples;
+  const int bits = sample ? p.col_bits : 5;
+  const int b = sample ? static_cast<int>(blockIdx.x) / p.sample_blocks : p.n_out;
+  const int first = (sample ? static_cast<int>(blockIdx.x) - b * p.sample_blocks : static_cast<int>(blockIdx.x) - of_samples) << bits;
+  const int col = first + (threadIdx.x & ((1 << bits) - 1)), slice = threadIdx.x >> bits, slices = kMergeThreads >> bits;
   grid_dependency_wait();
   const Span span = span_of(p.offsets, p.n_samples, p.n1, p.rows, p.blocks);
   const float* from = p.totals;
   int64_t lo = 0, hi = span.blocks;  // records [lo, hi)
-  if (b < p.n_out) {
+  if (sample) {
     const int64_t a = table_at(p.offsets, b, p.n1, span.first, span.first + span.total) - span.first;
     const int64_t e = table_at(p.offsets, b + 1, p.n1, span.first, span.first + span.total) - span.first;
     from = p.pieces;
@@ -364,14 +370,13 @@ __global__ void __launch_bounds__(32 * kMergeSlices) rms_norm_merge_kernel(const
   float x = 0.f;
   if (col < p.h)
 #pragma unroll 8
-    for (int64_t k = lo + threadIdx.y; k < hi; k += kMergeSlices) x += from[k * p.pitch + col];
-  sums[threadIdx.y][threadIdx.x] = x;
+    for (int64_t k = lo + slice; k < hi; k += slices) x += from[k * p.pitch + col];
+  sums[threadIdx.x] = x;
   __syncthreads();
-  if (threadIdx.y == 0 && col < p.h) {
+  if (slice == 0 && col < p.h) {
     x = 0.f;
-#pragma unroll
-    for (int k = 0; k < kMergeSlices; ++k) x += sums[k][threadIdx.x];
-    if (b < p.n_out) p.dw_samples[b * p.ld + col] = x * p.scale;
+    for (int k = 0; k < slices; ++k) x += sums[(k << bits) + threadIdx.x];
+    if (sample) p.dw_samples[b * p.ld + col] = x * p.scale;
     else p.dw[col] = x;
   }
 }
