@@ -14,7 +14,9 @@ Timing: CUDA events on the launching stream around `steps` back-to-back calls af
 replays are timed, so that the figure is device time.  Points whose working set is smaller than twice the L2 rotate over several
 independent buffer sets so that every call reads cold data.  GB/s counts algorithmic bytes:
 fused (K*s + 24) per coordinate (+4 with --gbar, +2 with --mixed), normtest K*s + 4,
-adamw 28 (+2 with --mixed), persample 4 (fp32) or 2 (bf16) per matrix element.
+adamw 28 (+2 with --mixed), persample 4 (fp32) or 2 (bf16) per matrix element, and for b rows of d values
+rms_norm 2s + 8 (x and the output, an fp32 residual stream read and written), rms_norm_grad s + 12 (with the
+weight's gradient of 8 samples), distill 2s (logits and their gradient) + 12 for each of 64 entries of the top.
 """
 import argparse
 import json
@@ -33,6 +35,28 @@ L2_BYTES = 126 * 1024 * 1024
 SWEEP_D = (1_048_576, 16_777_216, 124_439_808, 400_000_000, 1_235_814_400)
 SWEEP_K = (2, 4, 8, 16, 32)
 MEM_CAP = 160e9
+DISTILL_TOP = 64
+ROW_CALLS = ("rms_norm", "rms_norm_grad", "distill")
+
+
+def _row_buffers(call, b, d, tdt, dev):
+    """What a call on b rows of d values works on."""
+    x = torch.empty(b, d, device=dev).normal_().to(tdt)
+    if call == "distill":
+        # 64 different places a row, and a teacher that favours them
+        ids = (torch.randint(d, (b, 1), device=dev) + torch.arange(DISTILL_TOP, device=dev) * (d // DISTILL_TOP)) % d
+        return {"x": x, "ids": ids, "top": torch.empty(b, DISTILL_TOP, device=dev).normal_() + 6.0, "out": torch.empty_like(x),
+                "losses": torch.empty(b, device=dev)}
+    s = {"x": x, "w": torch.ones(d, device=dev, dtype=tdt), "stream": torch.empty(b, d, device=dev).normal_(),
+         "stream_out": torch.empty(b, d, device=dev)}
+    if call == "rms_norm":
+        s["out"] = torch.empty_like(x)
+    else:
+        s["add"] = torch.empty(b, d, device=dev).normal_()
+        s["offsets"] = torch.tensor([i * b // 8 for i in range(9)], dtype=torch.int32, device=dev)
+        s["dw"], s["apart"] = torch.empty(d, device=dev), torch.empty(8, d, device=dev)
+        s["work"] = B.alloc_rms_norm_work(x, 8)
+    return s
 
 
 def _sizes(d):
@@ -52,6 +76,12 @@ def bytes_per_call(call, d, K, esz, gbar, b):
         return (K * esz + 8) * d
     if call == "accumulate_adamw":  # the closing call: mean read, p/m/v read and written
         return (K * esz + 4 + 24) * d
+    if call == "rms_norm":
+        return (2 * esz + 8) * b * d
+    if call == "rms_norm_grad":
+        return (esz + 12) * b * d
+    if call == "distill":
+        return (2 * esz * d + 12 * DISTILL_TOP) * b
     return esz * b * d
 
 
@@ -84,6 +114,8 @@ def run_point(call, d, K, dtype, n_shards=1, steps=None, warmup=3, gbar=False, b
             s["G"] = torch.empty(b, d, dtype=torch.float32, device=dev).normal_().mul_(0.3).to(tdt)
             s["stats"] = B.alloc_persample_stats(b, d, dev)
             s["gbar"] = torch.zeros(d, dtype=torch.float32, device=dev)
+        if call in ROW_CALLS:
+            s = _row_buffers(call, b, d, tdt, dev)
         s["b_next"] = torch.zeros(1, dtype=torch.int64, device=dev)
         if mixed:
             s["p16"] = torch.zeros(d, dtype=torch.bfloat16, device=dev)
@@ -112,6 +144,13 @@ def run_point(call, d, K, dtype, n_shards=1, steps=None, warmup=3, gbar=False, b
             B.abs_norm_test_accumulate_adamw(s["grads"], 8 * K, 0.1, 512, s["stats"], s["gbar"],
                                              None, s["b_next"], s["p"], s["m"], s["v"], HP,
                                              100 + i, shard_offsets=offs)
+        elif call == "rms_norm":
+            B.abs_rms_norm(s["x"], s["w"], s["out"], residual=s["stream"], sum_out=s["stream_out"])
+        elif call == "rms_norm_grad":
+            B.abs_rms_norm_grad(s["x"], s["stream"], s["w"], s["stream_out"], s["dw"], dresidual=s["add"],
+                                offsets=s["offsets"], dweight_samples=s["apart"], work=s["work"])
+        elif call == "distill":
+            B.abs_distill_loss(s["x"], s["ids"], s["top"], s["losses"], dlogits=s["out"])
         else:
             fn = B.abs_persample_norm_test_coordwise if coordwise else B.abs_persample_norm_test
             fn(s["G"], 0.1, s["stats"], s["gbar"], s["b_next"])
@@ -174,7 +213,7 @@ def run_point(call, d, K, dtype, n_shards=1, steps=None, warmup=3, gbar=False, b
            "steps": steps, "buffer_sets": n_sets, "cuda_graph": bool(graph),
            "ms": ms,
            "bytes": nbytes, "GBps": nbytes / (ms * 1e-3) / 1e9}
-    if call == "persample":
+    if call == "persample" or call in ROW_CALLS:
         out["b"] = b
     ck = sampler.summary(t_begin, t_end)
     out["clocks"] = {"sm_mhz": ck["sm_mhz"], "sm_max_mhz": ck["sm_max_mhz"],
@@ -209,6 +248,9 @@ REPORT_POINTS = (
     # the carry-in form: K new gradients merged into the running mean per call
     + [("accumulate", GPT2, K, dt, 1, {}) for K in (1, 2, 4, 8, 9, 12, 16, 32) for dt in ("bf16", "f32")]
     + [("accumulate_adamw", GPT2, K, "bf16", 1, {}) for K in (1, 4, 8, 16)]
+    # calls on rows: a layer's norm and its gradient (width 2048), the loss over the vocabularies of the models
+    + [(call, 2048, 0, "bf16", 1, {"b": b}) for call in ("rms_norm", "rms_norm_grad") for b in (64, 2048, 16384)]
+    + [("distill", d, 0, "bf16", 1, {"b": b}) for d, b in ((32_000, 64), (32_000, 8192), (50_257, 4096), (128_256, 2048))]
     # the paper's own model sizes (Table 4), J = 4 workers, bf16
     + [("fused", d, 4, "bf16", 1, {}) for d in (304_600_000, 1_100_000_000, 3_400_000_000)])
 
@@ -282,7 +324,7 @@ def format_markdown(path):
         name = r["call"] + (" +gbar" if r.get("gbar") and r["call"] == "fused" else "") + (
             " +bf16 copy" if r.get("mixed") else "") + (" +Q" if r.get("with_q") else "") + (
             " coordinate-wise" if r.get("coordwise") else "")
-        kb = r["b"] if r["call"] == "persample" else (r["K"] if r["call"] != "adamw" else "-")
+        kb = r["b"] if "b" in r else (r["K"] if r["call"] != "adamw" else "-")
         mhz, why = clk(r)
         print("| %s | %d | %s | %s | %d | %.4f | %.0f | %.3f | %s | %s | %s |" % (
             name, r["d"], kb, r["dtype"], r["n_shards"], r["ms"], r["GBps"], r["GBps"] / 8000.0,
@@ -292,12 +334,12 @@ def format_markdown(path):
 def main(argv=None):
     ap = argparse.ArgumentParser()
     ap.add_argument("--call", choices=["fused", "normtest", "adamw", "persample", "accumulate",
-                                       "accumulate_adamw"], default="fused")
+                                       "accumulate_adamw", *ROW_CALLS], default="fused")
     ap.add_argument("--d", type=int, default=33_554_432)
     ap.add_argument("--K", type=int, default=8)
     ap.add_argument("--dtype", choices=["bf16", "f32"], default="bf16")
     ap.add_argument("--shards", type=int, default=1)
-    ap.add_argument("--b", type=int, default=4096, help="rows of the per-sample matrix")
+    ap.add_argument("--b", type=int, default=4096, help="rows of the per-sample matrix, or of the calls on rows")
     ap.add_argument("--steps", type=int, default=None)
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--gbar", action="store_true", help="fused: also write gbar")
