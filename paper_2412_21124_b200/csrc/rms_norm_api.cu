@@ -245,10 +245,11 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* a, abs_stream_t stream) {
   m.h = p.h;
   m.blocks = static_cast<int>(blocks);
   m.n_out = a->dweight_samples ? p.n_samples : 0;
-  m.col_bits = m.n_out > 0 && blocks / m.n_out < 64 ? 7 : 5;
+  // 2048 x 2048 with 8 samples: 17.4 us with 128 columns, 18.3 with 32; 2048 x 4096 28.7 and 30.3
+  m.col_bits = m.n_out > 0 && blocks / m.n_out < 128 ? 7 : 5;
   m.sample_blocks = ((p.h - 1) >> m.col_bits) + 1;
   m.scale = static_cast<float>(a->sample_scale);
-  const int64_t grid = static_cast<int64_t>(m.n_out) * m.sample_blocks + (a->dweight ? (p.h + 31) / 32 : 0);
+  const int64_t grid = static_cast<int64_t>(m.n_out) * m.sample_blocks + (a->dweight ? ((p.h - 1) >> kTotalsBits) + 1 : 0);
   const cudaError_t e = launch_pdl(rms_norm_merge_kernel, dim3(static_cast<unsigned>(grid)), dim3(kMergeThreads), st, m);
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
