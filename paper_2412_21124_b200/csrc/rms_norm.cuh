@@ -3,9 +3,14 @@
 //
 //   s = x + residual,   rstd = (sum_c s_c^2 / h + eps)^(-1/2),   y_c = s_c rstd w_c
 //
-// One pass: a row is loaded once into registers (at most 32 values a thread), its squares are summed over
-// the threads that hold it, and y, the rounded s and the scales are written from the same registers.  s is
-// not rounded before it is normalised.  Bound by HBM: 2 to 12 bytes a value and about ten instructions.
+// One pass: a row is loaded once into registers (a piece of 4 or 8 values a thread, more where the row would take
+// over 1024 threads), its squares are summed over the threads that hold it, and y, the rounded s and the
+// scales are written from the same registers.  s is not rounded before it is normalised.
+//
+// Bounds: HBM where the output has 16 or 32 bits, 16384 x 2048 with an fp32 residual stream 62 us, 6.4 TB/s.  In
+// 8 bits with a scale for 32 values it is instruction issue, some 40 of a warp for each value of a lane (8192 x 8192
+// 104 us, 4.5 TB/s); 524288 heads of 64 take 26 us, 5.2 TB/s.  Two values in one instruction slot brought nothing:
+// what they save goes into moving registers side by side.
 #pragma once
 #include "rows.cuh"
 
@@ -68,10 +73,10 @@ __device__ __forceinline__ float squares(const float (&s)[NI][E]) {
     for (int j = 0; j < E; ++j) t[j & 1] = fmaf(s[i][j], s[i][j], t[j & 1]);
   return t[0] + t[1];
 }
-// L lanes (a whole warp if BLOCK: blockDim.x / 32 of them) hold one row in NI pieces; without BLOCK a group
-// of lanes takes NR rows at once.  blockDim.y rows (warps) a block.
+// BLOCK: a row a block, in NI pieces a thread.  Otherwise L lanes hold a row in NI pieces, NR rows of a group of
+// lanes at once; blockDim.y warps a block.
 template <int XT, int RT, int VEC, int L, int NI, int NR, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 1024) : 256)
+__global__ void __launch_bounds__(BLOCK ? 1024 : 256)
     rms_norm_kernel(const NormParams p) {
   constexpr int E = lane_values<VEC>();
   constexpr bool HAS_R = RT >= 0;
@@ -83,9 +88,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
   const int lane = threadIdx.x & 31, l = lane % L;
   const int warps = BLOCK ? static_cast<int>(blockDim.x) >> 5 : 1;       // of a row
   const int warp = BLOCK ? static_cast<int>(threadIdx.x) >> 5 : 0;       // in the row
-  const int mine = BLOCK ? static_cast<int>(threadIdx.y) * warps : 0;    // first of the row's slots in part[]
-  const uint32_t slot = BLOCK ? blockIdx.x * blockDim.y + threadIdx.y
-                              : (blockIdx.x * blockDim.y + threadIdx.y) * (kGroups * NR) + lane / L;
+  const uint32_t slot = BLOCK ? blockIdx.x : (blockIdx.x * blockDim.y + threadIdx.y) * (kGroups * NR) + lane / L;
   uint32_t row[NR], ri[NR], rj[NR];
 #pragma unroll
   for (int k = 0; k < NR; ++k) {
@@ -141,11 +144,11 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 
   bool again;  // some row of the block (the warp) needs its squares summed again, scaled
   if constexpr (BLOCK) {
-    if (lane == 0) part[mine + warp] = ss[0];
+    if (lane == 0) part[warp] = ss[0];
     __syncthreads();
-    const int all = warps * static_cast<int>(blockDim.y);
-    again = __any_sync(0xffffffffu, lane < all && !(part[lane < all ? lane : 0] <= kSquaresLimit));
-    ss[0] = lanes_sum<32>(lane < warps ? part[mine + lane] : 0.f);
+    const float t = lane < warps ? part[lane] : 0.f;
+    again = __any_sync(0xffffffffu, !(t <= kSquaresLimit));
+    ss[0] = lanes_sum<32>(t);
   } else {
     bool over = false;
 #pragma unroll
@@ -165,9 +168,9 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
         for (int j = 0; j < E; ++j) s[k][i][j] *= down ? kDown : 1.f;
       float t = lanes_sum<L>(squares(s[k]));
       if constexpr (BLOCK) {
-        if (lane == 0) part_again[mine + warp] = t;
+        if (lane == 0) part_again[warp] = t;
         __syncthreads();
-        t = lanes_sum<32>(lane < warps ? part_again[mine + lane] : 0.f);
+        t = lanes_sum<32>(lane < warps ? part_again[lane] : 0.f);
       }
       if (down) rstd[k] = rsqrtf(t * p.inv_h);
     }
@@ -226,9 +229,9 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
         for (int j = 0; j < E; ++j) a = larger(a, s[k][i][j]);
       a_row[k] = lanes_max(__float_as_uint(a), L);
       if constexpr (BLOCK) {
-        if (lane == 0) part_max[mine + warp] = a_row[k];
+        if (lane == 0) part_max[warp] = a_row[k];
         __syncthreads();
-        a_row[k] = lanes_max(lane < warps ? part_max[mine + lane] : 0u, 32);
+        a_row[k] = lanes_max(lane < warps ? part_max[lane] : 0u, 32);
       }
     }
   }

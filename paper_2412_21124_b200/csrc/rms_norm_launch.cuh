@@ -19,7 +19,7 @@ cudaError_t norm_by_lanes(const NormParams& p, cudaStream_t st) {
 template <int XT, int RT, int VEC, int NI>
 cudaError_t norm_by_block(const NormParams& p, cudaStream_t st) {
   constexpr int cols = 32 * lane_values<VEC>() * NI;  // of a warp
-  return launch_pdl(rms_norm_kernel<XT, RT, VEC, 32, NI, 1, true>, dim3(p.rows), dim3(32 * ((p.h + cols - 1) / cols), 1), st, p);
+  return launch_pdl(rms_norm_kernel<XT, RT, VEC, 32, NI, 1, true>, dim3(p.rows), dim3(32 * ((p.h + cols - 1) / cols)), st, p);
 }
 // As many threads a row as it has pieces, up to 1024: 32 registers a thread and so 2048 threads on an SM, whatever the width.
 // Two pieces a thread 65 us instead of 62 (16384 x 2048, bf16 and fp32) and 124 instead of 104 (8192 x 8192 into
@@ -53,12 +53,14 @@ cudaError_t launch_norm(const NormParams& p, int r_dtype, int vec, cudaStream_t 
 }
 
 // ---- backward
-// A row of at most this many values goes to the lanes of a warp, four rows at once.
+// A row of at most this many values goes to the lanes of a warp, two or four rows at once; one of at most kGradHalf to
+// threads of eight values, wider ones to threads of sixteen (9001 x 1537 f16: five us more with sixteen).
+constexpr int kGradHalf = 2048;
 constexpr int grad_lane_values(int vec) { return vec == 8 ? 256 : 128; }
 // Blocks of the kernel that sums over rows: as many as fit the SMs at once, but two rows a block at least, since every
 // block leaves a record: 512 x 2048 with 8 samples 15 us by 512 blocks, 11 by 256, 13 by 128, and 512 x 768 8.9, 7.8, 8.8.
 inline int64_t grad_blocks(int64_t rows, int64_t h, int vec) {
-  const int64_t most = kSMs * (h <= 2048 && h > grad_lane_values(vec) ? 4 : h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec) : 1);
+  const int64_t most = kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec, h <= kGradHalf) : 1);
   const int64_t pairs = (rows + 1) / 2;
   return pairs < most ? pairs : most;
 }
@@ -92,7 +94,7 @@ cudaError_t grad_by_block(const NormGradParams& p, int64_t blocks, cudaStream_t 
   constexpr int cols = 32 * lane_values<VEC>() * grad_pieces<VEC>();
   static_assert(cols == 512, "grad_blocks counts on it");
   const int warps = (p.h + cols - 1) / cols;
-  if (p.h <= 2048) {
+  if (p.h <= kGradHalf) {
     constexpr int half = 32 * lane_values<VEC>() * (grad_pieces<VEC>() / 2);
     return grad_by_block_of<GT, ST, ADD, VEC, 256, grad_pieces<VEC>() / 2>(p, blocks, (p.h + half - 1) / half, st);
   }
