@@ -1,4 +1,6 @@
 // C entry points of the root-mean-square norm and its backward pass: checks and launches.
+#include <algorithm>
+
 #include "rms_norm_launch.cuh"
 #include "rows_checks.cuh"
 
@@ -135,11 +137,8 @@ int abs_rms_norm(const abs_rms_norm_args* a, abs_stream_t stream) {
 
 size_t abs_rms_norm_grad_bytes(int64_t n0, int64_t n1, int64_t h, int64_t n_samples) {
   if (check_shape(n0, n1, h) != ABS_OK || n_samples < 0 || n_samples > ABS_MAX_SAMPLES) return 0;
-  int64_t blocks = 0;  // the most that a call of this shape takes: its tensors' alignment decides
-  for (int vec : {8, 4, 1}) {
-    const int64_t n = grad_blocks(n0 * n1, h, vec);
-    if (n > blocks) blocks = n;
-  }
+  int64_t blocks = 0;  // the most that a call may take: its tensors' alignment decides; at most one for each row
+  for (int vec : {8, 4, 1}) blocks = std::max(blocks, std::min(n0 * n1, grad_most_blocks(h, vec)));
   // one record a block, and with a table one for each sample and one more for each block
   return static_cast<size_t>(blocks + (n_samples ? blocks + n_samples : 0) + 1) * record_pitch(h) * sizeof(float);
 }

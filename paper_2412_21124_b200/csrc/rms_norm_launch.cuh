@@ -59,9 +59,11 @@ constexpr int kGradHalf = 2048;
 constexpr int grad_lane_values(int vec) { return vec == 8 ? 256 : 128; }
 // Blocks of the kernel that sums over rows: as many as fit the SMs at once, but two rows a block at least, since every
 // block leaves a record: 512 x 2048 with 8 samples 15 us by 512 blocks, 11 by 256, 13 by 128, and 512 x 768 8.9, 7.8, 8.8.
+inline int64_t grad_most_blocks(int64_t h, int vec) {
+  return kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec, h <= kGradHalf) : 1);
+}
 inline int64_t grad_blocks(int64_t rows, int64_t h, int vec) {
-  const int64_t most = kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec, h <= kGradHalf) : 1);
-  const int64_t pairs = (rows + 1) / 2;
+  const int64_t most = grad_most_blocks(h, vec), pairs = (rows + 1) / 2;
   return pairs < most ? pairs : most;
 }
 inline int64_t record_pitch(int64_t h) { return (h + 7) / 8 * 8; }  // VEC 8 writes 32 bytes at once
