@@ -67,11 +67,6 @@ __device__ __forceinline__ float load_teacher(const DistillParams& p, uint32_t r
   return p.t_dtype == ABS_BF16 ? from_half_word<ABS_BF16>(w) : from_half_word<ABS_F16>(w);
 }
 template <int DT>
-__device__ __forceinline__ float load_one(const unsigned char* row, int i) {
-  if constexpr (DT == ABS_F32) return reinterpret_cast<const float*>(row)[i];
-  return from_half_word<DT>(reinterpret_cast<const unsigned short*>(row)[i]);
-}
-template <int DT>
 __device__ __forceinline__ void store_one(unsigned char* row, int i, float v) {
   if constexpr (DT == ABS_F32) reinterpret_cast<float*>(row)[i] = v;
   else if constexpr (DT == ABS_BF16) reinterpret_cast<__nv_bfloat16*>(row)[i] = __float2bfloat16_rn(v);
@@ -140,7 +135,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
   // the teacher's entries, one a thread
   const int id = tid < p.top ? load_id(p, row, tid) : -1;
   const float t = id >= 0 ? load_teacher(p, row, tid) : -INFINITY;
-  const float zt = id >= 0 ? load_one<DT>(z, id) : -INFINITY;
+  const float zt = id >= 0 ? load_value<DT>(z, id) : -INFINITY;
   for (int i = tid; i < (p.vocab + 31) / 32; i += kDistillThreads) in_top[i] = 0u;
   sh_id[tid] = id;
   const ExpSum own{fmaxf(t, kLowest), 0.f};  // a NaN stays in the sum, not in the reference

@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
           const RingTop top = top_of(stage);
           const int at = top.place[tid];
           if (static_cast<unsigned>(at) < static_cast<unsigned>(r.units * U)) {
-            top.z[tid] = load_one<DT>(stage, at);
+            top.z[tid] = load_value<DT>(stage, at);
             store_one<DT>(stage, at, -INFINITY);
           }
         }
@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
 #pragma unroll 1
           for (int u = tid; u < mine; u += THREADS)
 #pragma unroll 1
-            for (int j = 0; j < U; ++j) sum += ex.of_far(load_one<DT>(stage, u * U + j));
+            for (int j = 0; j < U; ++j) sum += ex.of_far(load_value<DT>(stage, u * U + j));
         }
         sum = lanes_sum<32>(dead ? nan : sum);
         if (lane == 0) from_warps[n & 1][warp] = {m, sum};
@@ -668,7 +668,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
 #pragma unroll 1
               for (int k = u * U; k < u * U + U; ++k)
                 if (i_before + k >= 0 && i_before + k < p.vocab)
-                  store_one<DT>(dz_before, k, f * ex.of_far(load_one<DT>(stage_before, k)));
+                  store_one<DT>(dz_before, k, f * ex.of_far(load_value<DT>(stage_before, k)));
           }
         }
         // the stage has been read: the copy of a later row may overwrite it

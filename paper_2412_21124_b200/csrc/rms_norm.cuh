@@ -3,14 +3,13 @@
 //
 //   s = x + residual,   rstd = (sum_c s_c^2 / h + eps)^(-1/2),   y_c = s_c rstd w_c
 //
-// One pass: a row is loaded once into registers (a piece of 4 or 8 values a thread, more where the row would take
-// over 1024 threads), its squares are summed over the threads that hold it, and y, the rounded s and the
-// scales are written from the same registers.  s is not rounded before it is normalised.
+// One pass: a row is loaded once into registers (8 to 32 values a thread), its squares are summed over the threads
+// that hold it, and y, the rounded s and the scales are written from the same registers.  s is not rounded before
+// it is normalised.
 //
-// Bounds: HBM where the output has 16 or 32 bits, 16384 x 2048 with an fp32 residual stream 62 us, 6.4 TB/s.  In
-// 8 bits with a scale for 32 values it is instruction issue, some 40 of a warp for each value of a lane (8192 x 8192
-// 104 us, 4.5 TB/s); 524288 heads of 64 take 26 us, 5.2 TB/s.  Two values in one instruction slot brought nothing:
-// what they save goes into moving registers side by side.
+// Bounds: HBM where the output has 16 or 32 bits, 16384 x 2048 with an fp32 residual stream 61 us, 6.6 TB/s;
+// 524288 heads of 64 23.5 us, 5.7 TB/s.  In 8 bits with a scale for 32 values it is instruction issue (8192 x 8192 91 us,
+// 5.2 TB/s).  Two values in one instruction slot brought nothing: what they save goes into moving registers side by side.
 #pragma once
 #include "rows.cuh"
 
@@ -76,7 +75,7 @@ __device__ __forceinline__ float squares(const float (&s)[NI][E]) {
 // BLOCK: a row a block, in NI pieces a thread.  Otherwise L lanes hold a row in NI pieces, NR rows of a group of
 // lanes at once; blockDim.y warps a block.
 template <int XT, int RT, int VEC, int L, int NI, int NR, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 256)
+__global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 1024) : 256, BLOCK ? 1 : NI > 2 ? 3 : 4)
     rms_norm_kernel(const NormParams p) {
   constexpr int E = lane_values<VEC>();
   constexpr bool HAS_R = RT >= 0;
@@ -252,40 +251,53 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256)
       for (int i = 0; i < NI; ++i)
 #pragma unroll
         for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+    } else if constexpr (VEC == 1) {
+      // a group is 1, 2 or 4 of the four values of every lane; the scale of value v's group is worked out by lane v
+      static_assert(NI * E <= 32, "a lane for every value");
+      uint32_t a = 0u;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(s[k][i][j]) & 0x7fffffffu);
+          if (lane == i * E + j) a = top;
+        }
+      if (p.group >= 64) a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+      if (p.group >= 128) a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+      const int c = ((lane / E) * warps + warp) * (L * E) + 32 * (lane % E);
+      const float inv = scale_from(a, lane < NI * E && c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * __shfl_sync(0xffffffffu, inv, i * E + j);
     } else {
+      uint32_t a[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int first = (i * warps + warp) * (L * E);
-        if constexpr (VEC == 1) {  // a group is 1, 2 or 4 of the four values of every lane
-          uint32_t a[E];
+        float top = 0.f;
 #pragma unroll
-          for (int j = 0; j < E; ++j) a[j] = __reduce_max_sync(0xffffffffu, __float_as_uint(s[k][i][j]) & 0x7fffffffu);
-          if (p.group >= 64) {
-            a[0] = a[1] = max(a[0], a[1]);
-            a[2] = a[3] = max(a[2], a[3]);
-          }
-          if (p.group >= 128) a[0] = a[1] = a[2] = a[3] = max(a[0], a[2]);
+        for (int j = 0; j < E; ++j) top = larger(top, s[k][i][j]);
+        // the lanes of a group: 32 / VEC, twice or four times as many
+        a[i] = __float_as_uint(top);
 #pragma unroll
-          for (int j = 0; j < E; ++j) {
-            const int c = first + 32 * j;
-            const float inv = scale_from(a[j], l == 0 && c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
-            s[k][i][j] = s[k][i][j] * rstd[k] * inv;
-          }
-        } else {
-          float top = 0.f;
+        for (int d = 1; d < 32 / VEC; d <<= 1) a[i] = max(a[i], __shfl_xor_sync(0xffffffffu, a[i], d));
+        if (p.group >= 64) a[i] = max(a[i], __shfl_xor_sync(0xffffffffu, a[i], 32 / VEC));
+        if (p.group >= 128) a[i] = max(a[i], __shfl_xor_sync(0xffffffffu, a[i], 64 / VEC));
+      }
+      // of four lanes, which are always of one group, each works out the scale of another piece
+      static_assert(NI <= 4 && 32 / VEC >= 4, "a lane for every piece");
+      const int i_mine = NI > 1 ? l & 3 : 0;
+      uint32_t a_mine = a[0];
 #pragma unroll
-          for (int j = 0; j < E; ++j) top = larger(top, s[k][i][j]);
-          // the lanes of a group: 32 / VEC, twice or four times as many
-          uint32_t a = __float_as_uint(top);
+      for (int i = 1; i < NI; ++i)
+        if (i_mine == i) a_mine = a[i];
+      const int c = (i_mine * warps + warp) * (L * E) + (l - i_mine) * VEC;
+      const float inv_mine = scale_from(a_mine, i_mine < NI && c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
 #pragma unroll
-          for (int d = 1; d < 32 / VEC; d <<= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, d));
-          if (p.group >= 64) a = max(a, __shfl_xor_sync(0xffffffffu, a, 32 / VEC));
-          if (p.group >= 128) a = max(a, __shfl_xor_sync(0xffffffffu, a, 64 / VEC));
-          const int c = first + l * VEC;
-          const float inv = scale_from(a, c < p.h && (c & (p.group - 1)) == 0, c >> p.group_shift);
+      for (int i = 0; i < NI; ++i) {
+        const float inv = NI > 1 ? __shfl_sync(0xffffffffu, inv_mine, (lane & ~3) | i) : inv_mine;
 #pragma unroll
-          for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
-        }
+        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
       }
     }
     if (live) {

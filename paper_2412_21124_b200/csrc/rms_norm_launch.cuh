@@ -21,27 +21,38 @@ cudaError_t norm_by_block(const NormParams& p, cudaStream_t st) {
   constexpr int cols = 32 * lane_values<VEC>() * NI;  // of a warp
   return launch_pdl(rms_norm_kernel<XT, RT, VEC, 32, NI, 1, true>, dim3(p.rows), dim3(32 * ((p.h + cols - 1) / cols)), st, p);
 }
-// As many threads a row as it has pieces, up to 1024: 32 registers a thread and so 2048 threads on an SM, whatever the width.
-// Two pieces a thread 65 us instead of 62 (16384 x 2048, bf16 and fp32) and 124 instead of 104 (8192 x 8192 into
-// 8 bits), four 68 and 133.  Narrow rows share a warp, four of a lane's at once: 26 us for 524288 rows of 64, one at a
-// time 36.
+// Rows of a warp or less go to its lanes, several rows of a lane at once: 100000 x 255 in 16 bits 32 us, by a block a row 54;
+// 80000 x 512 39 and 58; 40000 x 1024 29 and 33 (fp32, 51 and 50: by blocks).  Heads of 64, 524288 of them: 24 us
+// with four rows at once, 36 with one.  Wider ones take a block, whose threads hold eight or sixteen values: more threads
+// a row cost more in their meeting than they bring in loads (8192 x 8192 into 8 bits 101 us with 8 values a thread, 94
+// with 16; 20000 x 2048 36 and 30), and from 4096 on 32 of them (91).  In smaller pieces: 40000 x 1028 61 us with 4
+// values a thread, 44 with 8 and with 16; 10000 x 4100 48 with 8, 41 with 16.
 template <int XT, int RT>
 cudaError_t norm_vec(const NormParams& p, int vec, cudaStream_t st) {
   const int h = p.h;
   if (vec == 8) {
     if (h <= 64) return norm_by_lanes<XT, RT, 8, 8, 1, 4>(p, st);
     if (h <= 128) return norm_by_lanes<XT, RT, 8, 16, 1, 4>(p, st);
-    if (h <= 256) return norm_by_lanes<XT, RT, 8, 32, 1, 2>(p, st);
-    if (h <= 8192) return norm_by_block<XT, RT, 8, 1>(p, st);
-    return norm_by_block<XT, RT, 8, 2>(p, st);
+    if (h <= 256) return norm_by_lanes<XT, RT, 8, 32, 1, 4>(p, st);
+    if (h <= 512) return norm_by_lanes<XT, RT, 8, 32, 2, 2>(p, st);
+    if constexpr (XT != ABS_F32) {
+      if (h <= 768) return norm_by_lanes<XT, RT, 8, 32, 3, 1>(p, st);
+      if (h <= 1024) return norm_by_lanes<XT, RT, 8, 32, 4, 1>(p, st);
+    }
+    if (h <= 4096) return norm_by_block<XT, RT, 8, 2>(p, st);
+    return norm_by_block<XT, RT, 8, 4>(p, st);
   }
   if (vec == 4) {
     if (h <= 128) return norm_by_lanes<XT, RT, 4, 32, 1, 4>(p, st);
-    if (h <= 4096) return norm_by_block<XT, RT, 4, 1>(p, st);
+    if (h <= 256) return norm_by_lanes<XT, RT, 4, 32, 2, 4>(p, st);
+    if (h <= 512) return norm_by_lanes<XT, RT, 4, 32, 4, 2>(p, st);
+    if (h <= 1536) return norm_by_block<XT, RT, 4, 2>(p, st);
     return norm_by_block<XT, RT, 4, 4>(p, st);
   }
   if (h <= 128) return norm_by_lanes<XT, RT, 1, 32, 1, 4>(p, st);
-  if (h <= 4096) return norm_by_block<XT, RT, 1, 1>(p, st);
+  if (h <= 256) return norm_by_lanes<XT, RT, 1, 32, 2, 2>(p, st);
+  if (h <= 512) return norm_by_lanes<XT, RT, 1, 32, 4, 1>(p, st);
+  if (h <= 1536) return norm_by_block<XT, RT, 1, 2>(p, st);
   return norm_by_block<XT, RT, 1, 4>(p, st);
 }
 // r_dtype < 0: no residual
