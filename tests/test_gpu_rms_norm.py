@@ -117,6 +117,27 @@ def test_norm_in_eight_bits(width, out, group):
         assert torch.equal(turned.float(), scales.float()) and torch.equal(again.float(), q.float())
 
 
+@pytest.mark.parametrize("width", (129, 132, 252, 255, 257, 385, 508, 511, 516, 520, 576, 700, 776, 1025, 1535, 1536, 1540, 4096, 4104))
+def test_rows_where_the_work_is_dealt_out_another_way(width):
+    """Both sides of the widths at which rows go from lanes to blocks and from few values a thread to more."""
+    g = gen(width)
+    for dtype, rows in ((BF16, 131), (F32, 70), (F16, 1)):
+        x, r = rand((rows, width), dtype, g, 0.7), rand((rows, width), F32, g, 2.0)
+        w = (1 + 0.2 * torch.randn(width, device=DEV, generator=g)).to(dtype)
+        out, s_out = torch.empty_like(x), torch.empty_like(r)
+        absnt.abs_rms_norm(x, w, out, EPS)
+        near(out, plain(x, w)[1], dtype)
+        absnt.abs_rms_norm(x, w, out, EPS, residual=r, sum_out=s_out)
+        s, y = plain(x, w, r)
+        near(out, y, dtype)
+        near(s_out, s, F32, E)
+        for group in (0, 32, 64, 128):
+            q = torch.empty(rows, width, device=DEV, dtype=E4M3)
+            scales = torch.empty(rows, -(-width // group) if group else 1, device=DEV)
+            absnt.abs_rms_norm(x, w, q, EPS, residual=r, scales_out=scales, group=group)
+            near_scaled(q, scales, y, group)
+
+
 @pytest.mark.parametrize("width", (64, 80, 100, 128, 99))
 @pytest.mark.parametrize("dtype", (F32, BF16, F16))
 def test_heads_of_a_fused_projection(width, dtype):
