@@ -8,8 +8,8 @@
 // it is normalised.
 //
 // Bounds: HBM where the output has 16 or 32 bits, 16384 x 2048 with an fp32 residual stream 61 us, 6.6 TB/s;
-// 524288 heads of 64 23.5 us, 5.7 TB/s.  In 8 bits with a scale for 32 values it is instruction issue (8192 x 8192 91 us,
-// 5.2 TB/s).  Two values in one instruction slot brought nothing: what they save goes into moving registers side by side.
+// 524288 heads of 64 24 us, 5.6 TB/s.  In 8 bits with a scale for 32 values it is instruction issue (8192 x 8192 92 us,
+// 5.1 TB/s).  Two values in one instruction slot brought nothing: what they save goes into moving registers side by side.
 #pragma once
 #include "rows.cuh"
 
@@ -55,6 +55,14 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t a, int out_dtype, int scal
 __device__ __forceinline__ void store_scale(unsigned char* scales, int64_t at, int scale_dtype, uint32_t stored) {
   if (scale_dtype == ABS_F32) reinterpret_cast<uint32_t*>(scales)[at] = stored;
   else scales[at] = static_cast<unsigned char>(stored);
+}
+
+// v^(-1/2) with one step of Newton's method behind the approximation, whose 2 units in the last place would decide more often
+// than the other roundings on which side of a power of two, or of a tie of 8-bit values, a result falls
+__device__ __forceinline__ float inverse_root(float v) {
+  const float r = rsqrtf(v), t = v * r;
+  const float e = fmaf(-fmaf(v, r, -t), r, fmaf(-t, r, 1.f));
+  return fabsf(e) < 1.f ? fmaf(0.5f * r, e, r) : r;  // as it is for an infinity and a NaN
 }
 
 // max(a, |b|), NaN if one is: a's sign is clear
@@ -156,7 +164,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
   }
   float rstd[NR];
 #pragma unroll
-  for (int k = 0; k < NR; ++k) rstd[k] = rsqrtf(fmaf(ss[k], p.inv_h, p.eps));
+  for (int k = 0; k < NR; ++k) rstd[k] = inverse_root(fmaf(ss[k], p.inv_h, p.eps));
   if (again) {
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
         __syncthreads();
         t = lanes_sum<32>(lane < warps ? part_again[lane] : 0.f);
       }
-      if (down) rstd[k] = rsqrtf(t * p.inv_h);
+      if (down) rstd[k] = inverse_root(t * p.inv_h);
     }
   }
 
