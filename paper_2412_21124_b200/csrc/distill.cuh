@@ -189,12 +189,13 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
   if (p.lse && sum_p != sum_p) p_rest = sum_p;  // NaN
   if (rest.s == 0.f) p_rest = 0.f;              // nothing can be given to what is not in the top
   const float log_s = log2f(all.s);
-  // tau^2 ln(p / q), the distance of z from the reference without the factor c, which a masking value might not bear
-  const float mine = some && pj != 0.f ? pj * (p.loss_scale * (log_p + log_s) + p.tau * (all.m - zt)) : 0.f;
+  // p tau^2 ln(p / q), the distance of z from the reference without the factor c and times p first: a masking value might not
+  // bear c or tau alone
+  const float mine = some && pj != 0.f ? pj * p.loss_scale * (log_p + log_s) + pj * p.tau * (all.m - zt) : 0.f;
   float loss = block_sum(mine, room_l);
   if (tid == 0) {
     if (p_rest != 0.f)
-      loss += p_rest * (p.loss_scale * (log2f(p_rest) - log2f(rest.s) + log_s) + p.tau * (all.m - rest.m));
+      loss += p_rest * p.loss_scale * (log2f(p_rest) - log2f(rest.s) + log_s) + p_rest * p.tau * (all.m - rest.m);
     p.losses[row] = loss;
   }
   if (!dz) return;

@@ -46,7 +46,8 @@ struct RingParams {
 enum { kRowAlone = 0, kRowNoWeight = 1, kRowWork = 2 };
 
 // what a block knows of a row after pass 1: the rest's sum, the top's, and of the block's entries of the top the sum
-// of p (tau^2 ln p - tau (z - m)) with m the top's reference, and the sum of p
+// of p (tau^2 ln p - tau (z - m)) with m the top's reference, and the sum of p.  Distances of logits are multiplied by a
+// probability first: times tau alone that of a masking value may not be a float
 struct RingSums {
   ExpSum rest, top;
   float cross, p;
@@ -436,7 +437,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
               }
           if (first) sum += exp2_fast((z - m) * p.c);
           sum_p += pj;
-          if (pj != 0.f) cross += pj * (p.loss_scale * top.log_p[j] - p.tau * (z - m));
+          if (pj != 0.f) cross += pj * p.loss_scale * top.log_p[j] - pj * p.tau * (z - m);
           top.z[j] = z;
           top.log_p[j] = p_all;
         }
@@ -471,7 +472,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
         x = lane < r.blocks ? from_blocks[half][lane] : RingSums{{kLowest, 0.f}, {kLowest, 0.f}, 0.f, 0.f, {}};
         const float m_rest = warp_max(x.rest.m), m_top = warp_max(x.top.m);
         x.rest.s *= exp2_fast((x.rest.m - m_rest) * p.c);
-        if (x.p != 0.f) x.cross += p.tau * (m_top - x.top.m) * x.p;
+        if (x.p != 0.f) x.cross += x.p * p.tau * (m_top - x.top.m);
         x.top.s *= exp2_fast((x.top.m - m_top) * p.c);
         static_assert(kRingMaxCluster == 8, "sums over the first eight lanes");
 #pragma unroll
@@ -499,9 +500,9 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       if (rank == 0 && lane == 0) {
         const float log_s = log2f(all.s);
         float loss = x.cross + p.loss_scale * log_s * x.p;
-        if (x.p != 0.f) loss += p.tau * (all.m - x.top.m) * x.p;
+        if (x.p != 0.f) loss += x.p * p.tau * (all.m - x.top.m);
         if (p_rest != 0.f)
-          loss += p_rest * (p.loss_scale * (log2f(p_rest) - log2f(x.rest.s) + log_s) + p.tau * (all.m - x.rest.m));
+          loss += p_rest * p.loss_scale * (log2f(p_rest) - log2f(x.rest.s) + log_s) + p_rest * p.tau * (all.m - x.rest.m);
         p.losses[row] = loss;
       }
       __syncwarp();
