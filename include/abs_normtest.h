@@ -706,8 +706,9 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* args, abs_stream_t stream);
  *                         weight * grad_scale * loss
  *
  *   logits         rows x vocab, ABS_F32, ABS_BF16 or ABS_F16 (stride0 from row to row); vocab at most
- *                  ABS_MAX_VOCAB (ABS_ERR_TOO_LARGE).  -inf masks an index, and so does the type's lowest value, but
- *                  not as the whole rest of a row whose p_r is positive: the loss then says how far away it is
+ *                  ABS_MAX_VOCAB (ABS_ERR_TOO_LARGE).  -inf masks an index, and so does a finite value far below the
+ *                  others (-1e9, the type's lowest), but not as the whole rest of a row whose p_r is positive: the
+ *                  loss then says how far away it is
  *   top_ids        device, rows x top indices of id_bytes 4 or 8 (signed), ids_stride from row to row; top is
  *                  1..ABS_MAX_TOP.  An entry whose index is not one of 0..vocab-1 (-1, say) is left out; an index
  *                  that a row names twice has both probabilities

@@ -131,23 +131,24 @@ __device__ __forceinline__ float value_of(const uint32_t (&w)[4], int j) {
 }
 
 // 2^((z - m) c) as 2^(z c - r) with r the rounded m c: one fma and one exponential.  What the rounding of r costs is
-// the same factor for all values, 2^(m c - r), and is taken back once, in `correction`.  Where m c may not be a float
-// (m a masking value, or as large) values differ by so much that only those that equal m count; an infinite m and a NaN
-// among the values give NaN.
+// the same factor for all values, 2^(m c - r), and is taken back once, in `correction`.  From |m c| = 2^24 on (a masking
+// value, say) the exponent m c - r could exceed 1/2, and where |m c| is larger still the range of a float: there the
+// difference z - m is formed first, exactly where it counts.  An infinite m and a NaN among the values give NaN.
 struct Exponentials {
   float m, c, minus_r, correction;
   bool far;
   __device__ __forceinline__ Exponentials(float m_, float c_) : m(m_), c(c_) {
-    far = !(fabsf(m) < 1e36f);
     minus_r = -(m * c);
+    far = !(fabsf(minus_r) < 0x1p24f);
     correction = far ? 1.f : exp2_fast(-fmaf(m, c, minus_r));
   }
   __device__ __forceinline__ uint64_t operator()(float a, float b) const {
     const float2 x = pair_as(pair_fma(pair_of(a, b), pair_of(c, c), pair_of(minus_r, minus_r)));
     return pair_of(exp2_fast(x.x), exp2_fast(x.y));
   }
-  __device__ __forceinline__ float of_far(float z) const {
-    return z == m ? 1.f + (m - m) : z < m ? 0.f : __uint_as_float(0x7fffffffu);
+  __device__ __forceinline__ uint64_t of_far(float a, float b) const {
+    const float2 x = pair_as(pair_mul(pair_add(pair_of(a, b), pair_of(-m, -m)), pair_of(c, c)));
+    return pair_of(exp2_fast(x.x), exp2_fast(x.y));
   }
 };
 // the larger of two words of values, place by place
@@ -592,25 +593,21 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
         const float m = warp_max(fmaxf(max_of_word<DT>(top), kLowest));
         const Exponentials ex(m, p.c);
         uint64_t pairs = pair_of(0.f, 0.f);
-        float sum = 0.f;
-        if (!ex.far) {
+        auto sum_of = [&](auto exponentials) {
           for_units<THREADS>(0, mine, stage, none, [&](int, const uint32_t (&w)[4], bool) {
             uint64_t e[U / 2];
 #pragma unroll
-            for (int j = 0; j < U; j += 2) e[j / 2] = ex(value_of<DT>(w, j), value_of<DT>(w, j + 1));
+            for (int j = 0; j < U; j += 2) e[j / 2] = exponentials(value_of<DT>(w, j), value_of<DT>(w, j + 1));
 #pragma unroll
             for (int d = U / 4; d > 0; d /= 2)
 #pragma unroll
               for (int j = 0; j < d; ++j) e[j] = pair_add(e[j], e[j + d]);
             pairs = pair_add(pairs, e[0]);
           });
-          sum = (pair_as(pairs).x + pair_as(pairs).y) * ex.correction;
-        } else {
-#pragma unroll 1
-          for (int u = tid; u < mine; u += THREADS)
-#pragma unroll 1
-            for (int j = 0; j < U; ++j) sum += ex.of_far(load_value<DT>(stage, u * U + j));
-        }
+        };
+        if (!ex.far) sum_of([&](float a, float b) { return ex(a, b); });
+        else sum_of([&](float a, float b) { return ex.of_far(a, b); });
+        float sum = (pair_as(pairs).x + pair_as(pairs).y) * ex.correction;
         sum = lanes_sum<32>(dead ? nan : sum);
         if (lane == 0) from_warps[n & 1][warp] = {m, sum};
         part_arrive<THREADS + 64>(kSummed + (n & 1));
@@ -636,12 +633,12 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
           // the units that lie in the row whole, then its first and last by a thread each
           const int from = i_before < 0 ? 1 : 0;
           const int to = i_before + mine_before * U > p.vocab ? mine_before - 1 : mine_before;
-          if (!ex.far) {
-            const uint64_t ff = pair_of(f, f);
+          const uint64_t ff = pair_of(f, f);
+          auto write = [&](auto exponentials) {
             auto unit = [&](const uint32_t (&w)[4], uint32_t (&out)[4]) {
 #pragma unroll
               for (int j = 0; j < U; j += 2) {
-                const float2 d = pair_as(pair_mul(ex(value_of<DT>(w, j), value_of<DT>(w, j + 1)), ff));
+                const float2 d = pair_as(pair_mul(exponentials(value_of<DT>(w, j), value_of<DT>(w, j + 1)), ff));
                 if constexpr (DT == ABS_F32) {
                   out[j] = __float_as_uint(d.x);
                   out[j + 1] = __float_as_uint(d.y);
@@ -663,14 +660,9 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
               unit(w, out);
               write_unit<DT>(dz_before + u * 16, i_before + u * U, p.vocab, out);
             }
-          } else {
-#pragma unroll 1
-            for (int u = tid; u < mine_before; u += THREADS)
-#pragma unroll 1
-              for (int k = u * U; k < u * U + U; ++k)
-                if (i_before + k >= 0 && i_before + k < p.vocab)
-                  store_one<DT>(dz_before, k, f * ex.of_far(load_value<DT>(stage_before, k)));
-          }
+          };
+          if (!ex.far) write([&](float a, float b) { return ex(a, b); });
+          else write([&](float a, float b) { return ex.of_far(a, b); });
         }
         // the stage has been read: the copy of a later row may overwrite it
         fence_generic_to_async_smem();
