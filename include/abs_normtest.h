@@ -756,6 +756,14 @@ int abs_distill_loss(const abs_distill_args* args, abs_stream_t stream);
  */
 int abs_selftest_bounded_wait(int polls, int64_t* out, abs_stream_t stream);
 
+/*
+ * The same for abs_distill_loss: that call, in which the part that loads rows gives up after `polls` polls (0 .. 2^18)
+ * of a place that is still in use; with 0 it does so as soon as it needs a place again.  Whoever waits for its rows then gives
+ * up too, after about two seconds, and those rows' losses and gradients are NaN; all others are what they
+ * should be.  Calls that take the kernel of a block a row have no such wait.
+ */
+int abs_selftest_distill_wait(const abs_distill_args* args, int polls, abs_stream_t stream);
+
 const char* abs_status_string(int status);
 
 /* The cudaError_t of the most recent ABS_ERR_CUDA on this thread (0 if none). */

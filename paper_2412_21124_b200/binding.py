@@ -146,6 +146,8 @@ def lib():
     L.abs_rms_norm_grad_bytes.argtypes = [i64, i64, i64, i64]
     L.abs_distill_loss.restype = cint
     L.abs_distill_loss.argtypes = [ptr, ptr]
+    L.abs_selftest_distill_wait.restype = cint
+    L.abs_selftest_distill_wait.argtypes = [ptr, cint, ptr]
     L.abs_selftest_bounded_wait.restype = cint
     L.abs_selftest_bounded_wait.argtypes = [cint, ptr, ptr]
     L.abs_status_string.restype = ctypes.c_char_p

@@ -26,6 +26,7 @@ struct DistillParams {
   uint32_t rows;
   int n_samples;
   int vocab, top, t_dtype, id_bytes;
+  int empty_polls;         // of the ring's feeder at a stage that has not been given back: kBulkWaitLimit but for its self-test
   double inv_tau;
   float c;                 // log2(e) / tau
   float tau;

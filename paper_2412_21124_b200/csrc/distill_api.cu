@@ -40,7 +40,9 @@ int ring_clusters(const void* kernel, const cudaLaunchConfig_t& cfg) {
 
 }  // namespace absnt
 
-extern "C" int abs_distill_loss(const abs_distill_args* a, abs_stream_t stream) {
+namespace {
+
+int distill_loss(const abs_distill_args* a, int empty_polls, abs_stream_t stream) {
   if (!a) return ABS_ERR_NULL;
   const bool table = a->offsets != nullptr;
   if (a->rows < 0 || a->rows > INT32_MAX || a->vocab < 1 || a->top < 1 || a->top > ABS_MAX_TOP) return ABS_ERR_RANGE;
@@ -115,6 +117,7 @@ extern "C" int abs_distill_loss(const abs_distill_args* a, abs_stream_t stream) 
     p.top = static_cast<int>(a->top);
     p.t_dtype = t.dtype;
     p.id_bytes = a->id_bytes;
+    p.empty_polls = empty_polls;
     constexpr double kLog2e = 1.4426950408889634;
     p.c = static_cast<float>(kLog2e / a->temperature);
     p.inv_tau = 1.0 / a->temperature;
@@ -133,3 +136,16 @@ extern "C" int abs_distill_loss(const abs_distill_args* a, abs_stream_t stream) 
   const cudaError_t e = launch_pdl(distill_samples_kernel, dim3(static_cast<unsigned>(samples)), dim3(kSampleLossThreads), st, s);
   return e == cudaSuccess ? ABS_OK : cuda_fail(e);
 }
+
+}  // namespace
+
+extern "C" {
+
+int abs_distill_loss(const abs_distill_args* a, abs_stream_t stream) { return distill_loss(a, kBulkWaitLimit, stream); }
+
+int abs_selftest_distill_wait(const abs_distill_args* a, int polls, abs_stream_t stream) {
+  if (polls < 0 || polls > kBulkWaitLimit) return ABS_ERR_RANGE;
+  return distill_loss(a, polls, stream);
+}
+
+}  // extern "C"

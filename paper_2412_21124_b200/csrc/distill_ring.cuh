@@ -21,8 +21,12 @@
 // time, with and without the gradient; what is reached is 0.6 to 0.7 of the bandwidth, and the same without the loads or
 // without the stores: issue slots are half taken, the exponential unit a little less, and the rest is the chain of a
 // row (largest, sum, join, answer) that two rows under way do not cover.  bf16 with the gradient: 8192 rows of 128256,
-// a fifth of them without weight, 841 us, 4096 of 50257 218 us; f16, loss alone: 8192 of 32000 128 us.  Every wait is
-// bounded (see normtest_bulk.cuh); one that runs out makes its row NaN.
+// a fifth of them without weight, 841 us, 4096 of 50257 218 us; f16, loss alone: 8192 of 32000 127 us.
+//
+// Every wait is bounded (see normtest_bulk.cuh).  A part whose wait runs out says nothing further to any mbarrier: a phase that
+// is still open must not be entered twice.  A feeder or a joiner stops there, so that the waits of those that it
+// would have served run out as well; workers go on without waiting and make NaN of what they sum.  So the row whose
+// data did not come, and the rows behind it in the cluster, are NaN.
 #pragma once
 #include "distill.cuh"
 #include "normtest_bulk.cuh"
@@ -332,8 +336,12 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       const Ahead next = look_ahead();
       const uint32_t row = static_cast<uint32_t>(now.row);
       const int s = ring_n.s;
-      if (ring_n.turn > 0 && !dead) dead = !mbar_wait_bounded(&empty[s], (ring_n.turn - 1) & 1);
-      __syncwarp();
+      if (ring_n.turn > 0) {
+        // given back by the workers; and its last copy has landed, also where they gave up on it
+        const uint32_t before = (ring_n.turn - 1) & 1;
+        const bool free = mbar_wait_bounded(&empty[s], before, p.empty_polls) && mbar_wait_bounded(&full[s], before);
+        if (__any_sync(0xffffffffu, !free)) break;
+      }
       unsigned char* const stage = stage_of(ring_n);
       // the units of this block; the first and last of the row may reach out of the tensor at its ends
       const unsigned char* z = row_of(p.z, row, 0);
@@ -344,7 +352,7 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       if (a == 0 && from < r.z_begin) a = 1;
       if (e == n_units && from + static_cast<int64_t>(e) * 16 > r.z_end) --e;
       if (lane == 0) {
-        if (e > a && !dead) {
+        if (e > a) {
           const uint32_t bytes = static_cast<uint32_t>(e - a) * 16u;
           mbar_expect_tx(&full[s], bytes);
           bulk_load(stage + (a - first_unit) * 16, from + static_cast<int64_t>(a) * 16, bytes, &full[s]);
@@ -465,11 +473,13 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       x.rest = warp_join(lane < kWarps ? from_warps[half][lane] : ExpSum{kLowest, 0.f}, p.c);
       if (dead) x.rest.s = nan;
       if (r.blocks > 1) {
-        if (lane == 0) mbar_expect_tx(&sums_here[half], r.blocks * 32u);
-        __syncwarp();
-        if (lane < r.blocks) send_sums(x, &from_blocks[half][rank], &sums_here[half], lane);
-        if (!dead) dead = !mbar_wait_bounded(&sums_here[half], (n >> 1) & 1);
-        __syncwarp();
+        if (!dead) {
+          if (lane == 0) mbar_expect_tx(&sums_here[half], r.blocks * 32u);
+          __syncwarp();
+          if (lane < r.blocks) send_sums(x, &from_blocks[half][rank], &sums_here[half], lane);
+          dead = !mbar_wait_bounded(&sums_here[half], (n >> 1) & 1);
+          dead = __any_sync(0xffffffffu, dead);
+        }
         x = lane < r.blocks ? from_blocks[half][lane] : RingSums{{kLowest, 0.f}, {kLowest, 0.f}, 0.f, 0.f, {}};
         const float m_rest = warp_max(x.rest.m), m_top = warp_max(x.top.m);
         x.rest.s *= exp2_fast((x.rest.m - m_rest) * p.c);

@@ -88,8 +88,8 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
   return ok != 0;
 }
 // bounded wait; returns false when the limit ran out
-__device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity) {
-  for (int polls = 0; polls < kBulkWaitLimit; ++polls)
+__device__ __forceinline__ bool mbar_wait_bounded(uint64_t* bar, uint32_t parity, int limit = kBulkWaitLimit) {
+  for (int polls = 0; polls < limit; ++polls)
     if (mbar_try_wait(bar, parity)) return true;
   return false;
 }

@@ -209,3 +209,11 @@ DZ = rows(far(2), s0=100)
 ])
 def test_distillation_checks(L, change, status):
     assert distill(L, **change) == status
+
+
+def test_the_self_test_of_its_waits_takes_the_same_arguments(L):
+    args = B._DISTILL_ARGS.pack(10, 100, 8, *rows(far(1), s0=100), *NONE, *rows(far(3), s0=8), far(4), 0, 0, 0, far(5), 0, 8, 0, 1.0,
+                                1.0, 8, 0)
+    for polls, status in ((-1, B.ABS_ERR_RANGE), (0, LET_THROUGH), (2 ** 18, LET_THROUGH), (2 ** 18 + 1, B.ABS_ERR_RANGE)):
+        assert L.abs_selftest_distill_wait(args, polls, None) == status
+    assert L.abs_selftest_distill_wait(None, 0, None) == B.ABS_ERR_NULL
