@@ -432,14 +432,15 @@ __global__ void __launch_bounds__(THREADS + 96, ring_blocks_per_sm(THREADS))
       for (int j = lane; j < p.top; j += 32)
         if (top.place[j] >= 0) {
           // Of the workers of one index named twice one at least has read its logit, others perhaps the -inf
-          // already.  The first entry stands for all of them.
+          // already.  The first entry stands for all of them in the sums; all of them write the gradient, so the
+          // probabilities are added in the same order for each.
           float z = top.z[j];
           const float pj = top.p[j];
-          float p_all = pj;
+          float p_all = repeated ? 0.f : pj;
           bool first = true;
           if (repeated)
             for (int k = 0; k < p.top; ++k)
-              if (k != j && top.place[k] == top.place[j]) {
+              if (top.place[k] == top.place[j]) {
                 if (k < j) first = false;
                 p_all += top.p[k];
                 if (top.z[k] != -INFINITY) z = top.z[k];
