@@ -31,6 +31,8 @@ struct NormParams {
 // rows (and those that hold an infinity or a NaN, which stay what they are) are summed again scaled.
 constexpr float kSquaresLimit = 1e36f;
 constexpr float kDown = 0x1p-80f;
+// eps beside squares of scaled values: the factor's square alone is no float
+__device__ __forceinline__ float down_squared(float eps) { return eps * kDown * kDown; }
 
 // The scale of a group whose largest |y| has the bits `a`, as it is stored (a float's bits, or the byte), and its
 // reciprocal.  Not finite: NaN, which makes all values of the group NaN.
@@ -179,7 +181,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
         __syncthreads();
         t = lanes_sum<32>(lane < warps ? part_again[lane] : 0.f);
       }
-      if (down) rstd[k] = inverse_root(t * p.inv_h);
+      if (down) rstd[k] = inverse_root(fmaf(t, p.inv_h, down_squared(p.eps)));
     }
   }
 

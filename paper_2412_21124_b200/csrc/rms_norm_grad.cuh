@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 256 ? grad_blocks_per_sm(B
             tg = lanes_sum<32>(lane < warps ? part_again[parity][32 + mine + lane] : 0.f);
           }
           if (scale[k] != 1.f) {
-            rstd[k] = rsqrtf(ts * p.inv_h);
+            rstd[k] = rsqrtf(fmaf(ts, p.inv_h, down_squared(p.eps)));
             sg[k] = tg;
           }
         }
