@@ -185,20 +185,26 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     }
   }
 
-  if (!p.scales) {
-    // y, piece by piece; the branches on the types are taken once for all of a thread's pieces
+  // y, piece by piece; the branches on the types are taken once for all of a thread's pieces.  (For outputs of 8 bits too: s w
+  // without rstd, or rstd and a scale's reciprocal as one factor, may leave the range of a float where y does not.)
+  auto normalise = [&]() {
     with_type(p.w_dtype, [&](auto wt) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int first = (i * warps + warp) * (L * E);
         float w[E];
-        load_weight_of<decltype(wt)::value, VEC>(w, p.w, first, l, p.h);
+        load_weight_of<decltype(wt)::value, VEC>(w, p.w, (i * warps + warp) * (L * E), l, p.h);
 #pragma unroll
         for (int k = 0; k < NR; ++k)
 #pragma unroll
           for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * w[j];
       }
     });
+  };
+  // before the branch on the output for rows of lanes (524288 heads of 64: 23.0 us, in either branch 23.7), in either branch for
+  // rows of blocks (8192 x 8192 into 8 bits: 92.6 us, before it 94.2)
+  if constexpr (!BLOCK) normalise();
+  if (!p.scales) {
+    if constexpr (BLOCK) normalise();
     with_type(p.out_dtype, [&](auto ot) {
 #pragma unroll
       for (int k = 0; k < NR; ++k)
@@ -211,22 +217,11 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     return;
   }
 
-  // 8 bits: the largest |s w| of a group times rstd is its largest |y|.  (rstd and the scale's reciprocal are not made one
-  // factor: it may overflow where their products with s w do not.)
+  // 8 bits: the largest |y| of each group
+  if constexpr (BLOCK) normalise();
   uint32_t a_row[NR];
 #pragma unroll
   for (int k = 0; k < NR; ++k) a_row[k] = 0u;
-  with_type(p.w_dtype, [&](auto wt) {
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      float w[E];
-      load_weight_of<decltype(wt)::value, VEC>(w, p.w, (i * warps + warp) * (L * E), l, p.h);
-#pragma unroll
-      for (int k = 0; k < NR; ++k)
-#pragma unroll
-        for (int j = 0; j < E; ++j) s[k][i][j] *= w[j];
-    }
-  });
   const bool of_row = p.group >= p.h;
   if (of_row) {
 #pragma unroll
@@ -250,7 +245,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     unsigned char* const po = row_of<VEC>(p.out, ri[k], rj[k]);
     auto scale_from = [&](uint32_t a, bool writer, int group) {
       float inv;
-      const uint32_t stored = scale_of(__float_as_uint(__uint_as_float(a) * rstd[k]) & 0x7fffffffu, p.out_dtype, p.scale_dtype, inv);
+      const uint32_t stored = scale_of(a, p.out_dtype, p.scale_dtype, inv);
       if (writer && live)
         store_scale(p.scales, ri[k] * p.scale_s0 + rj[k] * p.scale_s1 + group * p.scale_s2, p.scale_dtype, stored);
       return inv;
@@ -260,7 +255,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+        for (int j = 0; j < E; ++j) s[k][i][j] *= inv;
     } else if constexpr (VEC == 1) {
       // a group is 1, 2 or 4 of the four values of every lane; the scale of value v's group is worked out by lane v
       static_assert(NI * E <= 32, "a lane for every value");
@@ -279,7 +274,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
 #pragma unroll
       for (int i = 0; i < NI; ++i)
 #pragma unroll
-        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * __shfl_sync(0xffffffffu, inv, i * E + j);
+        for (int j = 0; j < E; ++j) s[k][i][j] *= __shfl_sync(0xffffffffu, inv, i * E + j);
     } else {
       uint32_t a[NI];
 #pragma unroll
@@ -307,7 +302,7 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
       for (int i = 0; i < NI; ++i) {
         const float inv = NI > 1 ? __shfl_sync(0xffffffffu, inv_mine, (lane & ~3) | i) : inv_mine;
 #pragma unroll
-        for (int j = 0; j < E; ++j) s[k][i][j] = s[k][i][j] * rstd[k] * inv;
+        for (int j = 0; j < E; ++j) s[k][i][j] *= inv;
       }
     }
     if (live) {
