@@ -671,8 +671,10 @@ int abs_rms_norm(const abs_rms_norm_args* args, abs_stream_t stream);
  *   work             device, abs_rms_norm_grad_bytes(...) bytes, 32-byte aligned, where one of the two sums is asked
  *                    for (ABS_ERR_TOO_LARGE if work_bytes is less).  Nothing in it outlives the call; calls that
  *                    may overlap need one each
- * Sums over rows are formed in fp32 in an order that depends on the shapes and offsets alone.  Where a sample
- * has no rows, and where there are no rows at all, sums are 0.  One launch, two with a sum.
+ * Sums over rows are formed in fp32 in an order that depends on shapes, types, strides, the addresses' alignment and the
+ * offsets: the same call on buffers laid out alike gives the same bits, a copy at another alignment may not.  The
+ * sum of a row's g_i s_i has to be a float (for rows whose squares are none, times 2^-80).  Where a sample has
+ * no rows, and where there are no rows at all, sums are 0.  One launch, two with a sum.
  */
 typedef struct {
   int64_t n0, n1, h;
@@ -703,7 +705,9 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* args, abs_stream_t stream);
  *                         of the top (it is the whole vocabulary, or the rest is -inf) p_r counts as 0
  *   dlogits_i             weight * grad_scale * tau * (q_i - p_i) in the top,
  *                         weight * grad_scale * tau * q_i (1 - p_r / q_r) elsewhere: the derivative of
- *                         weight * grad_scale * loss
+ *                         weight * grad_scale * loss as long as P = sum_j p_j + p_r is 1.  A teacher_lse that is too
+ *                         small makes P larger, and a rest that is empty (p_r counts as 0) may leave it smaller; dlogits_i
+ *                         then exceeds the derivative by weight * grad_scale * tau * q_i (1 - P)
  *
  *   logits         rows x vocab, ABS_F32, ABS_BF16 or ABS_F16 (stride0 from row to row); vocab at most
  *                  ABS_MAX_VOCAB (ABS_ERR_TOO_LARGE).  -inf masks an index, and so does a finite value far below the
@@ -723,8 +727,10 @@ int abs_rms_norm_grad(const abs_rms_norm_grad_args* args, abs_stream_t stream);
  *   sample_losses  device, n_samples floats (one without offsets), or NULL: sum of weight * loss over the sample's rows
  *   dlogits        the logits' type, or not given; may be the logits themselves
  *   temperature    1e-3 .. 1e3
- * Sums are formed in fp32 (over samples in fp64) in an order that depends on the shapes alone.  A NaN or
- * infinity (+inf among the logits) makes its row's loss and gradient NaN.  One launch, two with sample_losses.
+ * Sums are formed in fp32 (over samples in fp64) in an order that depends on shapes, types, strides, each row's distance
+ * from a 16-byte boundary, and dlogits' distance from the logits: the same call on buffers laid out alike gives the
+ * same bits, a copy at another alignment may not.  A NaN or infinity (+inf among the logits) makes its row's loss and
+ * gradient NaN.  One launch, two with sample_losses.
  * Bound by reading the logits once and writing the gradient once.
  */
 enum { ABS_MAX_TOP = 512, ABS_MAX_VOCAB = 1 << 20 };

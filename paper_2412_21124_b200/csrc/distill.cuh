@@ -105,8 +105,8 @@ __device__ __forceinline__ float block_sum(float x, float* room) {
 
 // Any vocabulary, any alignment: a block a row, which is read twice (the second time mostly from L2).  The top's
 // places are bits in shared memory.  For rows that do not fit a cluster's shared memory, and gradients at another
-// distance from 16-byte boundaries than the logits: where both kernels may be taken it needs 464 us against 218 (4096
-// rows of 50257, bf16, gradient) and 316 against 128 (8192 rows of 32000, f16, loss alone).
+// distance from 16-byte boundaries than the logits: where both kernels may be taken it needs 464 us against 220 (4096
+// rows of 50257, bf16, gradient) and 316 against 127 (8192 rows of 32000, f16, loss alone).
 template <int DT, int VEC>
 __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams p) {
   constexpr int E = lane_values<VEC>();

@@ -21,7 +21,7 @@
 // time, with and without the gradient; what is reached is 0.6 to 0.7 of the bandwidth, and the same without the loads or
 // without the stores: issue slots are half taken, the exponential unit a little less, and the rest is the chain of a
 // row (largest, sum, join, answer) that two rows under way do not cover.  bf16 with the gradient: 8192 rows of 128256,
-// a fifth of them without weight, 841 us, 4096 of 50257 218 us; f16, loss alone: 8192 of 32000 127 us.
+// a fifth of them without weight, 842 us, 4096 of 50257 220 us; f16, loss alone: 8192 of 32000 127 us.
 //
 // Every wait is bounded (see normtest_bulk.cuh).  A part whose wait runs out says nothing further to any mbarrier: a phase that
 // is still open must not be entered twice.  A feeder or a joiner stops there, so that the waits of those that it

@@ -8,8 +8,8 @@
 // it is normalised.
 //
 // Bounds: HBM where the output has 16 or 32 bits, 16384 x 2048 with an fp32 residual stream 61 us, 6.6 TB/s;
-// 524288 heads of 64 24 us, 5.6 TB/s.  In 8 bits with a scale for 32 values it is instruction issue (8192 x 8192 92 us,
-// 5.1 TB/s).  Two values in one instruction slot brought nothing: what they save goes into moving registers side by side.
+// 524288 heads of 64 23 us, 5.7 TB/s.  In 8 bits with a scale for 32 values (8192 x 8192 92 us, 5.1 TB/s) it is latency: issue
+// is 50% busy and DRAM 55%, with 15 warps an SM of 88 registers.  Two values in one instruction slot brought nothing: what they save goes into moving registers side by side.
 #pragma once
 #include "rows.cuh"
 

@@ -5,7 +5,8 @@
 //   dw_c of sample b = sum over the rows of b of dy_c u_c
 //
 // rstd is formed again from s, which the pass reads anyway: one sum more in a row's reduction instead of a
-// saved vector that has to fit its rows.
+// saved vector that has to fit its rows.  Here it is the approximate root as it comes, two units in the last place of fp32:
+// no result of 8 bits hangs on it, as in the forward pass.
 //
 // Every block takes an equal run of consecutive rows, so that the sums over rows stay in registers while it
 // walks them; it writes them once for each sample that it meets (a piece) and once for the whole run (a

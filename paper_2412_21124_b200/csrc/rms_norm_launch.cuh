@@ -65,11 +65,15 @@ cudaError_t launch_norm(const NormParams& p, int r_dtype, int vec, cudaStream_t 
 
 // ---- backward
 // A row of at most this many values goes to the lanes of a warp, two or four rows at once; one of at most kGradHalf to
-// threads of eight values, wider ones to threads of sixteen (9001 x 1537 f16: five us more with sixteen).
+// threads of eight values, wider ones to threads of sixteen (9001 x 1537 f16: five us more with sixteen; bf16 with an fp32
+// stream, the residual's gradient and 8 samples, 43662 x 1537 182 us, 206 with sixteen, 43690 x 1536 156 and 157, 32768 x 2048 147
+// and 148).
 constexpr int kGradHalf = 2048;
 constexpr int grad_lane_values(int vec) { return vec == 8 ? 256 : 128; }
 // Blocks of the kernel that sums over rows: as many as fit the SMs at once, but two rows a block at least, since every
 // block leaves a record: 512 x 2048 with 8 samples 15 us by 512 blocks, 11 by 256, 13 by 128, and 512 x 768 8.9, 7.8, 8.8.
+// Rows above 4096 take blocks of 512 or 1024 threads, one an SM: 8192 x 8192 164 us, 169 with two of 64 registers.  (13106 x
+// 5120 takes 197 us, and 177 with two; 4096 x 16384, of 1024 threads, 186.)
 inline int64_t grad_most_blocks(int64_t h, int vec) {
   return kSMs * (h <= 8 * 512 ? grad_blocks_per_sm(h > grad_lane_values(vec), vec, h <= kGradHalf) : 1);
 }

@@ -252,6 +252,26 @@ def test_gradient_against_differences():
             assert abs(3.0 * (up - down) / 2e-5 - float(dz[i, j])) <= 3e-6
 
 
+@pytest.mark.parametrize("vocab,top,more", ((50, 6, -0.5), (1000, 20, -0.1), (40, 40, 0.7), (300_000, 6, -0.3)))
+def test_gradient_where_the_teachers_mass_is_not_one(vocab, top, more):
+    """A log-sum-exp that is too small, and a top that is the whole vocabulary with less mass: what the header says the
+    gradient then is beside the loss's derivative, which autograd takes from the definition in fp64."""
+    z, ids, t = make(4, vocab, top, F32, gen(vocab), sure=1.0)
+    lse = torch.logsumexp(t, -1) + more
+    losses, dz = torch.empty(4, device=DEV), torch.empty_like(z)
+    absnt.abs_distill_loss(z, ids, t, losses, teacher_lse=lse, dlogits=dz)
+    leaf = z.double().requires_grad_()
+    log_q = torch.log_softmax(leaf, -1)
+    log_p = t.double() - lse.double()[:, None]
+    loss = (log_p.exp() * (log_p - log_q.gather(1, ids))).sum(-1)
+    derivative, = torch.autograd.grad(loss.sum(), leaf)
+    mass = log_p.exp().sum(-1, keepdim=True)
+    assert (mass > 1.05).all() if more < 0 else (mass < 0.95).all()
+    assert ((losses.double() - loss.detach()).abs() <= plain(z, ids, t, lse=lse)[1]).all()
+    want, err = derivative + log_q.detach().exp() * (1 - mass), plain(z, ids, t, lse=lse)[3]
+    assert ((dz.double() - want).abs() <= err + want.abs() * ROUND[F32] + STEP[F32]).all()
+
+
 @pytest.mark.parametrize("vocab,rows", ((50257, 300), (32000, 700), (1000, 3000), (4096, 2500), (128256, 150), (151936, 110),
                                         (300000, 20)))
 def test_the_same_every_time_on_another_stream_and_in_a_graph(vocab, rows):
