@@ -185,8 +185,19 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     }
   }
 
-  // y, piece by piece; the branches on the types are taken once for all of a thread's pieces.  (For outputs of 8 bits too: s w
-  // without rstd, or rstd and a scale's reciprocal as one factor, may leave the range of a float where y does not.)
+  // y, piece by piece; the branches on the types are taken once for all of a thread's pieces.
+  // For 8 bits rstd is 2^e f with f in [1, 2), and y / f is formed: s 2^e w, mostly without a rounding for 16-bit tensors (s rstd w
+  // falls to the other side of a tie a third more often), and a float wherever y is one (s w need not be).  So is f times
+  // the scale's reciprocal, which is at most 2^127.  An rstd of 0 has f = 1, a NaN an infinite power.
+  float frac[NR];
+  auto split_rstd = [&]() {
+#pragma unroll
+    for (int k = 0; k < NR; ++k) {
+      const uint32_t bits = __float_as_uint(rstd[k]);
+      frac[k] = __uint_as_float((bits & 0x007fffffu) | 0x3f800000u);
+      rstd[k] = __uint_as_float(bits & 0x7f800000u);
+    }
+  };
   auto normalise = [&]() {
     with_type(p.w_dtype, [&](auto wt) {
 #pragma unroll
@@ -202,7 +213,10 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
   };
   // before the branch on the output for rows of lanes (524288 heads of 64: 23.0 us, in either branch 23.7), in either branch for
   // rows of blocks (8192 x 8192 into 8 bits: 92.6 us, before it 94.2)
-  if constexpr (!BLOCK) normalise();
+  if constexpr (!BLOCK) {
+    if (p.scales) split_rstd();
+    normalise();
+  }
   if (!p.scales) {
     if constexpr (BLOCK) normalise();
     with_type(p.out_dtype, [&](auto ot) {
@@ -218,7 +232,10 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
   }
 
   // 8 bits: the largest |y| of each group
-  if constexpr (BLOCK) normalise();
+  if constexpr (BLOCK) {
+    split_rstd();
+    normalise();
+  }
   uint32_t a_row[NR];
 #pragma unroll
   for (int k = 0; k < NR; ++k) a_row[k] = 0u;
@@ -245,10 +262,10 @@ __global__ void __launch_bounds__(BLOCK ? (NI * lane_values<VEC>() > 16 ? 512 : 
     unsigned char* const po = row_of<VEC>(p.out, ri[k], rj[k]);
     auto scale_from = [&](uint32_t a, bool writer, int group) {
       float inv;
-      const uint32_t stored = scale_of(a, p.out_dtype, p.scale_dtype, inv);
+      const uint32_t stored = scale_of(__float_as_uint(__uint_as_float(a) * frac[k]) & 0x7fffffffu, p.out_dtype, p.scale_dtype, inv);
       if (writer && live)
         store_scale(p.scales, ri[k] * p.scale_s0 + rj[k] * p.scale_s1 + group * p.scale_s2, p.scale_dtype, stored);
-      return inv;
+      return inv * frac[k];
     };
     if (of_row) {
       const float inv = scale_from(a_row[k], l == 0 && warp == 0, 0);
